@@ -53,6 +53,7 @@ extern "C" {
 #define MOA_STATUS_APPEND_RANGE  1  /* append: pos[b] outside [0,n_max); that row was skipped */
 #define MOA_STATUS_SEQLEN_RANGE  2  /* decode: seq_lens[b] outside [1,n_max]; that item's out untouched */
 #define MOA_STATUS_WAIT_TIMEOUT  4  /* a bounded in-kernel wait expired; results of that call are invalid */
+#define MOA_STATUS_PAGE_RANGE    8  /* paged cache: a page number outside [0, num_pages) among the rows of a call */
 
 /*
  * Decode attention over a dense cache (problem statement of section 2; batch/head
@@ -213,6 +214,115 @@ int moa_decode_step_strided(const float *q, float *K, float *V, const float *k_n
                             const long long *k_strides, const long long *v_strides,
                             void *workspace, size_t workspace_bytes, void *stream);
 
+/* ==== paged caches ==================================================================
+ *
+ * A cache of many sequences as a pool of pages (section 5.3's pre-allocated cache, allocated a
+ * page at a time).  A page holds page_size consecutive rows of one sequence, for every kv head;
+ * a page table names the pages of each sequence in order:
+ *     row i of sequence b  =  row i % page_size of page  page_table[b][i / page_size].
+ * Element (page, h, r, t) of K lives at  k + page*k_strides[0] + h*k_strides[1] + r*k_strides[2] + t
+ * (element counts), likewise for V; the feature axis is contiguous.  Several sequences may name the
+ * same page (a shared prefix) as long as no call appends to it.
+ *
+ * Formats.  MOA_KV_F32, MOA_KV_BF16, MOA_KV_F16: rows of d elements of that type.
+ * MOA_KV_INT4: rows of d codes 0..15, two to a byte, feature 2i in the low half of byte i; strides
+ * count codes.  Every row has a pair of fp16 values (scale, least) beside it, at
+ * params[((page * h_kv + h) * page_size + r) * 2], and stands for  scale * code + least.
+ *
+ * d is 64 or 128, for K and V alike; page_size and num_pages are any positive numbers.  Pools are
+ * 16-byte aligned, strides non-negative multiples of 16 bytes (32 codes), at most 2^40, the row
+ * stride at least d; params are 4-byte aligned and dense.  The descriptor is HOST memory, read
+ * during the call.
+ */
+#define MOA_F32  0      /* element types of tensors */
+#define MOA_BF16 1
+#define MOA_F16  2
+#define MOA_KV_F32  0   /* formats of a paged cache */
+#define MOA_KV_BF16 1
+#define MOA_KV_F16  2
+#define MOA_KV_INT4 3
+typedef struct moa_paged_cache {
+    void *k, *v;                   /* pools */
+    void *k_params, *v_params;     /* MOA_KV_INT4 only (otherwise ignored) */
+    long long k_strides[3];        /* page, kv head, row */
+    long long v_strides[3];
+    int format;
+    int num_pages, page_size;
+    int h_kv, d;
+} moa_paged_cache;
+
+/*
+ * Append with the position rotation on the way (eqs. (4),(5) on a paged cache): the new rows of
+ * every sequence are stored behind the ones it has, the keys and the queries turned by their
+ * positions, in one pass and one launch.
+ *   q [tokens, h_q, d], k, v [tokens, h_kv, d], q_out [tokens, h_q, d]: type `dtype`, which is the
+ *       cache's own for 16 and 32 bits, MOA_BF16 or MOA_F16 for MOA_KV_INT4.
+ *   token_strides: HOST array of four element counts {q, k, v, q_out} between consecutive tokens (the heads of
+ *       a token are dense: slices of one projection's output are taken as they are), or NULL: dense.
+ *   h_q may be 0: then q and q_out are not touched (and may be NULL).  q_out may be q, with the same stride.
+ *   token_start: device int32[batch + 1], token_start[0] = 0, ascending: tokens [token_start[b],
+ *       token_start[b+1]) belong to sequence b; tokens behind token_start[batch] are left alone
+ *       (a padded batch).  NULL: token t is the one new token of sequence t (tokens == batch).
+ *   seq_lens: device int32[batch], the lengths WITH the new rows (what moa_paged_decode_attn is
+ *       then given): sequence b's token i of n lands in row seq_lens[b] - n + i, its position.
+ *   page_table: device int32[batch][max_pages].  Entries of pages that a call has no rows in are
+ *       not read.  The rows that a call writes are distinct: no page that takes new rows belongs
+ *       to two sequences (what such a row then holds is undefined; nothing else is).
+ *   cos_sin: device fp32 [rope_rows][rot_dim], row p: the rot_dim/2 cosines, then the sines, of
+ *       position p.  16-byte aligned.  Pair i of a head, (x, y), becomes (x cos - y sin, y cos + x sin):
+ *       features i and rot_dim/2 + i (MOA_ROPE_HALVES) or 2i and 2i + 1 (MOA_ROPE_PAIRS);
+ *       features from rot_dim on stay.  rot_dim is even, 0 <= rot_dim <= d; 0: no rotation, cos_sin
+ *       may be NULL.
+ * The arithmetic is fp32, each operation rounded, and one rounding to the stored type.  A 4-bit row has
+ *   scale = fp16((max - min) * fp32(1/15)), least = fp16(min), code = round_to_even((x - least) / scale) cut to 0..15
+ * (scale 0: code 0; values beyond +-65504 as if cut off there for scale and least; a row with a NaN or an infinity
+ * reads back as NaN).
+ * A token whose row is outside [0, max_pages*page_size), or whose position is not below rope_rows
+ * (when rot_dim > 0), sets MOA_STATUS_APPEND_RANGE; one whose page is outside [0, num_pages) sets
+ * MOA_STATUS_PAGE_RANGE: its rows are not stored and its part of q_out is left as it was.
+ * q, k, v, q_out are 16-byte aligned, token strides multiples of 16 bytes.  A stride of 0 is
+ * refused for what is written.
+ */
+#define MOA_ROPE_HALVES 0
+#define MOA_ROPE_PAIRS  1
+int moa_paged_append(const moa_paged_cache *cache, const void *q, const void *k, const void *v, void *q_out,
+                     int dtype, const long long *token_strides, int tokens, int h_q, int batch,
+                     const int32_t *token_start, const int32_t *seq_lens, const int32_t *page_table,
+                     int max_pages, const float *cos_sin, int rope_rows, int rot_dim, int rope_style,
+                     void *stream);
+
+/*
+ * Decode attention over a paged cache: Algorithm 1 for one query per sequence and head over rows
+ * [0, seq_lens[b]), with the head grouping of section 6.
+ *   q [batch, h_q, d], `q_stride` elements between sequences (a multiple of 16 bytes; 0: h_q * d);
+ *   out [batch, h_q, d], dense.  Both of type `dtype`: the cache's own for 16 and 32 bits, MOA_BF16
+ *   or MOA_F16 for MOA_KV_INT4.  16-byte aligned.
+ * Scores, softmax and sums are fp32; out is rounded once.  seq_lens and page_table are read on the
+ * device at execution time.  A sequence of length 0 (a padded batch) gets zeros.  A length below 0
+ * or above max_pages*page_size sets MOA_STATUS_SEQLEN_RANGE and leaves that item's out untouched; a page number outside
+ * [0, num_pages) among a sequence's rows sets MOA_STATUS_PAGE_RANGE, nothing outside the pools
+ * is read, and the rows of `out` that depend on it become NaN.
+ * `workspace`: as for moa_decode_attn_varlen, at least moa_paged_workspace_bytes(...) bytes.
+ * One launch; allocates nothing; can be captured into a CUDA graph after one uncaptured call.
+ */
+int moa_paged_decode_attn(const moa_paged_cache *cache, const void *q, void *out, int dtype, long long q_stride,
+                          int batch, int h_q, const int32_t *seq_lens, const int32_t *page_table,
+                          int max_pages, float scale, void *workspace, size_t workspace_bytes, void *stream);
+size_t moa_paged_workspace_bytes(int batch, int h_q, int h_kv, int d);
+
+/*
+ * Read rows back: rows [row_start[b], seq_lens[b]) of every sequence into
+ *   k_out, v_out [batch, h_kv, n_out, d], type `dtype` (any of the three, whatever the cache's format),
+ * dense and 16-byte aligned, from row 0 of each slab on; rows behind stay as they were.
+ * row_start: device int32[batch], or NULL: from row 0.  With MOA_F32 the result is the cache that
+ * the dense calls take.  A sequence with row_start < 0, more than n_out rows, a length
+ * below row_start or beyond the table sets MOA_STATUS_SEQLEN_RANGE and is left out; a row
+ * whose page number is outside [0, num_pages) sets MOA_STATUS_PAGE_RANGE and is left out.
+ */
+int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int dtype, int batch, int n_out,
+                     const int32_t *row_start, const int32_t *seq_lens, const int32_t *page_table,
+                     int max_pages, void *stream);
+
 /*
  * Host-buffer convenience call: q, K, V, out are HOST pointers (pinned memory gives
  * full copy bandwidth).  Copies the inputs to library-owned device staging buffers,
@@ -318,6 +428,7 @@ const char *moa_strerror(int code);
                                   fused step: 17..32) */
 #define MOA_PATH_MMA       4   /* streaming kernel with warp-level MMA, 8 or 16 heads per fetched row (larger groups in
                                   several passes), d_k, d_v in {64,128} */
+#define MOA_PATH_PAGED     5   /* reported only: the paged calls have one kernel family, never forced */
 int moa_set_option(int option, int value);
 int moa_last_path(void);
 

@@ -16,13 +16,35 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoa.so")
 
 OK, ERR_INVALID, ERR_UNSUPPORTED, ERR_ALIGN, ERR_CAPACITY, ERR_WORKSPACE, ERR_CUDA = range(7)
-STATUS_APPEND_RANGE, STATUS_SEQLEN_RANGE, STATUS_WAIT_TIMEOUT = 1, 2, 4
+STATUS_APPEND_RANGE, STATUS_SEQLEN_RANGE, STATUS_WAIT_TIMEOUT, STATUS_PAGE_RANGE = 1, 2, 4, 8
 OPT_FORCE_PATH, OPT_NUM_CTAS, OPT_GROUPED_HEADS, OPT_DEPENDENT_LAUNCH, OPT_GROUPED_OPERANDS = 1, 2, 3, 4, 5
 OPT_WAIT_LIMIT, OPT_TEST_SKIP_COPY = 7, 8
 NOALLOC_SCRATCH_BYTES = 4 << 20
-PATH_AUTO, PATH_GENERIC, PATH_STREAM, PATH_GROUPED, PATH_MMA = 0, 1, 2, 3, 4
+PATH_AUTO, PATH_GENERIC, PATH_STREAM, PATH_GROUPED, PATH_MMA, PATH_PAGED = 0, 1, 2, 3, 4, 5
+F32, BF16, F16 = 0, 1, 2                               # element types of tensors
+KV_F32, KV_BF16, KV_F16, KV_INT4 = 0, 1, 2, 3          # formats of a paged cache
+ROPE_HALVES, ROPE_PAIRS = 0, 1
 
 _lib = None
+
+
+class PagedCache(C.Structure):
+    """``moa_paged_cache``: where the pages of a cache are and how their rows are held.
+
+    ``k``, ``v`` (and ``k_params``, ``v_params`` of a 4-bit cache) are tensors or addresses; the object
+    keeps the tensors alive.  Strides are (page, kv head, row) element counts; the default is dense
+    ``[num_pages, h_kv, page_size, d]``.
+    """
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_params", C.c_void_p), ("v_params", C.c_void_p),
+                ("k_strides", C.c_longlong * 3), ("v_strides", C.c_longlong * 3), ("format", C.c_int),
+                ("num_pages", C.c_int), ("page_size", C.c_int), ("h_kv", C.c_int), ("d", C.c_int)]
+
+    def __init__(self, format, k, v, num_pages, page_size, h_kv, d, k_strides=None, v_strides=None, k_params=None,
+                 v_params=None):
+        dense = (h_kv * page_size * d, page_size * d, d)
+        super().__init__(_ptr(k), _ptr(v), _ptr(k_params), _ptr(v_params), _strides3(k_strides or dense),
+                         _strides3(v_strides or dense), format, num_pages, page_size, h_kv, d)
+        self.tensors = (k, v, k_params, v_params)
 
 
 class MoaError(RuntimeError):
@@ -57,6 +79,12 @@ def lib():
         L.moa_kv_append_strided.argtypes = [p, p, p, p, p, i, i, i, i, i, ll3, ll3, p]
         L.moa_decode_step_strided.argtypes = [p, p, p, p, p, p, p, i, i, i, i, i, i, f, ll3, ll3, p, sz, p]
         L.moa_decode_attn_host.argtypes = [p, p, p, p, i, i, i, i, i, i, f]
+        pc = C.POINTER(PagedCache)
+        L.moa_paged_append.argtypes = [pc, p, p, p, p, i, p, i, i, i, p, p, p, i, p, i, i, i, p]
+        L.moa_paged_decode_attn.argtypes = [pc, p, p, i, C.c_longlong, i, i, p, p, i, f, p, sz, p]
+        L.moa_paged_workspace_bytes.argtypes = [i, i, i, i]
+        L.moa_paged_workspace_bytes.restype = sz
+        L.moa_paged_gather.argtypes = [pc, p, p, i, i, i, p, p, p, i, p]
         L.moa_device_status.argtypes = [p, C.POINTER(C.c_int)]
         L.moa_min_bytes.argtypes = [i, i, i, C.c_longlong, i, i]
         L.moa_min_bytes.restype = C.c_longlong
@@ -201,6 +229,38 @@ def moa_decode_step_strided(q, K, V, k_new, v_new, out, lens, batch, h_q, h_kv, 
                                          _ptr(lens), batch, h_q, h_kv, n_max, d_k, d_v, scale,
                                          _strides3(k_strides), _strides3(v_strides), _ptr(workspace),
                                          workspace_bytes, _stream(stream)), "moa_decode_step_strided")
+
+
+def moa_paged_append(cache, q, k, v, q_out, dtype, token_strides, tokens, h_q, batch, token_start, seq_lens,
+                     page_table, max_pages, cos_sin, rope_rows, rot_dim, rope_style, stream=None):
+    """Store new rows behind the ones each sequence has, keys and queries turned by their positions.
+    token_strides: None (dense) or element counts between tokens of (q, k, v, q_out)."""
+    if token_strides is not None:
+        if len(token_strides) != 4:
+            raise ValueError("token strides are (q, k, v, q_out) element counts")
+        token_strides = (C.c_longlong * 4)(*[int(x) for x in token_strides])
+    _check(lib().moa_paged_append(cache, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), dtype, token_strides, tokens, h_q,
+                                  batch, _ptr(token_start), _ptr(seq_lens), _ptr(page_table), max_pages,
+                                  _ptr(cos_sin), rope_rows, rot_dim, rope_style, _stream(stream)),
+           "moa_paged_append")
+
+
+def moa_paged_decode_attn(cache, q, out, dtype, q_stride, batch, h_q, seq_lens, page_table, max_pages, scale,
+                          workspace, workspace_bytes, stream=None):
+    _check(lib().moa_paged_decode_attn(cache, _ptr(q), _ptr(out), dtype, q_stride, batch, h_q, _ptr(seq_lens),
+                                       _ptr(page_table), max_pages, scale, _ptr(workspace), workspace_bytes,
+                                       _stream(stream)), "moa_paged_decode_attn")
+
+
+def moa_paged_workspace_bytes(batch, h_q, h_kv, d) -> int:
+    return int(lib().moa_paged_workspace_bytes(batch, h_q, h_kv, d))
+
+
+def moa_paged_gather(cache, k_out, v_out, dtype, batch, n_out, row_start, seq_lens, page_table, max_pages,
+                     stream=None):
+    """Rows [row_start[b], seq_lens[b]) of every sequence into k_out, v_out [batch, h_kv, n_out, d]."""
+    _check(lib().moa_paged_gather(cache, _ptr(k_out), _ptr(v_out), dtype, batch, n_out, _ptr(row_start),
+                                  _ptr(seq_lens), _ptr(page_table), max_pages, _stream(stream)), "moa_paged_gather")
 
 
 def moa_decode_attn_host(q, K, V, out, batch, h_q, h_kv, n, d_k, d_v, scale):

@@ -15,6 +15,8 @@
 #include "moa_mma.cuh"
 #include "moa_grouped.cuh"
 #include "moa_grouped64.cuh"
+#include "moa_paged.cuh"
+#include "moa_paged_io.cuh"
 
 namespace moa {
 
@@ -864,6 +866,270 @@ static int decode_impl(const float *q, const float *K, const float *V, float *ou
 static __device__ __align__(256) unsigned char g_noalloc_scratch[MOA_NOALLOC_SCRATCH_BYTES];
 static void *g_noalloc_scratch_dev[kMaxDevices] = {};   // resolved device address, per device
 
+// ---- paged caches --------------------------------------------------------------------------
+static int element_bytes(int dtype) { return dtype == MOA_F32 ? 4 : 2; }
+
+// The descriptor's own rules; strides in bytes through `ks` and `vs`.
+static int check_paged(const moa_paged_cache *c, long long *ks, long long *vs, bool written)
+{
+    if (!c || !c->k || !c->v) return MOA_ERR_INVALID;
+    if (c->format < MOA_KV_F32 || c->format > MOA_KV_INT4) return MOA_ERR_INVALID;
+    if (c->num_pages < 1 || c->page_size < 1 || c->h_kv < 1 || c->d < 1) return MOA_ERR_INVALID;
+    const bool q4 = c->format == MOA_KV_INT4;
+    if (q4 && (!c->k_params || !c->v_params)) return MOA_ERR_INVALID;
+    if (c->d != 64 && c->d != 128) return MOA_ERR_UNSUPPORTED;
+    const long long *st[2] = {c->k_strides, c->v_strides};
+    long long *to[2] = {ks, vs};
+    bool wide = true;
+    for (int i = 0; i < 2; ++i) {
+        for (int e = 0; e < 3; ++e) {
+            if (st[i][e] < 0 || st[i][e] > (1LL << 40)) return MOA_ERR_INVALID;
+            if (written && st[i][e] == 0 && (e == 2 || (e == 0 ? c->num_pages : c->h_kv) > 1)) return MOA_ERR_INVALID;
+            to[i][e] = q4 ? st[i][e] / 2 : st[i][e] * element_bytes(c->format);
+            if (q4 ? st[i][e] % 32 != 0 : to[i][e] % 16 != 0) wide = false;
+        }
+        if (st[i][2] < c->d) return MOA_ERR_INVALID;
+    }
+    if (!wide || !aligned(c->k, 16) || !aligned(c->v, 16)) return MOA_ERR_ALIGN;
+    if (q4 && (!aligned(c->k_params, 4) || !aligned(c->v_params, 4))) return MOA_ERR_ALIGN;
+    return MOA_OK;
+}
+
+// Tensors have the cache's own type; a 4-bit cache takes the two 16-bit types.
+static bool paged_dtype_ok(int format, int dtype)
+{
+    return format == MOA_KV_INT4 ? (dtype == MOA_BF16 || dtype == MOA_F16) : dtype == format;
+}
+
+static int page_shift_of(int page_size)
+{
+    for (int s = 0; s < 31; ++s)
+        if (page_size == (1 << s)) return s;
+    return -1;
+}
+
+// Query heads of one pass over a unit's rows: 8, or 16 for the larger groups of the 16- and 4-bit
+// formats (fp32 keeps its query in 64 registers per 8 heads, so it takes 8 at a time and reads the
+// rows of a larger group again, from L2).
+static int paged_heads(int format, int g) { return format != MOA_KV_F32 && g > 8 ? 16 : 8; }
+
+static int paged_grid(const DeviceState &s)
+{
+    return g_num_ctas > 0 ? (g_num_ctas < kTicketCtas ? g_num_ctas : kTicketCtas) : (s.sm_count < kTicketCtas ? s.sm_count : kTicketCtas);
+}
+
+static size_t paged_slot_bytes(int grid, int heads, int d)
+{
+    return ((size_t)grid * 2 * heads * (d + 4) * sizeof(float) + 255) / 256 * 256;
+}
+
+template <class C>
+static cudaError_t launch_paged_cfg(const PagedArgs &a, int grid, cudaStream_t st)
+{
+    static bool attr_set[kMaxDevices] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(paged_decode_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)C::SMEM_BYTES);
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
+    {
+        TimedLaunch t(st);
+        launch_dependent(paged_decode_kernel<C>, grid, C::THREADS, C::SMEM_BYTES, st, a);
+    }
+    count_launch();
+    return cudaGetLastError();
+}
+
+template <int D>
+static cudaError_t launch_paged(int format, int heads, const PagedArgs &a, int grid, cudaStream_t st)
+{
+    constexpr bool wide = D == 128;        //                                            NT  W   S
+    switch (format) {
+    case MOA_KV_F32: return launch_paged_cfg<PagedCfg<MOA_KV_F32, D, 1, wide ? 6 : 8, 2>>(a, grid, st);
+    case MOA_KV_BF16:
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 1, 8, wide ? 2 : 4>>(a, grid, st);
+        return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 2, 8, wide ? 2 : 4>>(a, grid, st);
+    case MOA_KV_F16:
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 1, 8, wide ? 2 : 4>>(a, grid, st);
+        return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 2, 8, wide ? 2 : 4>>(a, grid, st);
+    default:
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 16, wide ? 4 : 6>>(a, grid, st);
+        return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 12, wide ? 4 : 6>>(a, grid, st);
+    }
+}
+
+static int paged_decode_impl(const moa_paged_cache *c, const void *q, void *out, int dtype, long long q_stride,
+                             int batch, int h_q, const int32_t *seq_lens, const int32_t *page_table, int max_pages,
+                             float scale, void *ws, size_t ws_bytes, cudaStream_t st)
+{
+    if (!c || !q || !out || !seq_lens || !page_table) return MOA_ERR_INVALID;
+    if (batch < 1 || h_q < 1 || max_pages < 1 || !isfinite(scale) || q_stride < 0) return MOA_ERR_INVALID;
+    PagedArgs a = {};
+    long long ks[3], vs[3];
+    int rc = check_paged(c, ks, vs, false);
+    if (rc != MOA_OK) return rc;
+    if (h_q % c->h_kv != 0 || dtype < MOA_F32 || dtype > MOA_F16) return MOA_ERR_INVALID;
+    if (!paged_dtype_ok(c->format, dtype)) return MOA_ERR_UNSUPPORTED;
+    if (q_stride == 0) q_stride = (long long)h_q * c->d;
+    if (q_stride > (1LL << 40)) return MOA_ERR_INVALID;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(seq_lens, 4) || !aligned(page_table, 4) ||
+        q_stride * element_bytes(dtype) % 16 != 0)
+        return MOA_ERR_ALIGN;
+    if ((long long)batch * h_q > 0x7fffffffLL) return MOA_ERR_CAPACITY;
+    if (!ws) return MOA_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return MOA_ERR_ALIGN;
+    DeviceState *dev = nullptr;
+    rc = current_device(&dev);
+    if (rc != MOA_OK) return rc;
+    const int g = h_q / c->h_kv, heads = paged_heads(c->format, g), grid = paged_grid(*dev);
+    const size_t slots = paged_slot_bytes(grid, heads, c->d);
+    if (ws_bytes < slots + kTicketBytes) return MOA_ERR_WORKSPACE;
+
+    a.k = static_cast<const unsigned char *>(c->k); a.v = static_cast<const unsigned char *>(c->v);
+    a.kp = static_cast<const uint32_t *>(c->k_params); a.vp = static_cast<const uint32_t *>(c->v_params);
+    a.k_sp = ks[0]; a.k_sh = ks[1]; a.k_sr = ks[2];
+    a.v_sp = vs[0]; a.v_sh = vs[1]; a.v_sr = vs[2];
+    a.num_pages = c->num_pages; a.page_size = c->page_size;
+    a.page_shift = page_shift_of(c->page_size); a.one_page = c->page_size % 16 == 0;
+    a.table = page_table; a.max_pages = max_pages; a.seq_lens = seq_lens;
+    const long long cap = (long long)max_pages * c->page_size;
+    a.len_max = cap < 0x7fffffffLL - 16 ? (int)cap : 0x7fffffff - 16;
+    a.q = q; a.out = out; a.q_sb = q_stride; a.dtype = dtype;
+    a.batch = batch; a.h_q = h_q; a.h_stored = c->h_kv;
+    a.share = (g + heads - 1) / heads;
+    a.g_s = (g + a.share - 1) / a.share;
+    a.g_total = g;
+    a.qscale = scale * kLog2e;
+    a.ws = static_cast<float *>(ws);
+    a.tickets = reinterpret_cast<unsigned long long *>(static_cast<unsigned char *>(ws) + slots);
+    unsigned long long tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
+    if (tag == 0) tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
+    a.ticket_tag = (tag << 20) | 1ull;
+    const cudaError_t e = c->d == 128 ? launch_paged<128>(c->format, heads, a, grid, st) : launch_paged<64>(c->format, heads, a, grid, st);
+    if (e != cudaSuccess) return MOA_ERR_CUDA;
+    g_last_path = MOA_PATH_PAGED;
+    return MOA_OK;
+}
+
+static PagedIoArgs paged_io_args(const moa_paged_cache *c, const long long *ks, const long long *vs, int batch,
+                                 const int32_t *seq_lens, const int32_t *page_table, int max_pages)
+{
+    PagedIoArgs a = {};
+    a.k_pool = static_cast<unsigned char *>(c->k); a.v_pool = static_cast<unsigned char *>(c->v);
+    a.kp = static_cast<uint32_t *>(c->k_params); a.vp = static_cast<uint32_t *>(c->v_params);
+    a.k_sp = ks[0]; a.k_sh = ks[1]; a.k_sr = ks[2];
+    a.v_sp = vs[0]; a.v_sh = vs[1]; a.v_sr = vs[2];
+    a.num_pages = c->num_pages; a.page_size = c->page_size; a.page_shift = page_shift_of(c->page_size); a.h_kv = c->h_kv;
+    a.table = page_table; a.max_pages = max_pages; a.batch = batch; a.seq_lens = seq_lens;
+    return a;
+}
+
+template <int FMT, int DT>
+static cudaError_t launch_append(const PagedIoArgs &a, int d, cudaStream_t st)
+{
+    const int heads = a.h_q + 2 * a.h_kv, runs = (heads + a.heads_per_thread - 1) / a.heads_per_thread;
+    const long long rows = (long long)a.tokens * runs, per_block = 256 / (d / 16);
+    const int blocks = (int)((rows + per_block - 1) / per_block);
+    if (d == 128) launch_dependent(paged_append_kernel<FMT, DT, 128>, blocks, 256, 0, st, a);
+    else launch_dependent(paged_append_kernel<FMT, DT, 64>, blocks, 256, 0, st, a);
+    count_launch();
+    return cudaGetLastError();
+}
+
+static int paged_append_impl(const moa_paged_cache *c, const void *q, const void *k, const void *v, void *q_out, int dtype,
+                             const long long *ts, int tokens, int h_q, int batch, const int32_t *token_start,
+                             const int32_t *seq_lens, const int32_t *page_table, int max_pages, const float *cos_sin,
+                             int rope_rows, int rot_dim, int rope_style, cudaStream_t st)
+{
+    if (!c || !k || !v || !seq_lens || !page_table) return MOA_ERR_INVALID;
+    if (tokens < 1 || h_q < 0 || batch < 1 || max_pages < 1) return MOA_ERR_INVALID;
+    if (h_q > 0 && (!q || !q_out)) return MOA_ERR_INVALID;
+    long long ks[3], vs[3];
+    int rc = check_paged(c, ks, vs, true);
+    if (rc != MOA_OK) return rc;
+    if (dtype < MOA_F32 || dtype > MOA_F16 || h_q % c->h_kv != 0) return MOA_ERR_INVALID;
+    if (!paged_dtype_ok(c->format, dtype)) return MOA_ERR_UNSUPPORTED;
+    if (rot_dim < 0 || rot_dim > c->d || rot_dim % 2 != 0) return MOA_ERR_INVALID;
+    if (rot_dim > 0 && (!cos_sin || rope_rows < 1 || (rope_style != MOA_ROPE_HALVES && rope_style != MOA_ROPE_PAIRS))) return MOA_ERR_INVALID;
+    if (!token_start && tokens != batch) return MOA_ERR_INVALID;
+    const long long dense[4] = {(long long)h_q * c->d, (long long)c->h_kv * c->d, (long long)c->h_kv * c->d, (long long)h_q * c->d};
+    long long s[4];
+    const int es = element_bytes(dtype);
+    bool wide = true;
+    for (int i = 0; i < 4; ++i) {
+        s[i] = ts ? ts[i] : dense[i];
+        if (h_q == 0 && (i == 0 || i == 3)) { s[i] = 0; continue; }
+        if (s[i] < 0 || s[i] > (1LL << 40)) return MOA_ERR_INVALID;
+        if (i == 3 && s[i] < dense[i] && tokens > 1) return MOA_ERR_INVALID;      // rows of q_out may not overlap
+        if (s[i] * es % 16 != 0) wide = false;
+    }
+    if (h_q > 0 && q == q_out && s[0] != s[3]) return MOA_ERR_INVALID;
+    if (!wide || !aligned(k, 16) || !aligned(v, 16) || !aligned(seq_lens, 4) || !aligned(page_table, 4) ||
+        (h_q > 0 && (!aligned(q, 16) || !aligned(q_out, 16))) || (token_start && !aligned(token_start, 4)) ||
+        (rot_dim > 0 && !aligned(cos_sin, 16)))
+        return MOA_ERR_ALIGN;
+    const long long rows = (long long)tokens * (h_q + 2LL * c->h_kv);
+    if (h_q + 2LL * c->h_kv > 0x7fffffffLL || rows > 0x7fffffffLL * 16) return MOA_ERR_CAPACITY;
+    DeviceState *dev = nullptr;
+    rc = current_device(&dev);
+    if (rc != MOA_OK) return rc;
+    PagedIoArgs a = paged_io_args(c, ks, vs, batch, seq_lens, page_table, max_pages);
+    a.q = q; a.k = k; a.v = v; a.q_out = q_out;
+    a.q_st = s[0]; a.k_st = s[1]; a.v_st = s[2]; a.o_st = s[3];
+    a.tokens = tokens; a.h_q = h_q; a.token_start = token_start;
+    a.cos_sin = cos_sin; a.rope_rows = rope_rows; a.rot = rot_dim; a.pairs = rope_style == MOA_ROPE_PAIRS;
+    a.heads_per_thread = rows >= 32768 ? 4 : 1;
+    cudaError_t e;
+    switch (c->format) {
+    case MOA_KV_F32: e = launch_append<MOA_KV_F32, MOA_F32>(a, c->d, st); break;
+    case MOA_KV_BF16: e = launch_append<MOA_KV_BF16, MOA_BF16>(a, c->d, st); break;
+    case MOA_KV_F16: e = launch_append<MOA_KV_F16, MOA_F16>(a, c->d, st); break;
+    default:
+        e = dtype == MOA_BF16 ? launch_append<MOA_KV_INT4, MOA_BF16>(a, c->d, st) : launch_append<MOA_KV_INT4, MOA_F16>(a, c->d, st);
+    }
+    return e == cudaSuccess ? MOA_OK : MOA_ERR_CUDA;
+}
+
+template <int D>
+static cudaError_t launch_gather(int format, const PagedIoArgs &a, int dtype, cudaStream_t st)
+{
+    const long long rows = (long long)a.batch * a.h_kv * a.n_out, per_block = 256 / (D / 8);
+    const int blocks = (int)((rows + per_block - 1) / per_block);
+    switch (format) {
+    case MOA_KV_F32: launch_dependent(paged_gather_kernel<MOA_KV_F32, D>, blocks, 256, 0, st, a, dtype); break;
+    case MOA_KV_BF16: launch_dependent(paged_gather_kernel<MOA_KV_BF16, D>, blocks, 256, 0, st, a, dtype); break;
+    case MOA_KV_F16: launch_dependent(paged_gather_kernel<MOA_KV_F16, D>, blocks, 256, 0, st, a, dtype); break;
+    default: launch_dependent(paged_gather_kernel<MOA_KV_INT4, D>, blocks, 256, 0, st, a, dtype);
+    }
+    count_launch();
+    return cudaGetLastError();
+}
+
+static int paged_gather_impl(const moa_paged_cache *c, void *k_out, void *v_out, int dtype, int batch, int n_out,
+                             const int32_t *row_start, const int32_t *seq_lens, const int32_t *page_table, int max_pages,
+                             cudaStream_t st)
+{
+    if (!c || !k_out || !v_out || !seq_lens || !page_table) return MOA_ERR_INVALID;
+    if (batch < 1 || n_out < 1 || max_pages < 1 || dtype < MOA_F32 || dtype > MOA_F16) return MOA_ERR_INVALID;
+    long long ks[3], vs[3];
+    int rc = check_paged(c, ks, vs, false);
+    if (rc != MOA_OK) return rc;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(seq_lens, 4) || !aligned(page_table, 4) ||
+        (row_start && !aligned(row_start, 4)))
+        return MOA_ERR_ALIGN;
+    if ((double)batch * c->h_kv * n_out > 2147483647.0 * 16) return MOA_ERR_CAPACITY;
+    DeviceState *dev = nullptr;
+    rc = current_device(&dev);
+    if (rc != MOA_OK) return rc;
+    PagedIoArgs a = paged_io_args(c, ks, vs, batch, seq_lens, page_table, max_pages);
+    a.k_out = k_out; a.v_out = v_out; a.row_start = row_start; a.n_out = n_out;
+    const cudaError_t e = c->d == 128 ? launch_gather<128>(c->format, a, dtype, st) : launch_gather<64>(c->format, a, dtype, st);
+    return e == cudaSuccess ? MOA_OK : MOA_ERR_CUDA;
+}
+
 }  // namespace moa
 
 using namespace moa;
@@ -1144,6 +1410,45 @@ int moa_decode_step_strided(const float *q, float *K, float *V, const float *k_n
         return MOA_ERR_INVALID;
     return step_impl(q, K, V, k_new, v_new, out, lens, lens, batch, h_q, h_kv, n_max, d_k, d_v, scale,
                      workspace, workspace_bytes, stream, true, &lay);
+}
+
+int moa_paged_append(const moa_paged_cache *cache, const void *q, const void *k, const void *v, void *q_out, int dtype,
+                     const long long *token_strides, int tokens, int h_q, int batch, const int32_t *token_start,
+                     const int32_t *seq_lens, const int32_t *page_table, int max_pages, const float *cos_sin,
+                     int rope_rows, int rot_dim, int rope_style, void *stream)
+{
+    Lock lock(g_mu);
+    return paged_append_impl(cache, q, k, v, q_out, dtype, token_strides, tokens, h_q, batch, token_start, seq_lens,
+                             page_table, max_pages, cos_sin, rope_rows, rot_dim, rope_style, static_cast<cudaStream_t>(stream));
+}
+
+int moa_paged_decode_attn(const moa_paged_cache *cache, const void *q, void *out, int dtype, long long q_stride, int batch,
+                          int h_q, const int32_t *seq_lens, const int32_t *page_table, int max_pages, float scale,
+                          void *workspace, size_t workspace_bytes, void *stream)
+{
+    Lock lock(g_mu);
+    return paged_decode_impl(cache, q, out, dtype, q_stride, batch, h_q, seq_lens, page_table, max_pages, scale, workspace,
+                             workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+size_t moa_paged_workspace_bytes(int batch, int h_q, int h_kv, int d)
+{
+    Lock lock(g_mu);
+    if (batch < 1 || h_q < 1 || h_kv < 1 || h_q % h_kv != 0 || (d != 64 && d != 128)) return 0;
+    DeviceState *dev = nullptr;
+    DeviceState plain;
+    plain.sm_count = 256;                  // no device: an upper bound
+    const int grid = paged_grid(current_device(&dev) == MOA_OK ? *dev : plain);
+    return paged_slot_bytes(grid, paged_heads(MOA_KV_BF16, h_q / h_kv), d) + (kTicketBytes + 255) / 256 * 256;
+}
+
+int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int dtype, int batch, int n_out,
+                     const int32_t *row_start, const int32_t *seq_lens, const int32_t *page_table, int max_pages,
+                     void *stream)
+{
+    Lock lock(g_mu);
+    return paged_gather_impl(cache, k_out, v_out, dtype, batch, n_out, row_start, seq_lens, page_table, max_pages,
+                             static_cast<cudaStream_t>(stream));
 }
 
 int moa_decode_attn_host(const float *q, const float *K, const float *V, float *out, int batch,

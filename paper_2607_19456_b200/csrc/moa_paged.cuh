@@ -1,0 +1,880 @@
+// moa_paged.cuh -- single-query attention over a paged cache held in fp32, bf16, fp16 or 4 bits.
+//
+// Steps I-III of Algorithm 1 in online-softmax form, as in the streaming kernels, on a cache whose
+// rows are found through a page table.  What is different here:
+//
+//  - Work is dealt to WARPS.  The cached rows of every (sequence, kv head) unit are cut into tiles
+//    of 16 rows; all tiles form one flat list, cut into equal contiguous ranges first for the CTAs,
+//    then for the warps of a CTA.  A unit that lies inside one warp's range never leaves the warp;
+//    only the (at most two) units that a range cuts go through shared memory, once, at the end of
+//    the CTA.  Small caches (16 and 4 bits) have units that take a CTA a microsecond or two; a block
+//    barrier for every unit, as the fp32 streaming kernels have, would cost as much again.
+//  - Tiles come through per-lane 16-byte asynchronous copies into a ring of the warp's own: rows of
+//    one page are a few hundred bytes to a few KB, less than a bulk copy needs to be worth its issue
+//    (one per 70 cycles and SM), and a page may end inside a tile.  The page numbers of a tile are
+//    read while the tile before it is issued.
+//  - Both products run on the warp-level MMA with the cached operand as A (16 rows or 16 features),
+//    heads as the 8 columns: S[16 rows x 8 heads] = K Q^T, O^T[16 features x 8 heads] += V^T P^T.
+//    A query group of one head to eight costs the same; what bounds the kernel is the copy.
+//
+// Number formats of the products:
+//  - bf16, fp16: the stored values are the A operand; q is the B operand as it is (the scale is
+//    applied to the fp32 score).  The probabilities are split into two 16-bit terms, p = hi + lo,
+//    so that their rounding (2^-9 for bf16) does not add to the one rounding of the output.
+//  - fp32: both operands split into two tf32 terms, three products (hi*hi, hi*lo, lo*hi), short chains.
+//  - 4 bits: a code c in 0..15 is used as the fp16 bit pattern c, the subnormal c * 2^-24: unpacking
+//    is one AND for two codes (another for the codes four bits up, which come out 16 times as large).
+//    The score of a row is scale * (s * <q, c> + m * sum(q)) with the row's (s, m); in the weighted
+//    sum the weight of a row is p * s, and sum(p * m) is kept beside it.  q is brought to fp16 by a
+//    power of two per head (exact but for terms 2^-38 of the largest); the weights are brought into
+//    fp16's range by a power of two that follows the largest s seen.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "moa_device.cuh"
+#include "moa_mma.cuh"
+
+namespace moa {
+
+struct PagedArgs {
+    const unsigned char *k, *v;      // pools
+    const uint32_t *kp, *vp;         // 4-bit rows: (scale, least) pairs, [num_pages][h_stored][page_size]
+    long long k_sp, k_sh, k_sr;      // byte strides: page, kv head, row
+    long long v_sp, v_sh, v_sr;
+    int num_pages, page_size;
+    int page_shift;                  // log2(page_size), or -1
+    int one_page;                    // page_size % 16 == 0: a tile lies in one page
+    const int32_t *table;            // [batch, max_pages]
+    int max_pages;
+    const int32_t *seq_lens;         // [batch]
+    int len_max;                     // min(max_pages * page_size, INT_MAX)
+    const void *q;
+    void *out;
+    long long q_sb;                  // elements between the queries of consecutive sequences
+    int dtype;                       // of q and out (MOA_F32, MOA_BF16, MOA_F16)
+    int batch, h_q, h_stored;
+    int share;                       // virtual kv heads per stored one
+    int g_s;                         // query heads per virtual kv head
+    int g_total;                     // query heads per stored kv head
+    float qscale;                    // scale * log2(e)
+    float *ws;                       // two partial slots per CTA
+    unsigned long long *tickets;
+    unsigned long long ticket_tag;
+};
+
+// W warps, S ring stages of 16 rows (K and V) each.  The ring and the slots of the first cut unit
+// share the 227 KB of an SM; the slot of the last cut unit is the ring itself, empty by then.
+template <int FMT_, int D_, int NT_, int W_, int S_>
+struct PagedCfg {
+    static constexpr int FMT = FMT_, D = D_, NT = NT_, W = W_, S = S_;
+    static constexpr int THREADS = W * 32, R = 16;
+    static constexpr int ROWB = FMT == MOA_KV_F32 ? 4 * D : FMT == MOA_KV_INT4 ? D / 2 : 2 * D;   // bytes of a row
+    static constexpr int CPR = ROWB / 16;                  // 16-byte chunks of a row
+    static constexpr int NCH = R * CPR / 32;               // chunks a lane copies per tile and operand
+    static constexpr int KB = R * ROWB;                    // bytes of one operand's tile
+    static constexpr int STAGE = 2 * KB + (FMT == MOA_KV_INT4 ? 2 * R * 4 : 0);
+    static constexpr int MT = D / 16;                      // 16-feature output tiles
+    static constexpr int G = 8 * NT;                       // heads of a unit
+    static constexpr int PS = D + 4;                       // floats of a partial: o[D], m, l, 2 pad
+    static constexpr int SLOT = G * PS;                    // floats of a unit's partial
+    static constexpr int KSTEPS = FMT == MOA_KV_F32 ? D / 8 : D / 16;
+    static constexpr int QREGS = FMT == MOA_KV_F32 ? 4 : 2;    // B registers per k-step (fp32: two terms)
+    static constexpr size_t OFF_FIRST = (size_t)W * S * STAGE;
+    static constexpr size_t OFF_PREF = OFF_FIRST + sizeof(float) * (size_t)W * SLOT;
+    static constexpr size_t SMEM_BYTES = OFF_PREF + sizeof(long long) * (THREADS + 1);
+    static_assert(W <= 16, "two segments per warp have to fit a warp's lanes");
+    static_assert((size_t)S * STAGE >= sizeof(float) * SLOT, "the ring holds the last partial");
+    static_assert(OFF_FIRST % 16 == 0 && OFF_PREF % 16 == 0, "alignment of the regions");
+    static_assert(SMEM_BYTES <= 227 * 1024 - 2048, "shared memory of an SM, less the static part");
+};
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool full)
+{
+    const int n = full ? 16 : 0;                           // 0: the 16 bytes are zero-filled, src is not read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void *src, bool full)
+{
+    const int n = full ? 4 : 0;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+template <bool BF16>
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                            uint32_t b0, uint32_t b1)
+{
+    if (BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Two floats as one register of 16-bit values (lo in the low half), and the values they were rounded to.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi)
+{
+    uint32_t r;
+    if (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <bool BF16>
+__device__ __forceinline__ float2 unpack16(uint32_t r)
+{
+    if (BF16) return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&r));
+}
+// One element of a tensor of `dtype` as a float, and four floats into one.
+__device__ __forceinline__ float load_as_float(const void *p, long long i, int dtype)
+{
+    if (dtype == MOA_F32) return static_cast<const float *>(p)[i];
+    if (dtype == MOA_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    return __half2float(static_cast<const __half *>(p)[i]);
+}
+__device__ __forceinline__ void store4(void *p, long long i, const float4 &v, int dtype)
+{
+    if (dtype == MOA_F32) *reinterpret_cast<float4 *>(static_cast<float *>(p) + i) = v;
+    else {
+        const uint2 r = dtype == MOA_BF16 ? make_uint2(pack16<true>(v.x, v.y), pack16<true>(v.z, v.w))
+                                          : make_uint2(pack16<false>(v.x, v.y), pack16<false>(v.z, v.w));
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p) + i) = r;
+    }
+}
+__device__ __forceinline__ void store1(void *p, long long i, float v, int dtype)
+{
+    if (dtype == MOA_F32) static_cast<float *>(p)[i] = v;
+    else if (dtype == MOA_BF16) static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
+    else static_cast<__half *>(p)[i] = __float2half_rn(v);
+}
+
+__device__ __forceinline__ int paged_len(const PagedArgs &a, int b)       // 0: nothing to attend to
+{
+    const int len = a.seq_lens[b];
+    return (len >= 1 && len <= a.len_max) ? len : 0;
+}
+
+// Query head that is head g of virtual kv head vh of sequence b; -1: padding (or no such sequence).
+__device__ __forceinline__ int paged_query_head(const PagedArgs &a, int b, int vh, int g)
+{
+    const int in_stored = (vh % a.share) * a.g_s + g;
+    return (g < a.g_s && in_stored < a.g_total && b < a.batch) ? (vh / a.share) * a.g_total + in_stored : -1;
+}
+
+// A place in the flat list: tile i of the ub tiles of unit (b, h).
+struct TileCursor {
+    int b, h, i, ub, len;
+};
+__device__ __forceinline__ void tile_advance(const PagedArgs &a, int hv, TileCursor &c)
+{
+    if (++c.i < c.ub) return;
+    c.i = 0;
+    if (++c.h < hv) return;
+    c.h = 0;
+    do {
+        if (++c.b >= a.batch) { c.b = a.batch; c.len = 0; c.ub = 1; return; }
+        c.len = paged_len(a, c.b);
+    } while (c.len == 0);
+    c.ub = (c.len + 15) >> 4;
+}
+
+// Registers of one warp's unit: accumulators of O^T, reference maxima, sums.
+template <class C>
+struct PagedState {
+    float acc[C::NT][C::MT][4];
+    float m[C::NT][2], msub[C::NT][2], l[C::NT][2];        // heads 8n + 2t and 8n + 2t + 1; msub: m, or 0 while m is -inf
+    float om[C::NT][2];                                    // 4 bits: sum of p * least
+    float ref;                                             // 4 bits: power of two, at least every row's scale so far
+};
+
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const PagedArgs a)
+{
+    constexpr int FMT = C::FMT, D = C::D, NT = C::NT, W = C::W, S = C::S, MT = C::MT, PS = C::PS, G = C::G;
+    constexpr bool BF = FMT == MOA_KV_BF16, Q4 = FMT == MOA_KV_INT4, F32 = FMT == MOA_KV_F32;
+    extern __shared__ __align__(128) unsigned char smem[];
+    float *first_slots = reinterpret_cast<float *>(smem + C::OFF_FIRST);
+    long long *s_pref = reinterpret_cast<long long *>(smem + C::OFF_PREF);
+    __shared__ long long s_warp[16];
+    __shared__ long long s_seg[32];                        // unit of segment 2 * warp + (0: first, 1: last), or -1
+    __shared__ long long s_seg_lo[32];                     // flat index of that unit's first tile
+    __shared__ int s_seg_ub[32], s_seg_vh[32];             // its tiles, its virtual kv head (with the sequence in s_seg_b)
+    __shared__ int s_seg_b[32];
+    __shared__ int s_grp_lo[32], s_grp_hi[32], s_ngrp, s_last;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int hv = a.h_stored * a.share;
+    const int dtype = F32 ? MOA_F32 : FMT == MOA_KV_BF16 ? MOA_BF16 : FMT == MOA_KV_F16 ? MOA_F16 : a.dtype;
+
+    launch_dependents();
+    grid_dependency_wait();
+
+    // ---- lengths: tiles per sequence, prefix over the threads' runs of sequences -----------
+    const int per_thread = (a.batch + C::THREADS - 1) / C::THREADS;
+    long long mine = 0;
+    bool empty = false;
+    for (int i = 0; i < per_thread; ++i) {
+        const int b = tid * per_thread + i;
+        if (b >= a.batch) break;
+        const int len = a.seq_lens[b];
+        const bool here = (unsigned)b % gridDim.x == blockIdx.x;
+        if (len < 0 || len > a.len_max) { if (here) raise_status(MOA_STATUS_SEQLEN_RANGE); }
+        else { mine += (len + 15) >> 4; empty |= (len == 0 && here); }
+    }
+    long long inc = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, inc, off);
+        if (lane >= off) inc += x;
+    }
+    if (lane == 31) s_warp[warp] = inc;
+    if (tid < 32) s_seg[tid] = -1;
+    const int any_empty = __syncthreads_or(empty);
+    long long before = 0, total1 = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (w < warp) before += s_warp[w];
+        total1 += s_warp[w];
+    }
+    s_pref[tid] = before + inc - mine;
+    if (tid == 0) s_pref[C::THREADS] = total1;
+    if (any_empty) {                                       // a sequence without rows: zeros
+        const long long row_bytes = (long long)a.h_q * D * (dtype == MOA_F32 ? 4 : 2);
+        for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
+            if (a.seq_lens[b] == 0)
+                for (long long i = tid; i < row_bytes / 16; i += C::THREADS)
+                    reinterpret_cast<uint4 *>(static_cast<unsigned char *>(a.out) + (long long)b * row_bytes)[i] =
+                        make_uint4(0u, 0u, 0u, 0u);
+    }
+    __syncthreads();
+    const long long total = total1 * hv;
+    // A CTA takes at least W tiles: a cut costs a partial, a counter round trip and a merge.
+    long long active = (total + W - 1) / W;
+    if (active > gridDim.x) active = gridDim.x;
+    if (blockIdx.x >= active) return;                      // (also when there is nothing to do)
+    const long long c0 = total * blockIdx.x / active, c1 = total * (blockIdx.x + 1) / active;
+    const long long j0 = c0 + (c1 - c0) * warp / W, j1 = c0 + (c1 - c0) * (warp + 1) / W;
+
+    unsigned char *ring = smem + (size_t)warp * S * C::STAGE;
+    const uint32_t ring_u = smem_u32(ring);
+
+    if (j0 < j1) {
+        // ---- the tile that the range begins with ------------------------------------------
+        TileCursor cc;
+        long long unit_lo;                                 // flat index of the current unit's first tile
+        {
+            int lo = 0, hi = C::THREADS;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s_pref[mid] * hv <= j0) lo = mid; else hi = mid;
+            }
+            long long at = s_pref[lo] * hv;
+            int b = lo * per_thread, ub = 0, len = 0;
+            for (; b < a.batch; ++b) {                     // ends before: j0 < total
+                len = paged_len(a, b);
+                ub = (len + 15) >> 4;
+                if (j0 < at + (long long)ub * hv) break;
+                at += (long long)ub * hv;
+            }
+            cc.b = b; cc.len = len; cc.ub = ub; cc.h = cc.i = 0;
+            if (b < a.batch) { cc.h = (int)((j0 - at) / ub); cc.i = (int)((j0 - at) % ub); }
+            else cc.len = 0, cc.ub = 1;                    // (lengths that changed meanwhile: no rows, no output)
+            unit_lo = j0 - cc.i;
+        }
+        TileCursor lc = cc;
+        long long jl = j0;
+        int load_stage = 0;
+        unsigned bad_stages = 0;
+
+        // Page number of this lane's row (lane & 15) of the tile under `lc`; -1 behind the last row.
+        auto fetch_page = [&]() -> int {
+            const int row = lc.i * 16 + (lane & 15);
+            if (row >= lc.len) return -1;
+            const int p = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size;
+            return __ldg(a.table + (long long)lc.b * a.max_pages + p);
+        };
+        int page = fetch_page();
+
+        auto issue = [&]() {                               // copies of the tile under `lc`, then on to the next
+            const uint32_t st = ring_u + load_stage * C::STAGE;
+            const int row0 = lc.i * 16, nr = min(16, lc.len - row0);
+            const int hs = lc.h / a.share;
+            const bool bad = (lane & 15) < nr && (unsigned)page >= (unsigned)a.num_pages;
+            if (__any_sync(0xffffffffu, bad)) {
+                bad_stages |= 1u << load_stage;
+                if (lane == 0) raise_status(MOA_STATUS_PAGE_RANGE);
+                if (bad) page = -1;
+            } else bad_stages &= ~(1u << load_stage);
+            const int my_row = row0 + (lane & 15);
+            const int my_off = a.page_shift >= 0 ? my_row & (a.page_size - 1) : my_row % a.page_size;
+            const unsigned char *kh = a.k + hs * a.k_sh, *vh = a.v + hs * a.v_sh;
+            const unsigned char *k1 = nullptr, *v1 = nullptr;      // the tile's first row, where it lies in one page
+            if (a.one_page) {
+                const long long pg = __shfl_sync(0xffffffffu, page, 0), off0 = __shfl_sync(0xffffffffu, my_off, 0);
+                k1 = kh + pg * a.k_sp + off0 * a.k_sr;
+                v1 = vh + pg * a.v_sp + off0 * a.v_sr;
+            }
+            const int c = lane % C::CPR;
+#pragma unroll
+            for (int i = 0; i < C::NCH; ++i) {
+                const int r = lane / C::CPR + i * (32 / C::CPR);
+                const int pg = __shfl_sync(0xffffffffu, page, r), off = __shfl_sync(0xffffffffu, my_off, r);
+                const bool ok = pg >= 0;
+                const unsigned char *kr, *vr;
+                if (a.one_page) { kr = k1 + (ok ? r * a.k_sr : 0); vr = v1 + (ok ? r * a.v_sr : 0); }
+                else { kr = kh + (long long)(ok ? pg : 0) * a.k_sp + off * a.k_sr; vr = vh + (long long)(ok ? pg : 0) * a.v_sp + off * a.v_sr; }
+                uint32_t kd, vd;                           // places in the tile: what keeps the reads free of bank conflicts
+                if constexpr (Q4) {
+                    const int slot = (r & 8) | ((r & 3) << 1) | ((r >> 2) & 1);
+                    kd = slot * C::ROWB + c * 16;
+                    vd = r * C::ROWB + ((c * 16) ^ (D == 128 ? ((r >> 1) & 1) << 5 : 0));
+                } else if constexpr (F32) {
+                    kd = r * C::ROWB + ((c ^ ((r & 1) << 2)) << 4);
+                    vd = r * C::ROWB + ((c ^ ((r & 3) << 1)) << 4);
+                } else {
+                    kd = vd = r * C::ROWB + ((c ^ (r & 7)) << 4);
+                }
+                cp16(st + kd, ok ? kr + c * 16 : a.k, ok);
+                cp16(st + C::KB + vd, ok ? vr + c * 16 : a.v, ok);
+            }
+            if (Q4) {
+                const bool ok = page >= 0;
+                const uint32_t *src = (lane < 16 ? a.kp : a.vp) +
+                                      (ok ? ((long long)page * a.h_stored + hs) * a.page_size + my_off : 0);
+                cp4(st + 2 * C::KB + lane * 4, src, ok);
+            }
+            if (++load_stage == S) load_stage = 0;
+            ++jl;
+            if (jl < j1) {
+                tile_advance(a, hv, lc);
+                page = fetch_page();
+            }
+        };
+#pragma unroll 1
+        for (int i = 0; i < S; ++i) {
+            if (jl < j1) issue();
+            cp_commit();
+        }
+
+        // ---- the unit's query and state ----------------------------------------------------
+        uint32_t qf[NT][C::KSTEPS][C::QREGS];
+        float fa[NT][2], fm[NT][2];                        // 4 bits: factors of <q, c> and of the least value
+        PagedState<C> s;
+        auto begin_unit = [&]() {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int qh = paged_query_head(a, cc.b, cc.h, 8 * n + g);
+                const long long base = (long long)cc.b * a.q_sb + (long long)qh * D;
+                if constexpr (F32) {
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (qh >= 0) x = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + base + 4 * (t + 4 * i));
+                        const Split4 sp = split4(x);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            qf[n][2 * i + e][0] = sp.h[2 * e]; qf[n][2 * i + e][1] = sp.h[2 * e + 1];
+                            qf[n][2 * i + e][C::QREGS - 2] = sp.l[2 * e]; qf[n][2 * i + e][C::QREGS - 1] = sp.l[2 * e + 1];
+                        }
+                    }
+                } else if constexpr (!Q4) {
+                    const uint16_t *q = static_cast<const uint16_t *>(a.q) + base;
+#pragma unroll
+                    for (int i = 0; i < C::KSTEPS; ++i) {
+                        qf[n][i][0] = qh >= 0 ? *reinterpret_cast<const uint32_t *>(q + 16 * i + 2 * t) : 0u;
+                        qf[n][i][1] = qh >= 0 ? *reinterpret_cast<const uint32_t *>(q + 16 * i + 2 * t + 8) : 0u;
+                    }
+                } else {
+                    // Lane t holds features [t * D/4, (t+1) * D/4) of head g, in the order of the codes' words.
+                    float most = 0.f, sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < D / 4; ++i) {
+                        const float x = qh >= 0 ? load_as_float(a.q, base + t * (D / 4) + i, dtype) : 0.f;
+                        most = fmaxf(most, fabsf(x));
+                        sum += x;
+                    }
+#pragma unroll
+                    for (int off = 1; off < 4; off <<= 1) {
+                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+                        sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                    }
+                    // largest magnitude into [2^13, 2^14)
+                    int e = 13 - ((int)((__float_as_uint(most) >> 23) & 255u) - 127);
+                    e = e > 100 ? 100 : e < -100 ? -100 : e;
+                    const float up = __uint_as_float((uint32_t)(127 + e) << 23), up16 = up * 0.0625f;
+#pragma unroll
+                    for (int i = 0; i < C::KSTEPS; ++i) {
+                        float x[4] = {0.f, 0.f, 0.f, 0.f};
+                        const long long at = base + t * (D / 4) + 8 * (i / 2) + 2 * (i & 1);
+                        if (qh >= 0) {
+                            x[0] = load_as_float(a.q, at, dtype); x[1] = load_as_float(a.q, at + 4, dtype);
+                            x[2] = load_as_float(a.q, at + 1, dtype); x[3] = load_as_float(a.q, at + 5, dtype);
+                        }
+                        qf[n][i][0] = pack16<false>(x[0] * up, x[1] * up);
+                        qf[n][i][1] = pack16<false>(x[2] * up16, x[3] * up16);
+                    }
+                    const float down = __uint_as_float((uint32_t)(127 - e) << 23) * 16777216.0f * a.qscale;
+                    sum *= a.qscale;
+#pragma unroll
+                    for (int e2 = 0; e2 < 2; ++e2) {       // of heads 8n + 2t + e2: held by lanes with g = 2t + e2
+                        fa[n][e2] = __shfl_sync(0xffffffffu, down, (2 * t + e2) * 4);
+                        fm[n][e2] = __shfl_sync(0xffffffffu, sum, (2 * t + e2) * 4);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s.acc[n][i][e] = 0.f;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) { s.m[n][e] = -INFINITY; s.msub[n][e] = 0.f; s.l[n][e] = 0.f; s.om[n][e] = 0.f; }
+            }
+            s.ref = 5.9604644775390625e-8f;                // 2^-24, fp16's least positive value
+        };
+
+        // ---- one tile: scores, probabilities, weighted sum ----------------------------------
+        auto process = [&](uint32_t st, int nr, bool bad) {
+            float x[NT][4];
+            float2 vpar[2] = {};                           // 4 bits: V's (scale, least) of this lane's two rows
+            const uint32_t sv = st + C::KB;
+            if constexpr (F32) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[n][e] = 0.f;
+                float lh[NT][4] = {}, hl[NT][4] = {};
+#pragma unroll
+                for (int i4 = 0; i4 < D / 16; i4 += 2) {   // chains of four large products, added in fp32
+                    float hh[NT][4] = {};
+#pragma unroll
+                    for (int i = i4; i < i4 + 2; ++i) {
+                        const int ch = (t + 4 * i) ^ ((g & 1) << 2);
+                        float4 r0, r1;
+                        const unsigned char *p = ring + (st - ring_u) + g * C::ROWB + ch * 16;
+                        r0 = *reinterpret_cast<const float4 *>(p);
+                        r1 = *reinterpret_cast<const float4 *>(p + 8 * C::ROWB);
+                        const Split4 s0 = split4(r0), s1 = split4(r1);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t ah[4] = {s0.h[2 * e], s1.h[2 * e], s0.h[2 * e + 1], s1.h[2 * e + 1]};
+                            const uint32_t al[4] = {s0.l[2 * e], s1.l[2 * e], s0.l[2 * e + 1], s1.l[2 * e + 1]};
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+                                mma3(hh[n], lh[n], hl[n], ah, al, qf[n][2 * i + e][0], qf[n][2 * i + e][1],
+                                     qf[n][2 * i + e][C::QREGS - 2], qf[n][2 * i + e][C::QREGS - 1]);
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[n][e] += hh[n][e];
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[n][e] = (x[n][e] + (lh[n][e] + hl[n][e])) * a.qscale;
+            } else if constexpr (!Q4) {
+                float c[NT][4] = {};
+#pragma unroll
+                for (int i = 0; i < C::KSTEPS; ++i) {
+                    uint32_t r[4];
+                    ldsm4(r, st + (lane & 15) * C::ROWB + (((2 * i + (lane >> 4)) ^ (lane & 7)) << 4));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma_16x8x16<BF>(c[n], r[0], r[1], r[2], r[3], qf[n][i][0], qf[n][i][1]);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[n][e] = c[n][e] * a.qscale;
+            } else {
+                constexpr int NW = D / 32;
+                uint32_t w0[NW], w1[NW];
+                const unsigned char *p = ring + (st - ring_u) + g * C::ROWB + t * (D / 8);
+                if constexpr (NW == 4) {
+                    *reinterpret_cast<uint4 *>(w0) = *reinterpret_cast<const uint4 *>(p);
+                    *reinterpret_cast<uint4 *>(w1) = *reinterpret_cast<const uint4 *>(p + 8 * C::ROWB);
+                } else {
+                    *reinterpret_cast<uint2 *>(w0) = *reinterpret_cast<const uint2 *>(p);
+                    *reinterpret_cast<uint2 *>(w1) = *reinterpret_cast<const uint2 *>(p + 8 * C::ROWB);
+                }
+                const int tok = ((g & 1) << 2) | (g >> 1); // the row that score row g stands for (score row g + 8: 8 more)
+                const __half2 *par = reinterpret_cast<const __half2 *>(ring + (st - ring_u) + 2 * C::KB);
+                const float2 k0 = __half22float2(par[tok]), k1 = __half22float2(par[tok + 8]);
+                vpar[0] = __half22float2(par[16 + tok]);
+                vpar[1] = __half22float2(par[16 + tok + 8]);
+                float c[NT][4] = {};
+#pragma unroll
+                for (int w = 0; w < NW; ++w)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t u0 = e ? w0[w] >> 8 : w0[w], u1 = e ? w1[w] >> 8 : w1[w];
+                        const uint32_t a0 = u0 & 0x000f000fu, a2 = u0 & 0x00f000f0u, a1 = u1 & 0x000f000fu, a3 = u1 & 0x00f000f0u;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma_16x8x16<false>(c[n], a0, a1, a2, a3, qf[n][2 * w + e][0], qf[n][2 * w + e][1]);
+                    }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        x[n][e] = fmaf(k0.x, c[n][e] * fa[n][e], k0.y * fm[n][e]);
+                        x[n][2 + e] = fmaf(k1.x, c[n][2 + e] * fa[n][e], k1.y * fm[n][e]);
+                    }
+            }
+            if (nr < 16) {                                 // rows behind the last one
+                const int r0 = Q4 ? ((g & 1) << 2) | (g >> 1) : g;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (r0 >= nr) x[n][e] = -INFINITY;
+                        if (r0 + 8 >= nr) x[n][2 + e] = -INFINITY;
+                    }
+            }
+            // The reference maximum moves only when a score exceeds it by more than 8 (a factor of
+            // 256, far inside the range of every format used here): rarely after the first tiles.
+            bool up = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) up |= x[n][e] > s.m[n][e & 1] + 8.0f;
+            if (Q4) up |= vpar[0].x > s.ref || vpar[1].x > s.ref;
+            if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = fmaxf(x[n][e], x[n][2 + e]);
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                        const float m_new = fmaxf(s.m[n][e], top);
+                        const float alpha = exp2_diff(s.m[n][e], m_new);
+                        s.m[n][e] = m_new;
+                        s.msub[n][e] = m_new == -INFINITY ? 0.f : m_new;
+                        s.l[n][e] *= alpha;
+                        if (Q4) s.om[n][e] *= alpha;
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) { s.acc[n][i][e] *= alpha; s.acc[n][i][2 + e] *= alpha; }
+                    }
+                if (Q4) {
+                    float top = fmaxf(vpar[0].x, vpar[1].x);
+#pragma unroll
+                    for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                    if (top > s.ref) {                     // next power of two (2^16 at most: scales are fp16)
+                        const float r = __uint_as_float((__float_as_uint(top) + 0x7fffffu) & 0x7f800000u);
+                        const float f = s.ref / r;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) s.acc[n][i][e] *= f;
+                        s.ref = r;
+                    }
+                }
+            }
+            if (bad) {                                     // a row whose page does not exist: the unit's result is NaN
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s.l[n][0] = s.l[n][1] = __int_as_float(0x7fffffff);
+            }
+            float p[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[n][e] = fast_exp2(x[n][e] - s.msub[n][e & 1]);
+                    s.l[n][e & 1] += p[n][e];
+                }
+            if constexpr (F32) {
+                float4 vr[2][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    // P^T as B operand: row t (+4) of each 8-row half, head g
+                    uint32_t bh[4], bl[4];                 // rows t, t+4, 8+t, 12+t
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const int src = (t + (h & 1) * 4) * 4 + (g >> 1);
+                        const float y0 = __shfl_sync(0xffffffffu, p[n][(h >> 1) * 2], src);
+                        const float y1 = __shfl_sync(0xffffffffu, p[n][(h >> 1) * 2 + 1], src);
+                        const float y = (g & 1) ? y1 : y0;
+                        bh[h] = (__float_as_uint(y) + 0x1000u) & 0xFFFFE000u;
+                        bl[h] = (__float_as_uint(y - __uint_as_float(bh[h])) + 0x1000u) & 0xFFFFE000u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            const int r = t + (h & 1) * 4 + (h >> 1) * 8;
+                            const int ch = (g + 8 * i) ^ ((r & 3) << 1);
+                            vr[h >> 1][h & 1] = *reinterpret_cast<const float4 *>(ring + (sv - ring_u) + r * C::ROWB + ch * 16);
+                        }
+                        Split4 v[2][2];
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) v[h >> 1][h & 1] = split4(vr[h >> 1][h & 1]);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {      // output tile 2i + e: features 4(g + 8i) + 2e, + 1
+                            float hh[4] = {}, lh[4] = {}, hl[4] = {};
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const uint32_t ah[4] = {v[k][0].h[2 * e], v[k][0].h[2 * e + 1], v[k][1].h[2 * e], v[k][1].h[2 * e + 1]};
+                                const uint32_t al[4] = {v[k][0].l[2 * e], v[k][0].l[2 * e + 1], v[k][1].l[2 * e], v[k][1].l[2 * e + 1]};
+                                mma3(hh, lh, hl, ah, al, bh[2 * k], bh[2 * k + 1], bl[2 * k], bl[2 * k + 1]);
+                            }
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) s.acc[n][2 * i + e][z] += hh[z] + (lh[z] + hl[z]);
+                        }
+                    }
+                }
+            } else if constexpr (!Q4) {
+                uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t r = pack16<BF>(p[n][2 * h], p[n][2 * h + 1]);
+                        const float2 f = unpack16<BF>(r);
+                        hi[n][h] = movmatrix_trans(r);
+                        lo[n][h] = movmatrix_trans(pack16<BF>(p[n][2 * h] - f.x, p[n][2 * h + 1] - f.y));
+                    }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    uint32_t r[4];
+                    const int row = (lane & 7) + ((lane >> 4) << 3);
+                    ldsm4t(r, sv + row * C::ROWB + (((2 * i + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma_16x8x16<BF>(s.acc[n][i], r[0], r[1], r[2], r[3], lo[n][0], lo[n][1]);
+                        mma_16x8x16<BF>(s.acc[n][i], r[0], r[1], r[2], r[3], hi[n][0], hi[n][1]);
+                    }
+                }
+            } else {
+                const float inv = 128.0f / s.ref;          // exact: a power of two; weights reach 2^15 at most
+                const float s0 = vpar[0].x * inv, s1 = vpar[1].x * inv;
+                uint32_t wt[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    wt[n][0] = movmatrix_trans(pack16<false>(p[n][0] * s0, p[n][1] * s0));
+                    wt[n][1] = movmatrix_trans(pack16<false>(p[n][2] * s1, p[n][3] * s1));
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) s.om[n][e] += fmaf(p[n][e], vpar[0].y, p[n][2 + e] * vpar[1].y);
+                }
+                constexpr int NW = D / 64;
+                uint32_t w[4][NW];                         // rows t, 4 + t, 8 + t, 12 + t: what the weights' columns stand for
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const int r = t + 4 * h;
+                    const unsigned char *src = ring + (sv - ring_u) + r * C::ROWB + ((g * (D / 16)) ^ (D == 128 ? ((r >> 1) & 1) << 5 : 0));
+                    if constexpr (NW == 2) *reinterpret_cast<uint2 *>(w[h]) = *reinterpret_cast<const uint2 *>(src);
+                    else w[h][0] = *reinterpret_cast<const uint32_t *>(src);
+                }
+#pragma unroll
+                for (int i = 0; i < NW; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {          // output tile 4i + e: features 2e and 2e + 1 of the word
+                        uint32_t u0 = __byte_perm(w[0][i], w[1][i], e < 2 ? 0x5410 : 0x7632);
+                        uint32_t u1 = __byte_perm(w[2][i], w[3][i], e < 2 ? 0x5410 : 0x7632);
+                        if (e & 1) { u0 >>= 8; u1 >>= 8; }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            mma_16x8x16<false>(s.acc[n][4 * i + e], u0 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x000f000fu,
+                                               u1 & 0x00f000f0u, wt[n][0], wt[n][1]);
+                    }
+            }
+        };
+
+        // ---- end of a unit, or of this warp's part of it ------------------------------------
+        // Feature of accumulator (i, half h): 16-bit: 16i + 8h + g; fp32: 4(g + 8(i/2)) + 2(i%2) + h;
+        // 4 bits: g * D/8 + 8(i/4) + 2(i%4) + h.  dst: a partial slot, or null for the output row.
+        auto close = [&](float *dst) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float l = s.l[n][e], om = s.om[n][e];
+#pragma unroll
+                    for (int off = 4; off < 32; off <<= 1) {
+                        l += __shfl_xor_sync(0xffffffffu, l, off);
+                        if (Q4) om += __shfl_xor_sync(0xffffffffu, om, off);
+                    }
+                    const int head = 8 * n + 2 * t + e;
+                    float f0 = 1.f, f1 = 1.f, add = 0.f;   // of the features that come from the low and the high codes
+                    if (Q4) { f0 = s.ref * 131072.0f; f1 = s.ref * 8192.0f; add = om; }
+                    long long at = -1;
+                    if (dst != nullptr) {
+                        if (g == 0) { dst[head * PS + D] = s.m[n][e]; dst[head * PS + D + 1] = l; }
+                    } else {
+                        const int qh = paged_query_head(a, cc.b, cc.h, head);
+                        if (qh >= 0) at = ((long long)cc.b * a.h_q + qh) * D;
+                        const float inv = 1.0f / l;
+                        f0 *= inv; f1 *= inv; add *= inv;
+                    }
+                    auto val = [&](int i, int h) { return fmaf(s.acc[n][i][2 * h + e], h ? f1 : f0, add); };
+                    if (Q4 || F32) {
+#pragma unroll
+                        for (int i = 0; i < MT; i += 2) {
+                            const float4 v4 = make_float4(val(i, 0), val(i, 1), val(i + 1, 0), val(i + 1, 1));
+                            const int d = Q4 ? g * (D / 8) + 2 * i : 4 * (g + 4 * i);
+                            if (dst != nullptr) *reinterpret_cast<float4 *>(dst + head * PS + d) = v4;
+                            else if (at >= 0) store4(a.out, at + d, v4, dtype);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < MT; ++i)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const int d = 16 * i + 8 * h + g;
+                                if (dst != nullptr) dst[head * PS + d] = val(i, h);
+                                else if (at >= 0) store1(a.out, at + d, val(i, h), dtype);
+                            }
+                    }
+                }
+        };
+
+        int stage = 0;
+        bool fresh = true;
+#pragma unroll 1
+        for (long long j = j0; j < j1; ++j) {
+            if (fresh) { begin_unit(); fresh = false; }
+            cp_wait<S - 1>();
+            __syncwarp();
+            process(ring_u + stage * C::STAGE, min(16, cc.len - cc.i * 16), (bad_stages >> stage) & 1u);
+            __syncwarp();                                  // every lane is done with the stage
+            if (++stage == S) stage = 0;
+            if (jl < j1) issue();
+            cp_commit();
+            const bool unit_ends = cc.i + 1 == cc.ub;
+            if (unit_ends || j + 1 == j1) {
+                const bool whole = unit_ends && unit_lo >= j0;
+                if (whole) close(nullptr);
+                else {
+                    const int which = j + 1 == j1 ? 1 : 0; // a cut unit that ends before the range does is its first
+                    if (which) { cp_wait<0>(); __syncwarp(); }
+                    close(which ? reinterpret_cast<float *>(ring) : first_slots + (size_t)warp * C::SLOT);
+                    if (lane == 0) {
+                        const int sg = 2 * warp + which;
+                        s_seg[sg] = (long long)cc.b * hv + cc.h;
+                        s_seg_lo[sg] = unit_lo; s_seg_ub[sg] = cc.ub; s_seg_vh[sg] = cc.h; s_seg_b[sg] = cc.b;
+                    }
+                }
+                if (unit_ends) { unit_lo += cc.ub; fresh = true; }
+            }
+            if (j + 1 < j1) tile_advance(a, hv, cc);
+        }
+    }
+    __syncthreads();
+
+    // ---- join the pieces of units that this CTA's warps share -------------------------------
+    if (warp == 0) {
+        const long long u = s_seg[lane];
+        const unsigned valid = __ballot_sync(0xffffffffu, u >= 0);
+        const unsigned below = valid & ((1u << lane) - 1u);
+        const int prev = below ? 31 - __clz(below) : lane;
+        const long long pu = __shfl_sync(0xffffffffu, u, prev);
+        const bool leads = u >= 0 && (below == 0 || pu != u);
+        const unsigned leaders = __ballot_sync(0xffffffffu, leads);
+        if (leads) {
+            const int k = __popc(leaders & ((1u << lane) - 1u));
+            const unsigned above = lane < 31 ? leaders >> (lane + 1) : 0u;
+            s_grp_lo[k] = lane;
+            s_grp_hi[k] = above ? lane + __ffs(above) : 32;
+        }
+        if (lane == 0) s_ngrp = __popc(leaders);
+    }
+    __syncthreads();
+    constexpr int LPR = D / 4, COLS = G * LPR;
+    auto seg_slot = [&](int sg) -> const float * {
+        const int w = sg >> 1;
+        return (sg & 1) ? reinterpret_cast<const float *>(smem + (size_t)w * S * C::STAGE) : first_slots + (size_t)w * C::SLOT;
+    };
+    const int ngrp = s_ngrp;
+    for (int idx = tid; idx < ngrp * COLS; idx += C::THREADS) {
+        const int k = idx / COLS, col = idx % COLS, head = col / LPR, d = (col % LPR) * 4;
+        const int lo = s_grp_lo[k], hi = s_grp_hi[k];
+        float M = -INFINITY;
+        for (int sg = lo; sg < hi; ++sg)
+            if (s_seg[sg] >= 0) M = fmaxf(M, seg_slot(sg)[head * PS + D]);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float L = 0.f;
+        for (int sg = lo; sg < hi; ++sg) {
+            if (s_seg[sg] < 0) continue;
+            const float *p = seg_slot(sg) + head * PS;
+            const float f = exp2_diff(p[D], M);
+            const float4 y = *reinterpret_cast<const float4 *>(p + d);
+            o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
+            L = fmaf(f, p[D + 1], L);
+        }
+        const long long ulo = s_seg_lo[lo], uhi = ulo + s_seg_ub[lo];
+        if (ulo >= c0 && uhi <= c1) {
+            const int qh = paged_query_head(a, s_seg_b[lo], s_seg_vh[lo], head);
+            const float inv = 1.0f / L;
+            if (qh >= 0)
+                store4(a.out, ((long long)s_seg_b[lo] * a.h_q + qh) * D + d,
+                       make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), dtype);
+        } else {
+            float *p = a.ws + ((size_t)blockIdx.x * 2 + (ulo <= c0 ? 0 : 1)) * C::SLOT + head * PS;
+            *reinterpret_cast<float4 *>(p + d) = o;
+            if (d == 0) { p[D] = M; p[D + 1] = L; }
+        }
+    }
+
+    // ---- units cut between CTAs: whoever delivers the last piece joins them ------------------
+    for (int k = 0; k < ngrp; k += (ngrp > 1 ? ngrp - 1 : 1)) {       // only the first and the last group can be cut
+        const int sg = s_grp_lo[k];
+        const long long ulo = s_seg_lo[sg], uhi = ulo + s_seg_ub[sg];
+        if (ulo >= c0 && uhi <= c1) continue;              // uniform for the CTA
+        const int first = (int)(((ulo + 1) * active - 1) / total), last = (int)((uhi * active - 1) / total);
+        __syncthreads();                                   // the pieces are written; s_last is free
+        if (tid == 0) {
+            __threadfence();
+            const int done = ticket_arrive(&a.tickets[first], a.ticket_tag) == (unsigned)(last - first);
+            if (done) a.tickets[first] = 0ull;
+            s_last = done;
+        }
+        __syncthreads();
+        if (!s_last) continue;
+        __threadfence();
+        const int b = s_seg_b[sg], vh = s_seg_vh[sg];
+        for (int col = tid; col < COLS; col += C::THREADS) {
+            const int head = col / LPR, d = (col % LPR) * 4;
+            auto slot = [&](int c) -> const float * {      // slot 0 of a CTA: the unit that its range begins in
+                return a.ws + ((size_t)c * 2 + (c > first || ulo == total * c / active ? 0 : 1)) * C::SLOT + head * PS;
+            };
+            float M = -INFINITY;
+#pragma unroll 4
+            for (int c = first; c <= last; ++c) M = fmaxf(M, __ldcg(slot(c) + D));
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f), oc = o;
+            float L = 0.f, Lc = 0.f;
+#pragma unroll 4
+            for (int c = first; c <= last; ++c) {
+                const float *p = slot(c);
+                const float f = exp2_diff(__ldcg(p + D), M);
+                comp_fma4(o, oc, __ldcg(reinterpret_cast<const float4 *>(p + d)), f);
+                comp_fma(L, Lc, __ldcg(p + D + 1), f);
+            }
+            const int qh = paged_query_head(a, b, vh, head);
+            const float inv = 1.0f / L;
+            if (qh >= 0)
+                store4(a.out, ((long long)b * a.h_q + qh) * D + d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), dtype);
+        }
+    }
+}
+
+}  // namespace moa

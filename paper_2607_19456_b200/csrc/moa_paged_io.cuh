@@ -1,0 +1,309 @@
+// moa_paged_io.cuh -- writing and reading the rows of a paged cache: the append, with the position
+// rotation of queries and keys on the way, and the read-back into dense rows.
+//
+// Both are bound by memory.  A row (one head of one token) belongs to D/16 neighbouring threads of a
+// warp, 16 features each, as two chunks of 8 (16 bytes in 16-bit types): under the rotation of
+// halves the two chunks are each other's partners, so no value crosses threads.  A thread takes
+// several heads of its token in turn and keeps the token's cosines and sines in registers.
+//
+// Every product, sum and quotient below is rounded on its own (no contraction into fused
+// multiply-adds): what a row holds is then defined by the formulas alone, and equals what any
+// other IEEE evaluation of them gives, which matters where a value lies next to a border between
+// two 4-bit codes.
+#pragma once
+
+#include "moa_paged.cuh"
+
+namespace moa {
+
+struct PagedIoArgs {
+    unsigned char *k_pool, *v_pool;
+    uint32_t *kp, *vp;
+    long long k_sp, k_sh, k_sr;      // byte strides of the pools: page, kv head, row
+    long long v_sp, v_sh, v_sr;
+    int num_pages, page_size, page_shift, h_kv;
+    const int32_t *table;
+    int max_pages, batch;
+    const int32_t *seq_lens;
+    // append
+    const void *q, *k, *v;
+    void *q_out;
+    long long q_st, k_st, v_st, o_st;    // elements between consecutive tokens
+    int tokens, h_q, heads_per_thread;
+    const int32_t *token_start;      // [batch + 1], or null: token t belongs to sequence t
+    const float *cos_sin;            // [rope_rows, rot]: rot/2 cosines, rot/2 sines
+    int rope_rows, rot;
+    int pairs;                       // features (2i, 2i+1) turn together; else (i, rot/2 + i)
+    // read-back
+    void *k_out, *v_out;
+    const int32_t *row_start;
+    int n_out;
+};
+
+template <int FMT> struct PagedElem { using type = uint16_t; };
+template <> struct PagedElem<MOA_KV_F32> { using type = float; };
+
+// Eight consecutive elements of a row as floats, and back.
+template <int DT>
+__device__ __forceinline__ void load8(float (&x)[8], const void *p)
+{
+    if constexpr (DT == MOA_F32) {
+        const float4 u = static_cast<const float4 *>(p)[0], w = static_cast<const float4 *>(p)[1];
+        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
+    } else {
+        const uint4 u = *static_cast<const uint4 *>(p);
+        const uint32_t r[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack16<DT == MOA_BF16>(r[i]);
+            x[2 * i] = f.x; x[2 * i + 1] = f.y;
+        }
+    }
+}
+template <int DT>
+__device__ __forceinline__ void store8(void *p, const float (&x)[8])
+{
+    if constexpr (DT == MOA_F32) {
+        static_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        static_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        constexpr bool BF = DT == MOA_BF16;
+        *static_cast<uint4 *>(p) = make_uint4(pack16<BF>(x[0], x[1]), pack16<BF>(x[2], x[3]), pack16<BF>(x[4], x[5]),
+                                              pack16<BF>(x[6], x[7]));
+    }
+}
+
+// (x, y) turned by the angle whose cosine and sine are c and s.
+__device__ __forceinline__ void turn(float &x, float &y, float c, float s)
+{
+    const float u = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
+    y = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
+    x = u;
+}
+
+// A row in 4 bits: s = fp16((max - min) / 15), m = fp16(min), code = round((x - m) / s) in 0..15.
+// The quotient by 15 is a product with fp32's nearest to 1/15.  Rows beyond fp16's range are held
+// as if cut off there; a row with a value that is no number or infinite reads back as NaN.
+// lo, hi: this thread's two chunks; the D/16 threads of a row are neighbours.
+template <int D>
+__device__ __forceinline__ void pack_row(const float (&lo)[8], const float (&hi)[8], uint32_t &c_lo, uint32_t &c_hi,
+                                         uint32_t &params)
+{
+    float mn = lo[0], mx = lo[0];
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        mn = fminf(mn, fminf(lo[i], hi[i]));
+        mx = fmaxf(mx, fmaxf(lo[i], hi[i]));
+        odd |= !isfinite(lo[i]) || !isfinite(hi[i]);
+    }
+    int bad = odd;
+#pragma unroll
+    for (int off = 1; off < D / 16; off <<= 1) {
+        mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+        bad |= __shfl_xor_sync(0xffffffffu, bad, off);
+    }
+    const float top = 65504.0f;
+    const __half s16 = __float2half_rn(fminf(__fmul_rn(__fsub_rn(mx, mn), 1.0f / 15.0f), top));
+    const __half m16 = __float2half_rn(fminf(fmaxf(mn, -top), top));
+    const float s = __half2float(s16), m = __half2float(m16);
+    c_lo = c_hi = 0u;
+    if (bad) { params = 0x7fff7fffu; return; }
+    if (s > 0.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(lo[i], m), s)), 0.f), 15.f);
+            const float b = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(hi[i], m), s)), 0.f), 15.f);
+            c_lo |= (uint32_t)a << (4 * i);
+            c_hi |= (uint32_t)b << (4 * i);
+        }
+    }
+    params = (uint32_t)__half_as_ushort(s16) | ((uint32_t)__half_as_ushort(m16) << 16);
+}
+
+// FMT: of the pools; DT: of q, k, v.  The same for 16 and 32 bits.
+template <int FMT, int DT, int D>
+__global__ void __launch_bounds__(256) paged_append_kernel(const PagedIoArgs a)
+{
+    constexpr int TPR = D / 16, SLOTS = 256 / TPR, ES = DT == MOA_F32 ? 4 : 2;
+    launch_dependents();
+    grid_dependency_wait();
+    const int part = threadIdx.x % TPR;
+    const int heads = a.h_q + 2 * a.h_kv;
+    const int runs = (heads + a.heads_per_thread - 1) / a.heads_per_thread;
+    const long long item = (long long)blockIdx.x * SLOTS + threadIdx.x / TPR;
+    const int tok = (int)(item / runs);
+    const int head0 = (int)(item % runs) * a.heads_per_thread;
+    // Every thread stays to the end: the rows of a warp exchange their extremes together.
+    bool live = item < (long long)a.tokens * runs;
+    int b = tok;
+    long long pos = 0;
+    if (live) {
+        if (a.token_start != nullptr) {
+            int lo = 0, hi = a.batch;                      // last b with token_start[b] <= tok
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (__ldg(a.token_start + mid) <= tok) lo = mid; else hi = mid;
+            }
+            b = lo;
+            const int first = __ldg(a.token_start + b), next = __ldg(a.token_start + b + 1);
+            live = first <= tok && tok < next;             // behind the last sequence: left as it is
+            pos = (long long)__ldg(a.seq_lens + b) - ((long long)next - tok);
+        } else {
+            live = tok < a.batch;
+            if (live) pos = (long long)__ldg(a.seq_lens + b) - 1;
+        }
+    }
+    long long page = 0;
+    int off = 0;
+    if (live) {
+        int status = 0;
+        const int pi = pos < 0 ? 0 : a.page_shift >= 0 ? (int)pos >> a.page_shift : (int)pos / a.page_size;
+        if (pos < 0 || pi >= a.max_pages || (a.rot > 0 && pos >= a.rope_rows)) status = MOA_STATUS_APPEND_RANGE;
+        else {
+            page = __ldg(a.table + (long long)b * a.max_pages + pi);
+            off = (int)pos - pi * a.page_size;
+            if (page < 0 || page >= a.num_pages) status = MOA_STATUS_PAGE_RANGE;
+        }
+        if (status != 0) {
+            live = false;
+            if (part == 0 && head0 == 0) raise_status(status);
+        }
+    }
+    // Places of this thread's two chunks, and its share of the token's cosines and sines.
+    const int rot = a.rot, half = rot / 2;
+    const bool by_chunk = !a.pairs && rot % 16 == 0;       // partners are the thread's own chunks
+    int d_lo = 16 * part, d_hi = 16 * part + 8;
+    if (by_chunk && 16 * part < rot) { d_lo = 8 * part; d_hi = half + 8 * part; }
+    const bool turns = live && 16 * part < rot;
+    float cs[8], sn[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
+    const float *row = a.cos_sin + pos * rot;
+    if (turns && (a.pairs || by_chunk)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (8 * part + i < half) { cs[i] = __ldg(row + 8 * part + i); sn[i] = __ldg(row + half + 8 * part + i); }
+    }
+#pragma unroll 2
+    for (int hd = head0; hd < head0 + a.heads_per_thread; ++hd) {
+        const bool on = live && hd < heads;
+        const bool is_q = hd < a.h_q, is_v = hd >= a.h_q + a.h_kv;
+        const int h = is_q ? hd : is_v ? hd - a.h_q - a.h_kv : hd - a.h_q;
+        const unsigned char *src = is_q ? static_cast<const unsigned char *>(a.q) + (tok * a.q_st + (long long)h * D) * ES
+                                 : is_v ? static_cast<const unsigned char *>(a.v) + (tok * a.v_st + (long long)h * D) * ES
+                                        : static_cast<const unsigned char *>(a.k) + (tok * a.k_st + (long long)h * D) * ES;
+        float lo[8] = {}, hi[8] = {};
+        if (on) { load8<DT>(lo, src + d_lo * ES); load8<DT>(hi, src + d_hi * ES); }
+        if (on && turns && !is_v) {
+            if (a.pairs) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (d_lo + 2 * i < rot) turn(lo[2 * i], lo[2 * i + 1], cs[i], sn[i]);
+                    if (d_hi + 2 * i < rot) turn(hi[2 * i], hi[2 * i + 1], cs[4 + i], sn[4 + i]);
+                }
+            } else if (by_chunk) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) turn(lo[i], hi[i], cs[i], sn[i]);
+            } else {                                       // partners in other threads' chunks: fetched one by one
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int d = 16 * part + i;
+                    if (d >= rot) continue;
+                    const int pair = d < half ? d : d - half;
+                    const float c = __ldg(row + pair), s = __ldg(row + half + pair);
+                    float x = load_as_float(src, pair, DT), y = load_as_float(src, pair + half, DT);
+                    turn(x, y, c, s);
+                    const float mine = d < half ? x : y;
+                    if (i < 8) lo[i] = mine; else hi[i - 8] = mine;
+                }
+            }
+        }
+        __syncwarp();                                      // q_out may be q: its row is read by now
+        if (is_q) {
+            if (on) {
+                unsigned char *dst = static_cast<unsigned char *>(a.q_out) + (tok * a.o_st + (long long)h * D) * ES;
+                store8<DT>(dst + d_lo * ES, lo);
+                store8<DT>(dst + d_hi * ES, hi);
+            }
+        }
+        if constexpr (FMT != MOA_KV_INT4) {
+            if (on && !is_q) {
+                unsigned char *dst = is_v ? a.v_pool + page * a.v_sp + h * a.v_sh + off * a.v_sr
+                                          : a.k_pool + page * a.k_sp + h * a.k_sh + off * a.k_sr;
+                store8<DT>(dst + d_lo * ES, lo);
+                store8<DT>(dst + d_hi * ES, hi);
+            }
+        } else if (__any_sync(0xffffffffu, on && !is_q)) {
+            uint32_t c_lo, c_hi, params;
+            pack_row<D>(lo, hi, c_lo, c_hi, params);       // (a collective of the warp)
+            if (on && !is_q) {
+                unsigned char *dst = is_v ? a.v_pool + page * a.v_sp + h * a.v_sh + off * a.v_sr
+                                          : a.k_pool + page * a.k_sp + h * a.k_sh + off * a.k_sr;
+                *reinterpret_cast<uint32_t *>(dst + d_lo / 2) = c_lo;
+                *reinterpret_cast<uint32_t *>(dst + d_hi / 2) = c_hi;
+                if (part == 0) (is_v ? a.vp : a.kp)[(page * a.h_kv + h) * a.page_size + off] = params;
+            }
+        }
+    }
+}
+
+// Rows [row_start, seq_len) of every sequence into [batch, h_kv, n_out, D]; a thread takes eight
+// features of one row of K and of V.
+template <int FMT, int D>
+__global__ void __launch_bounds__(256) paged_gather_kernel(const PagedIoArgs a, int out_dtype)
+{
+    constexpr int TPR = D / 8, SLOTS = 256 / TPR;
+    launch_dependents();
+    grid_dependency_wait();
+    const int d = (threadIdx.x % TPR) * 8;
+    const long long item = (long long)blockIdx.x * SLOTS + threadIdx.x / TPR;     // (b, h, i)
+    if (item >= (long long)a.batch * a.h_kv * a.n_out) return;
+    const int i = (int)(item % a.n_out);
+    const int b = (int)(item / a.n_out / a.h_kv), h = (int)(item / a.n_out % a.h_kv);
+    const int len = __ldg(a.seq_lens + b), from = a.row_start != nullptr ? __ldg(a.row_start + b) : 0;
+    if (from < 0 || len < from || (long long)len - from > a.n_out || len > (long long)a.max_pages * a.page_size) {
+        if (i == 0 && h == 0 && d == 0) raise_status(MOA_STATUS_SEQLEN_RANGE);
+        return;
+    }
+    const int row = from + i;
+    if (i >= len - from) return;
+    const int pi = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size;
+    const int off = row - pi * a.page_size;
+    const long long page = __ldg(a.table + (long long)b * a.max_pages + pi);
+    if (page < 0 || page >= a.num_pages) {
+        if (d == 0) raise_status(MOA_STATUS_PAGE_RANGE);
+        return;
+    }
+    const unsigned char *ks = a.k_pool + page * a.k_sp + h * a.k_sh + off * a.k_sr;
+    const unsigned char *vs = a.v_pool + page * a.v_sp + h * a.v_sh + off * a.v_sr;
+    float x[8], y[8];
+    if constexpr (FMT == MOA_KV_INT4) {
+        const long long at = (page * a.h_kv + h) * a.page_size + off;
+        const uint32_t kc = *reinterpret_cast<const uint32_t *>(ks + d / 2), vc = *reinterpret_cast<const uint32_t *>(vs + d / 2);
+        const float2 kf = unpack16<false>(a.kp[at]), vf = unpack16<false>(a.vp[at]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = fmaf(kf.x, (float)((kc >> (4 * e)) & 15u), kf.y);
+            y[e] = fmaf(vf.x, (float)((vc >> (4 * e)) & 15u), vf.y);
+        }
+    } else {
+        constexpr int ES = FMT == MOA_KV_F32 ? 4 : 2;
+        load8<FMT>(x, ks + d * ES);
+        load8<FMT>(y, vs + d * ES);
+    }
+    const long long to = item * D + d;
+    if (out_dtype == MOA_F32) {
+        store8<MOA_F32>(static_cast<float *>(a.k_out) + to, x);
+        store8<MOA_F32>(static_cast<float *>(a.v_out) + to, y);
+    } else if (out_dtype == MOA_BF16) {
+        store8<MOA_BF16>(static_cast<uint16_t *>(a.k_out) + to, x);
+        store8<MOA_BF16>(static_cast<uint16_t *>(a.v_out) + to, y);
+    } else {
+        store8<MOA_F16>(static_cast<uint16_t *>(a.k_out) + to, x);
+        store8<MOA_F16>(static_cast<uint16_t *>(a.v_out) + to, y);
+    }
+}
+
+}  // namespace moa
