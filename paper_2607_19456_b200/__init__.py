@@ -25,6 +25,7 @@ F32, BF16, F16 = 0, 1, 2                               # element types of tensor
 KV_F32, KV_BF16, KV_F16, KV_INT4 = 0, 1, 2, 3          # formats of a paged cache
 ROPE_HALVES, ROPE_PAIRS = 0, 1
 
+_Strides4 = C.c_longlong * 4
 _lib = None
 
 
@@ -101,12 +102,14 @@ def lib():
 
 def _ptr(x):
     """Device (or host) address of a tensor / array / int / None."""
-    if x is None:
-        return None
+    if x is None or type(x) is int:
+        return x
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        pass
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
     if hasattr(x, "ctypes"):
         return x.ctypes.data
     raise TypeError("expected a tensor, an array or an address")
@@ -115,7 +118,7 @@ def _ptr(x):
 def _stream(stream):
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -238,7 +241,7 @@ def moa_paged_append(cache, q, k, v, q_out, dtype, token_strides, tokens, h_q, b
     if token_strides is not None:
         if len(token_strides) != 4:
             raise ValueError("token strides are (q, k, v, q_out) element counts")
-        token_strides = (C.c_longlong * 4)(*[int(x) for x in token_strides])
+        token_strides = _Strides4(*token_strides)
     _check(lib().moa_paged_append(cache, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), dtype, token_strides, tokens, h_q,
                                   batch, _ptr(token_start), _ptr(seq_lens), _ptr(page_table), max_pages,
                                   _ptr(cos_sin), rope_rows, rot_dim, rope_style, _stream(stream)),

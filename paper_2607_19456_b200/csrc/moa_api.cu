@@ -946,18 +946,18 @@ static cudaError_t launch_paged_cfg(const PagedArgs &a, int grid, cudaStream_t s
 template <int D>
 static cudaError_t launch_paged(int format, int heads, const PagedArgs &a, int grid, cudaStream_t st)
 {
-    constexpr bool wide = D == 128;        //                                            NT  W   S
+    constexpr bool wide = D == 128;        //                                                      NT  W   S  TT
     switch (format) {
-    case MOA_KV_F32: return launch_paged_cfg<PagedCfg<MOA_KV_F32, D, 1, wide ? 6 : 8, 2>>(a, grid, st);
+    case MOA_KV_F32: return launch_paged_cfg<PagedCfg<MOA_KV_F32, D, 1, wide ? 6 : 8, 2, 1>>(a, grid, st);
     case MOA_KV_BF16:
-        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 1, 8, wide ? 2 : 4>>(a, grid, st);
-        return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 2, 8, wide ? 2 : 4>>(a, grid, st);
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 1, 8, wide ? 2 : 4, 1>>(a, grid, st);
+        return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 2, 8, wide ? 2 : 4, 1>>(a, grid, st);
     case MOA_KV_F16:
-        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 1, 8, wide ? 2 : 4>>(a, grid, st);
-        return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 2, 8, wide ? 2 : 4>>(a, grid, st);
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 1, 8, wide ? 2 : 4, 1>>(a, grid, st);
+        return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 2, 8, wide ? 2 : 4, 1>>(a, grid, st);
     default:
-        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 16, wide ? 4 : 6>>(a, grid, st);
-        return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 12, wide ? 4 : 6>>(a, grid, st);
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 16, wide ? 2 : 3, 2>>(a, grid, st);
+        return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 8, wide ? 3 : 4, 2>>(a, grid, st);
     }
 }
 

@@ -64,17 +64,20 @@ struct PagedArgs {
     unsigned long long ticket_tag;
 };
 
-// W warps, S ring stages of 16 rows (K and V) each.  The ring and the slots of the first cut unit
+// W warps, S ring stages of TT tiles of 16 rows (K and V) each.  The ring and the slots of the first cut unit
 // share the 227 KB of an SM; the slot of the last cut unit is the ring itself, empty by then.
-template <int FMT_, int D_, int NT_, int W_, int S_>
+template <int FMT_, int D_, int NT_, int W_, int S_, int TT_>
 struct PagedCfg {
-    static constexpr int FMT = FMT_, D = D_, NT = NT_, W = W_, S = S_;
-    static constexpr int THREADS = W * 32, R = 16;
+    static constexpr int FMT = FMT_, D = D_, NT = NT_, W = W_, S = S_, TT = TT_;
+    static constexpr int THREADS = W * 32, R = 16 * TT;    // rows of a stage
     static constexpr int ROWB = FMT == MOA_KV_F32 ? 4 * D : FMT == MOA_KV_INT4 ? D / 2 : 2 * D;   // bytes of a row
     static constexpr int CPR = ROWB / 16;                  // 16-byte chunks of a row
-    static constexpr int NCH = R * CPR / 32;               // chunks a lane copies per tile and operand
-    static constexpr int KB = R * ROWB;                    // bytes of one operand's tile
-    static constexpr int STAGE = 2 * KB + (FMT == MOA_KV_INT4 ? 2 * R * 4 : 0);
+    static constexpr int NCH = 16 * CPR / 32;              // chunks a lane copies per tile and operand
+    static constexpr int KB = 16 * ROWB;                   // bytes of one operand's tile
+    static constexpr int PB = FMT == MOA_KV_INT4 ? 128 : 0;    // bytes of a tile's (scale, least) pairs: 16 of K, 16 of V
+    static constexpr int TILE = 2 * KB + PB;
+    static constexpr int STAGE = TT * TILE;
+    static constexpr int WHOLE = 4 * W;                    // stages of a unit that is not cut when there are few units
     static constexpr int MT = D / 16;                      // 16-feature output tiles
     static constexpr int G = 8 * NT;                       // heads of a unit
     static constexpr int PS = D + 4;                       // floats of a partial: o[D], m, l, 2 pad
@@ -87,7 +90,7 @@ struct PagedCfg {
     static_assert(W <= 16, "two segments per warp have to fit a warp's lanes");
     static_assert((size_t)S * STAGE >= sizeof(float) * SLOT, "the ring holds the last partial");
     static_assert(OFF_FIRST % 16 == 0 && OFF_PREF % 16 == 0, "alignment of the regions");
-    static_assert(SMEM_BYTES <= 227 * 1024 - 2048, "shared memory of an SM, less the static part");
+    static_assert(SMEM_BYTES <= 227 * 1024 - 3328, "shared memory of an SM, less the static part");
 };
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool full)
@@ -99,6 +102,14 @@ __device__ __forceinline__ void cp4(uint32_t dst, const void *src, bool full)
 {
     const int n = full ? 4 : 0;
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -181,21 +192,75 @@ __device__ __forceinline__ int paged_query_head(const PagedArgs &a, int b, int v
     return (g < a.g_s && in_stored < a.g_total && b < a.batch) ? (vh / a.share) * a.g_total + in_stored : -1;
 }
 
-// A place in the flat list: tile i of the ub tiles of unit (b, h).
+// A place in the flat list: stage i of the ub stages (of R rows) of unit (b, h).
 struct TileCursor {
     int b, h, i, ub, len;
 };
-__device__ __forceinline__ void tile_advance(const PagedArgs &a, int hv, TileCursor &c)
+template <int R>
+__device__ __forceinline__ bool tile_advance(const PagedArgs &a, int hv, TileCursor &c)      // true: another unit
 {
-    if (++c.i < c.ub) return;
+    if (++c.i < c.ub) return false;
     c.i = 0;
-    if (++c.h < hv) return;
+    if (++c.h < hv) return true;
     c.h = 0;
     do {
-        if (++c.b >= a.batch) { c.b = a.batch; c.len = 0; c.ub = 1; return; }
+        if (++c.b >= a.batch) { c.b = a.batch; c.len = 0; c.ub = 1; return true; }
         c.len = paged_len(a, c.b);
     } while (c.len == 0);
-    c.ub = (c.len + 15) >> 4;
+    c.ub = (c.len + R - 1) / R;
+    return true;
+}
+
+// Place of a 16-byte chunk c of row r in the shared tile of K and of V: what keeps the reads free of
+// bank conflicts.
+template <class C>
+__device__ __forceinline__ void chunk_place(int r, int c, uint32_t &kd, uint32_t &vd)
+{
+    if constexpr (C::FMT == MOA_KV_INT4) {
+        const int slot = (r & 8) | ((r & 3) << 1) | ((r >> 2) & 1);
+        kd = slot * C::ROWB + c * 16;
+        vd = r * C::ROWB + ((c * 16) ^ (C::D == 128 ? ((r >> 1) & 1) << 5 : 0));
+    } else if constexpr (C::FMT == MOA_KV_F32) {
+        kd = r * C::ROWB + ((c ^ ((r & 1) << 2)) << 4);
+        vd = r * C::ROWB + ((c ^ ((r & 3) << 1)) << 4);
+    } else {
+        kd = vd = r * C::ROWB + ((c ^ (r & 7)) << 4);
+    }
+}
+
+// Copies of one tile whose rows may lie in several pages, end behind the sequence (zero-filled), or
+// have pages that do not exist (zero-filled, reported).  One row per lane (lanes 16..31 repeat); out of
+// line, so that the common case (16 rows of one page) has the loop to itself.
+template <class C>
+__device__ __noinline__ bool copy_ragged_tile(const PagedArgs &a, uint32_t dst, int b, int hs, int row0, int len)
+{
+    const int lane = threadIdx.x & 31, row = row0 + (lane & 15);
+    long long ko = -1, vo = 0, po = 0;
+    bool bad = false;
+    if (row < len) {
+        const int pi = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size, off = row - pi * a.page_size;
+        const long long page = __ldg(a.table + (long long)b * a.max_pages + pi);
+        bad = page < 0 || page >= a.num_pages;
+        if (!bad) {
+            ko = page * a.k_sp + hs * a.k_sh + off * a.k_sr;
+            vo = page * a.v_sp + hs * a.v_sh + off * a.v_sr;
+            po = (page * a.h_stored + hs) * a.page_size + off;
+        }
+    }
+    const int c = lane % C::CPR;
+#pragma unroll
+    for (int i = 0; i < C::NCH; ++i) {
+        const int r = lane / C::CPR + i * (32 / C::CPR);
+        const long long k1 = __shfl_sync(0xffffffffu, ko, r), v1 = __shfl_sync(0xffffffffu, vo, r);
+        uint32_t kd, vd;
+        chunk_place<C>(r, c, kd, vd);
+        cp16(dst + kd, k1 >= 0 ? a.k + k1 + c * 16 : a.k, k1 >= 0);
+        cp16(dst + C::KB + vd, k1 >= 0 ? a.v + v1 + c * 16 : a.v, k1 >= 0);
+    }
+    if constexpr (C::PB != 0) cp4(dst + 2 * C::KB + lane * 4, (lane < 16 ? a.kp : a.vp) + po, ko >= 0);
+    const bool any = __any_sync(0xffffffffu, bad);
+    if (any && lane == 0) raise_status(MOA_STATUS_PAGE_RANGE);
+    return any;
 }
 
 // Registers of one warp's unit: accumulators of O^T, reference maxima, sums.
@@ -204,23 +269,36 @@ struct PagedState {
     float acc[C::NT][C::MT][4];
     float m[C::NT][2], msub[C::NT][2], l[C::NT][2];        // heads 8n + 2t and 8n + 2t + 1; msub: m, or 0 while m is -inf
     float om[C::NT][2];                                    // 4 bits: sum of p * least
-    float ref;                                             // 4 bits: power of two, at least every row's scale so far
+    float ref, inv;                                        // 4 bits: power of two, at least every row's scale so far; 128 / ref
 };
 
-template <class C>
-__global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const PagedArgs a)
+// n * i / of, in 32 bits where that suffices.
+__device__ __forceinline__ long long split_at(long long n, int i, int of)
 {
-    constexpr int FMT = C::FMT, D = C::D, NT = C::NT, W = C::W, S = C::S, MT = C::MT, PS = C::PS, G = C::G;
+    return n <= 0x003fffff ? (long long)((unsigned)n * (unsigned)i / (unsigned)of) : n * i / of;      // (i <= of <= 1024)
+}
+// The part that stage j lies in, of `of` parts of n stages.
+__device__ __forceinline__ int part_of(long long n, long long j, int of)
+{
+    return n <= 0x003fffff ? (int)(((unsigned)(j + 1) * (unsigned)of - 1u) / (unsigned)n) : (int)(((j + 1) * of - 1) / n);
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __grid_constant__ PagedArgs a)
+{
+    constexpr int FMT = C::FMT, D = C::D, NT = C::NT, W = C::W, S = C::S, MT = C::MT, PS = C::PS, G = C::G, TT = C::TT, R = C::R;
     constexpr bool BF = FMT == MOA_KV_BF16, Q4 = FMT == MOA_KV_INT4, F32 = FMT == MOA_KV_F32;
     extern __shared__ __align__(128) unsigned char smem[];
     float *first_slots = reinterpret_cast<float *>(smem + C::OFF_FIRST);
     long long *s_pref = reinterpret_cast<long long *>(smem + C::OFF_PREF);
     __shared__ long long s_warp[16];
+    __shared__ bool s_large[16];
     __shared__ long long s_seg[32];                        // unit of segment 2 * warp + (0: first, 1: last), or -1
     __shared__ long long s_seg_lo[32];                     // flat index of that unit's first tile
     __shared__ int s_seg_ub[32], s_seg_vh[32];             // its tiles, its virtual kv head (with the sequence in s_seg_b)
     __shared__ int s_seg_b[32];
-    __shared__ int s_grp_lo[32], s_grp_hi[32], s_ngrp, s_last;
+    __shared__ float s_top[32][G];                         // reference maximum of the group that a segment leads
+    __shared__ int s_done[2];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int hv = a.h_stored * a.share;
@@ -232,14 +310,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
     // ---- lengths: tiles per sequence, prefix over the threads' runs of sequences -----------
     const int per_thread = (a.batch + C::THREADS - 1) / C::THREADS;
     long long mine = 0;
-    bool empty = false;
+    bool empty = false, large = false;
     for (int i = 0; i < per_thread; ++i) {
         const int b = tid * per_thread + i;
         if (b >= a.batch) break;
         const int len = a.seq_lens[b];
         const bool here = (unsigned)b % gridDim.x == blockIdx.x;
         if (len < 0 || len > a.len_max) { if (here) raise_status(MOA_STATUS_SEQLEN_RANGE); }
-        else { mine += (len + 15) >> 4; empty |= (len == 0 && here); }
+        else {
+            mine += (len + R - 1) / R;
+            empty |= (len == 0 && here);
+            large |= len > C::WHOLE * R;
+        }
     }
     long long inc = mine;
 #pragma unroll
@@ -247,7 +329,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
         const long long x = __shfl_up_sync(0xffffffffu, inc, off);
         if (lane >= off) inc += x;
     }
-    if (lane == 31) s_warp[warp] = inc;
+    large = __any_sync(0xffffffffu, large);
+    if (lane == 31) { s_warp[warp] = inc; s_large[warp] = large; }
     if (tid < 32) s_seg[tid] = -1;
     const int any_empty = __syncthreads_or(empty);
     long long before = 0, total1 = 0;
@@ -255,6 +338,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
     for (int w = 0; w < W; ++w) {
         if (w < warp) before += s_warp[w];
         total1 += s_warp[w];
+        large |= s_large[w];
     }
     s_pref[tid] = before + inc - mine;
     if (tid == 0) s_pref[C::THREADS] = total1;
@@ -268,15 +352,28 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
     }
     __syncthreads();
     const long long total = total1 * hv;
-    // A CTA takes at least W tiles: a cut costs a partial, a counter round trip and a merge.
-    long long active = (total + W - 1) / W;
-    if (active > gridDim.x) active = gridDim.x;
-    if (blockIdx.x >= active) return;                      // (also when there is nothing to do)
-    const long long c0 = total * blockIdx.x / active, c1 = total * (blockIdx.x + 1) / active;
-    const long long j0 = c0 + (c1 - c0) * warp / W, j1 = c0 + (c1 - c0) * (warp + 1) / W;
+    // A CTA takes at least W stages: a cut costs a partial, a counter round trip and a merge, about 3 us.
+    int active = total < (long long)W * gridDim.x ? (int)((unsigned)(total + W - 1) / W) : (int)gridDim.x;
+    long long c0, c1;
+    if (!large && per_thread == 1 && (long long)a.batch * hv <= gridDim.x) {      // small and few: a unit for each CTA, nothing is cut
+        const int b = blockIdx.x / hv, h = blockIdx.x % hv;
+        if (b >= a.batch) return;
+        const long long ub = s_pref[b + 1] - s_pref[b];
+        c0 = s_pref[b] * hv + h * ub;
+        c1 = c0 + ub;
+        if (ub == 0) return;
+    } else {
+        if (blockIdx.x >= active) return;                  // (also when there is nothing to do)
+        c0 = split_at(total, blockIdx.x, active);
+        c1 = split_at(total, blockIdx.x + 1, active);
+    }
+    const long long j0 = c0 + split_at(c1 - c0, warp, W), j1 = c0 + split_at(c1 - c0, warp + 1, W);
 
     unsigned char *ring = smem + (size_t)warp * S * C::STAGE;
-    const uint32_t ring_u = smem_u32(ring);
+    const uint32_t smem_u = smem_u32(smem), ring_u = smem_u + warp * S * C::STAGE;
+    // fp16 output: the weights of 4-bit rows in two fp16 terms (one term: 6.0e-4 off the definition where
+    // the rounding of the output alone is 2.0e-4; bf16 outputs, 1.7e-3, gain nothing from it).
+    const bool fine = Q4 && dtype == MOA_F16;
 
     if (j0 < j1) {
         // ---- the tile that the range begins with ------------------------------------------
@@ -292,12 +389,16 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
             int b = lo * per_thread, ub = 0, len = 0;
             for (; b < a.batch; ++b) {                     // ends before: j0 < total
                 len = paged_len(a, b);
-                ub = (len + 15) >> 4;
+                ub = (len + R - 1) / R;
                 if (j0 < at + (long long)ub * hv) break;
                 at += (long long)ub * hv;
             }
             cc.b = b; cc.len = len; cc.ub = ub; cc.h = cc.i = 0;
-            if (b < a.batch) { cc.h = (int)((j0 - at) / ub); cc.i = (int)((j0 - at) % ub); }
+            if (b < a.batch) {
+                const long long in = j0 - at;
+                cc.h = in <= 0x7fffffff ? (int)((unsigned)in / (unsigned)ub) : (int)(in / ub);
+                cc.i = (int)(in - (long long)cc.h * ub);
+            }
             else cc.len = 0, cc.ub = 1;                    // (lengths that changed meanwhile: no rows, no output)
             unit_lo = j0 - cc.i;
         }
@@ -305,69 +406,63 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
         long long jl = j0;
         int load_stage = 0;
         unsigned bad_stages = 0;
-
-        // Page number of this lane's row (lane & 15) of the tile under `lc`; -1 behind the last row.
-        auto fetch_page = [&]() -> int {
-            const int row = lc.i * 16 + (lane & 15);
-            if (row >= lc.len) return -1;
-            const int p = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size;
-            return __ldg(a.table + (long long)lc.b * a.max_pages + p);
+        // Of the unit under `lc`: its K/V head's part of the pools, its row of the table.
+        const unsigned char *kh, *vh;
+        const uint32_t *ph;                                // this lane's operand of the pairs
+        const int32_t *trow;
+        int hs;
+        auto load_unit = [&]() {
+            hs = a.share == 1 ? lc.h : lc.h / a.share;
+            kh = a.k + hs * a.k_sh + (lane / C::CPR) * a.k_sr + (lane % C::CPR) * 16;
+            vh = a.v + hs * a.v_sh + (lane / C::CPR) * a.v_sr + (lane % C::CPR) * 16;
+            if (Q4) ph = (lane < 16 ? a.kp : a.vp) + (long long)hs * a.page_size + (lane & 15);
+            trow = a.table + (long long)lc.b * a.max_pages;
         };
-        int page = fetch_page();
-
-        auto issue = [&]() {                               // copies of the tile under `lc`, then on to the next
-            const uint32_t st = ring_u + load_stage * C::STAGE;
-            const int row0 = lc.i * 16, nr = min(16, lc.len - row0);
-            const int hs = lc.h / a.share;
-            const bool bad = (lane & 15) < nr && (unsigned)page >= (unsigned)a.num_pages;
-            if (__any_sync(0xffffffffu, bad)) {
-                bad_stages |= 1u << load_stage;
-                if (lane == 0) raise_status(MOA_STATUS_PAGE_RANGE);
-                if (bad) page = -1;
-            } else bad_stages &= ~(1u << load_stage);
-            const int my_row = row0 + (lane & 15);
-            const int my_off = a.page_shift >= 0 ? my_row & (a.page_size - 1) : my_row % a.page_size;
-            const unsigned char *kh = a.k + hs * a.k_sh, *vh = a.v + hs * a.v_sh;
-            const unsigned char *k1 = nullptr, *v1 = nullptr;      // the tile's first row, where it lies in one page
-            if (a.one_page) {
-                const long long pg = __shfl_sync(0xffffffffu, page, 0), off0 = __shfl_sync(0xffffffffu, my_off, 0);
-                k1 = kh + pg * a.k_sp + off0 * a.k_sr;
-                v1 = vh + pg * a.v_sp + off0 * a.v_sr;
-            }
-            const int c = lane % C::CPR;
+        // Page numbers of the stage's tiles, one ahead of their copies; -1: the tile goes by row
+        // (it ends behind the sequence, or pages are no multiple of 16 rows).
+        int page[TT];
+        auto fetch_pages = [&]() {
 #pragma unroll
-            for (int i = 0; i < C::NCH; ++i) {
-                const int r = lane / C::CPR + i * (32 / C::CPR);
-                const int pg = __shfl_sync(0xffffffffu, page, r), off = __shfl_sync(0xffffffffu, my_off, r);
-                const bool ok = pg >= 0;
-                const unsigned char *kr, *vr;
-                if (a.one_page) { kr = k1 + (ok ? r * a.k_sr : 0); vr = v1 + (ok ? r * a.v_sr : 0); }
-                else { kr = kh + (long long)(ok ? pg : 0) * a.k_sp + off * a.k_sr; vr = vh + (long long)(ok ? pg : 0) * a.v_sp + off * a.v_sr; }
-                uint32_t kd, vd;                           // places in the tile: what keeps the reads free of bank conflicts
-                if constexpr (Q4) {
-                    const int slot = (r & 8) | ((r & 3) << 1) | ((r >> 2) & 1);
-                    kd = slot * C::ROWB + c * 16;
-                    vd = r * C::ROWB + ((c * 16) ^ (D == 128 ? ((r >> 1) & 1) << 5 : 0));
-                } else if constexpr (F32) {
-                    kd = r * C::ROWB + ((c ^ ((r & 1) << 2)) << 4);
-                    vd = r * C::ROWB + ((c ^ ((r & 3) << 1)) << 4);
+            for (int tt = 0; tt < TT; ++tt) {
+                const int row0 = lc.i * R + 16 * tt;
+                page[tt] = -1;
+                if (a.one_page && row0 + 16 <= lc.len) page[tt] = __ldg(trow + (a.page_shift >= 0 ? row0 >> a.page_shift : row0 / a.page_size));
+            }
+        };
+        load_unit();
+        fetch_pages();
+        const long long k_step = (32 / C::CPR) * a.k_sr, v_step = (32 / C::CPR) * a.v_sr;
+
+        auto issue = [&]() {                               // copies of the stage under `lc`, then on to the next
+            bool bad = false;
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt) {
+                const uint32_t dst = ring_u + load_stage * C::STAGE + tt * C::TILE;
+                const int row0 = lc.i * R + 16 * tt;
+                if ((unsigned)page[tt] < (unsigned)a.num_pages) {
+                    const int off0 = a.page_shift >= 0 ? row0 & (a.page_size - 1) : row0 % a.page_size;
+                    const unsigned char *kr = kh + page[tt] * a.k_sp + off0 * a.k_sr;
+                    const unsigned char *vr = vh + page[tt] * a.v_sp + off0 * a.v_sr;
+#pragma unroll
+                    for (int i = 0; i < C::NCH; ++i) {
+                        uint32_t kd, vd;
+                        chunk_place<C>(lane / C::CPR + i * (32 / C::CPR), lane % C::CPR, kd, vd);
+                        cp16(dst + kd, kr);
+                        cp16(dst + C::KB + vd, vr);
+                        kr += k_step; vr += v_step;
+                    }
+                    if (Q4) cp4(dst + 2 * C::KB + lane * 4, ph + ((long long)page[tt] * a.h_stored * a.page_size + off0));
                 } else {
-                    kd = vd = r * C::ROWB + ((c ^ (r & 7)) << 4);
+                    bad |= copy_ragged_tile<C>(a, dst, lc.b, hs, row0, lc.len);
                 }
-                cp16(st + kd, ok ? kr + c * 16 : a.k, ok);
-                cp16(st + C::KB + vd, ok ? vr + c * 16 : a.v, ok);
             }
-            if (Q4) {
-                const bool ok = page >= 0;
-                const uint32_t *src = (lane < 16 ? a.kp : a.vp) +
-                                      (ok ? ((long long)page * a.h_stored + hs) * a.page_size + my_off : 0);
-                cp4(st + 2 * C::KB + lane * 4, src, ok);
-            }
+            if (bad) bad_stages |= 1u << load_stage;
+            else bad_stages &= ~(1u << load_stage);
             if (++load_stage == S) load_stage = 0;
             ++jl;
             if (jl < j1) {
-                tile_advance(a, hv, lc);
-                page = fetch_page();
+                if (tile_advance<R>(a, hv, lc)) load_unit();
+                fetch_pages();
             }
         };
 #pragma unroll 1
@@ -406,13 +501,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
                     }
                 } else {
                     // Lane t holds features [t * D/4, (t+1) * D/4) of head g, in the order of the codes' words.
-                    float most = 0.f, sum = 0.f;
+                    uint4 raw[D / 32];
 #pragma unroll
-                    for (int i = 0; i < D / 4; ++i) {
-                        const float x = qh >= 0 ? load_as_float(a.q, base + t * (D / 4) + i, dtype) : 0.f;
-                        most = fmaxf(most, fabsf(x));
-                        sum += x;
-                    }
+                    for (int i = 0; i < D / 32; ++i)
+                        raw[i] = qh >= 0 ? *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + base + t * (D / 4) + 8 * i)
+                                         : make_uint4(0u, 0u, 0u, 0u);
+                    float most = 0.f, sum = 0.f;
+                    auto pair = [&](uint32_t r) { return dtype == MOA_BF16 ? unpack16<true>(r) : unpack16<false>(r); };
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 f = pair(reinterpret_cast<const uint32_t *>(&raw[i])[e]);
+                            most = fmaxf(most, fmaxf(fabsf(f.x), fabsf(f.y)));
+                            sum += f.x + f.y;
+                        }
 #pragma unroll
                     for (int off = 1; off < 4; off <<= 1) {
                         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
@@ -423,15 +526,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
                     e = e > 100 ? 100 : e < -100 ? -100 : e;
                     const float up = __uint_as_float((uint32_t)(127 + e) << 23), up16 = up * 0.0625f;
 #pragma unroll
-                    for (int i = 0; i < C::KSTEPS; ++i) {
-                        float x[4] = {0.f, 0.f, 0.f, 0.f};
-                        const long long at = base + t * (D / 4) + 8 * (i / 2) + 2 * (i & 1);
-                        if (qh >= 0) {
-                            x[0] = load_as_float(a.q, at, dtype); x[1] = load_as_float(a.q, at + 4, dtype);
-                            x[2] = load_as_float(a.q, at + 1, dtype); x[3] = load_as_float(a.q, at + 5, dtype);
-                        }
-                        qf[n][i][0] = pack16<false>(x[0] * up, x[1] * up);
-                        qf[n][i][1] = pack16<false>(x[2] * up16, x[3] * up16);
+                    for (int i = 0; i < D / 32; ++i) {     // word i: features 8i.. of the lane's; pairs (0,4) (1,5), then (2,6) (3,7)
+                        const float2 f01 = pair(raw[i].x), f23 = pair(raw[i].y), f45 = pair(raw[i].z), f67 = pair(raw[i].w);
+                        qf[n][2 * i][0] = pack16<false>(f01.x * up, f45.x * up);
+                        qf[n][2 * i][1] = pack16<false>(f01.y * up16, f45.y * up16);
+                        qf[n][2 * i + 1][0] = pack16<false>(f23.x * up, f67.x * up);
+                        qf[n][2 * i + 1][1] = pack16<false>(f23.y * up16, f67.y * up16);
                     }
                     const float down = __uint_as_float((uint32_t)(127 - e) << 23) * 16777216.0f * a.qscale;
                     sum *= a.qscale;
@@ -449,123 +549,136 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
                 for (int e = 0; e < 2; ++e) { s.m[n][e] = -INFINITY; s.msub[n][e] = 0.f; s.l[n][e] = 0.f; s.om[n][e] = 0.f; }
             }
             s.ref = 5.9604644775390625e-8f;                // 2^-24, fp16's least positive value
+            s.inv = 2147483648.0f;
         };
 
         // ---- one tile: scores, probabilities, weighted sum ----------------------------------
         auto process = [&](uint32_t st, int nr, bool bad) {
-            float x[NT][4];
-            float2 vpar[2] = {};                           // 4 bits: V's (scale, least) of this lane's two rows
-            const uint32_t sv = st + C::KB;
-            if constexpr (F32) {
+            float x[TT][NT][4];
+            float2 vpar[TT][2];                            // 4 bits: V's (scale, least) of this lane's two rows
+            const int tok = Q4 ? ((g & 1) << 2) | (g >> 1) : g;    // the row that score row g stands for (score row g + 8: 8 more)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int tt = 0; tt < TT; ++tt) {
+                const uint32_t sk = st + tt * C::TILE;
+                const unsigned char *skp = smem + (sk - smem_u);
+                if constexpr (F32) {
+                    float lh[NT][4] = {}, hl[NT][4] = {};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[n][e] = 0.f;
-                float lh[NT][4] = {}, hl[NT][4] = {};
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i4 = 0; i4 < D / 16; i4 += 2) {   // chains of four large products, added in fp32
-                    float hh[NT][4] = {};
+                        for (int e = 0; e < 4; ++e) x[tt][n][e] = 0.f;
 #pragma unroll
-                    for (int i = i4; i < i4 + 2; ++i) {
-                        const int ch = (t + 4 * i) ^ ((g & 1) << 2);
-                        float4 r0, r1;
-                        const unsigned char *p = ring + (st - ring_u) + g * C::ROWB + ch * 16;
-                        r0 = *reinterpret_cast<const float4 *>(p);
-                        r1 = *reinterpret_cast<const float4 *>(p + 8 * C::ROWB);
-                        const Split4 s0 = split4(r0), s1 = split4(r1);
+                    for (int i4 = 0; i4 < D / 16; i4 += 2) {   // chains of four large products, added in fp32
+                        float hh[NT][4] = {};
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t ah[4] = {s0.h[2 * e], s1.h[2 * e], s0.h[2 * e + 1], s1.h[2 * e + 1]};
-                            const uint32_t al[4] = {s0.l[2 * e], s1.l[2 * e], s0.l[2 * e + 1], s1.l[2 * e + 1]};
+                        for (int i = i4; i < i4 + 2; ++i) {
+                            const unsigned char *p = skp + g * C::ROWB + (((t + 4 * i) ^ ((g & 1) << 2)) << 4);
+                            const Split4 s0 = split4(*reinterpret_cast<const float4 *>(p));
+                            const Split4 s1 = split4(*reinterpret_cast<const float4 *>(p + 8 * C::ROWB));
 #pragma unroll
-                            for (int n = 0; n < NT; ++n)
-                                mma3(hh[n], lh[n], hl[n], ah, al, qf[n][2 * i + e][0], qf[n][2 * i + e][1],
-                                     qf[n][2 * i + e][C::QREGS - 2], qf[n][2 * i + e][C::QREGS - 1]);
+                            for (int e = 0; e < 2; ++e) {
+                                const uint32_t ah[4] = {s0.h[2 * e], s1.h[2 * e], s0.h[2 * e + 1], s1.h[2 * e + 1]};
+                                const uint32_t al[4] = {s0.l[2 * e], s1.l[2 * e], s0.l[2 * e + 1], s1.l[2 * e + 1]};
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+                                    mma3(hh[n], lh[n], hl[n], ah, al, qf[n][2 * i + e][0], qf[n][2 * i + e][1],
+                                         qf[n][2 * i + e][C::QREGS - 2], qf[n][2 * i + e][C::QREGS - 1]);
+                            }
                         }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[tt][n][e] += hh[n][e];
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[n][e] += hh[n][e];
-                }
+                        for (int e = 0; e < 4; ++e) x[tt][n][e] = (x[tt][n][e] + (lh[n][e] + hl[n][e])) * a.qscale;
+                } else if constexpr (!Q4) {
+                    float c[NT][4] = {};
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                    for (int i = 0; i < C::KSTEPS; ++i) {
+                        uint32_t r[4];
+                        ldsm4(r, sk + (lane & 15) * C::ROWB + (((2 * i + (lane >> 4)) ^ (lane & 7)) << 4));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[n][e] = (x[n][e] + (lh[n][e] + hl[n][e])) * a.qscale;
-            } else if constexpr (!Q4) {
-                float c[NT][4] = {};
+                        for (int n = 0; n < NT; ++n) mma_16x8x16<BF>(c[n], r[0], r[1], r[2], r[3], qf[n][i][0], qf[n][i][1]);
+                    }
 #pragma unroll
-                for (int i = 0; i < C::KSTEPS; ++i) {
-                    uint32_t r[4];
-                    ldsm4(r, st + (lane & 15) * C::ROWB + (((2 * i + (lane >> 4)) ^ (lane & 7)) << 4));
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma_16x8x16<BF>(c[n], r[0], r[1], r[2], r[3], qf[n][i][0], qf[n][i][1]);
-                }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[n][e] = c[n][e] * a.qscale;
-            } else {
-                constexpr int NW = D / 32;
-                uint32_t w0[NW], w1[NW];
-                const unsigned char *p = ring + (st - ring_u) + g * C::ROWB + t * (D / 8);
-                if constexpr (NW == 4) {
-                    *reinterpret_cast<uint4 *>(w0) = *reinterpret_cast<const uint4 *>(p);
-                    *reinterpret_cast<uint4 *>(w1) = *reinterpret_cast<const uint4 *>(p + 8 * C::ROWB);
+                        for (int e = 0; e < 4; ++e) x[tt][n][e] = c[n][e] * a.qscale;
                 } else {
-                    *reinterpret_cast<uint2 *>(w0) = *reinterpret_cast<const uint2 *>(p);
-                    *reinterpret_cast<uint2 *>(w1) = *reinterpret_cast<const uint2 *>(p + 8 * C::ROWB);
+                    constexpr int NW = D / 32;
+                    uint32_t w0[NW], w1[NW];
+                    const unsigned char *p = skp + g * C::ROWB + t * (D / 8);
+                    if constexpr (NW == 4) {
+                        *reinterpret_cast<uint4 *>(w0) = *reinterpret_cast<const uint4 *>(p);
+                        *reinterpret_cast<uint4 *>(w1) = *reinterpret_cast<const uint4 *>(p + 8 * C::ROWB);
+                    } else {
+                        *reinterpret_cast<uint2 *>(w0) = *reinterpret_cast<const uint2 *>(p);
+                        *reinterpret_cast<uint2 *>(w1) = *reinterpret_cast<const uint2 *>(p + 8 * C::ROWB);
+                    }
+                    const __half2 *par = reinterpret_cast<const __half2 *>(skp + 2 * C::KB);
+                    const float2 k0 = __half22float2(par[tok]), k1 = __half22float2(par[tok + 8]);
+                    vpar[tt][0] = __half22float2(par[16 + tok]);
+                    vpar[tt][1] = __half22float2(par[16 + tok + 8]);
+                    float c[NT][4] = {};
+#pragma unroll
+                    for (int w = 0; w < NW; ++w)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t u0 = e ? w0[w] >> 8 : w0[w], u1 = e ? w1[w] >> 8 : w1[w];
+                            const uint32_t a0 = u0 & 0x000f000fu, a2 = u0 & 0x00f000f0u, a1 = u1 & 0x000f000fu, a3 = u1 & 0x00f000f0u;
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma_16x8x16<false>(c[n], a0, a1, a2, a3, qf[n][2 * w + e][0], qf[n][2 * w + e][1]);
+                        }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            x[tt][n][e] = fmaf(k0.x, c[n][e] * fa[n][e], k0.y * fm[n][e]);
+                            x[tt][n][2 + e] = fmaf(k1.x, c[n][2 + e] * fa[n][e], k1.y * fm[n][e]);
+                        }
                 }
-                const int tok = ((g & 1) << 2) | (g >> 1); // the row that score row g stands for (score row g + 8: 8 more)
-                const __half2 *par = reinterpret_cast<const __half2 *>(ring + (st - ring_u) + 2 * C::KB);
-                const float2 k0 = __half22float2(par[tok]), k1 = __half22float2(par[tok + 8]);
-                vpar[0] = __half22float2(par[16 + tok]);
-                vpar[1] = __half22float2(par[16 + tok + 8]);
-                float c[NT][4] = {};
-#pragma unroll
-                for (int w = 0; w < NW; ++w)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t u0 = e ? w0[w] >> 8 : w0[w], u1 = e ? w1[w] >> 8 : w1[w];
-                        const uint32_t a0 = u0 & 0x000f000fu, a2 = u0 & 0x00f000f0u, a1 = u1 & 0x000f000fu, a3 = u1 & 0x00f000f0u;
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) mma_16x8x16<false>(c[n], a0, a1, a2, a3, qf[n][2 * w + e][0], qf[n][2 * w + e][1]);
-                    }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        x[n][e] = fmaf(k0.x, c[n][e] * fa[n][e], k0.y * fm[n][e]);
-                        x[n][2 + e] = fmaf(k1.x, c[n][2 + e] * fa[n][e], k1.y * fm[n][e]);
-                    }
             }
-            if (nr < 16) {                                 // rows behind the last one
-                const int r0 = Q4 ? ((g & 1) << 2) | (g >> 1) : g;
+            if (nr < R) {                                  // rows behind the last one
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        if (r0 >= nr) x[n][e] = -INFINITY;
-                        if (r0 + 8 >= nr) x[n][2 + e] = -INFINITY;
-                    }
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (16 * tt + tok >= nr) x[tt][n][e] = -INFINITY;
+                            if (16 * tt + tok + 8 >= nr) x[tt][n][2 + e] = -INFINITY;
+                        }
             }
             // The reference maximum moves only when a score exceeds it by more than 8 (a factor of
             // 256, far inside the range of every format used here): rarely after the first tiles.
+            float top[NT][2], vtop = 0.f;
             bool up = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) up |= x[n][e] > s.m[n][e & 1] + 8.0f;
-            if (Q4) up |= vpar[0].x > s.ref || vpar[1].x > s.ref;
+                for (int e = 0; e < 2; ++e) {
+                    top[n][e] = fmaxf(x[0][n][e], x[0][n][2 + e]);
+#pragma unroll
+                    for (int tt = 1; tt < TT; ++tt) top[n][e] = fmaxf(top[n][e], fmaxf(x[tt][n][e], x[tt][n][2 + e]));
+                    up |= top[n][e] > s.m[n][e] + 8.0f;
+                }
+            if constexpr (Q4) {
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt) vtop = fmaxf(vtop, fmaxf(vpar[tt][0].x, vpar[tt][1].x));
+                up |= vtop > s.ref;
+            }
             if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(x[n][e], x[n][2 + e]);
+                        float most = top[n][e];
 #pragma unroll
-                        for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                        const float m_new = fmaxf(s.m[n][e], top);
+                        for (int off = 4; off < 32; off <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+                        const float m_new = fmaxf(s.m[n][e], most);
                         const float alpha = exp2_diff(s.m[n][e], m_new);
                         s.m[n][e] = m_new;
                         s.msub[n][e] = m_new == -INFINITY ? 0.f : m_new;
@@ -574,12 +687,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
 #pragma unroll
                         for (int i = 0; i < MT; ++i) { s.acc[n][i][e] *= alpha; s.acc[n][i][2 + e] *= alpha; }
                     }
-                if (Q4) {
-                    float top = fmaxf(vpar[0].x, vpar[1].x);
+                if constexpr (Q4) {
 #pragma unroll
-                    for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                    if (top > s.ref) {                     // next power of two (2^16 at most: scales are fp16)
-                        const float r = __uint_as_float((__float_as_uint(top) + 0x7fffffu) & 0x7f800000u);
+                    for (int off = 4; off < 32; off <<= 1) vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, off));
+                    if (vtop > s.ref) {                    // next power of two (2^16 at most: scales are fp16)
+                        const float r = __uint_as_float((__float_as_uint(vtop) + 0x7fffffu) & 0x7f800000u);
                         const float f = s.ref / r;
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
@@ -588,6 +700,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) s.acc[n][i][e] *= f;
                         s.ref = r;
+                        s.inv = 128.0f / r;                // exact: weights reach 2^15 at most
                     }
                 }
             }
@@ -595,108 +708,117 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
 #pragma unroll
                 for (int n = 0; n < NT; ++n) s.l[n][0] = s.l[n][1] = __int_as_float(0x7fffffff);
             }
-            float p[NT][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[n][e] = fast_exp2(x[n][e] - s.msub[n][e & 1]);
-                    s.l[n][e & 1] += p[n][e];
-                }
-            if constexpr (F32) {
-                float4 vr[2][2];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    // P^T as B operand: row t (+4) of each 8-row half, head g
-                    uint32_t bh[4], bl[4];                 // rows t, t+4, 8+t, 12+t
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const int src = (t + (h & 1) * 4) * 4 + (g >> 1);
-                        const float y0 = __shfl_sync(0xffffffffu, p[n][(h >> 1) * 2], src);
-                        const float y1 = __shfl_sync(0xffffffffu, p[n][(h >> 1) * 2 + 1], src);
-                        const float y = (g & 1) ? y1 : y0;
-                        bh[h] = (__float_as_uint(y) + 0x1000u) & 0xFFFFE000u;
-                        bl[h] = (__float_as_uint(y - __uint_as_float(bh[h])) + 0x1000u) & 0xFFFFE000u;
-                    }
-#pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) {
-                            const int r = t + (h & 1) * 4 + (h >> 1) * 8;
-                            const int ch = (g + 8 * i) ^ ((r & 3) << 1);
-                            vr[h >> 1][h & 1] = *reinterpret_cast<const float4 *>(ring + (sv - ring_u) + r * C::ROWB + ch * 16);
-                        }
-                        Split4 v[2][2];
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) v[h >> 1][h & 1] = split4(vr[h >> 1][h & 1]);
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {      // output tile 2i + e: features 4(g + 8i) + 2e, + 1
-                            float hh[4] = {}, lh[4] = {}, hl[4] = {};
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const uint32_t ah[4] = {v[k][0].h[2 * e], v[k][0].h[2 * e + 1], v[k][1].h[2 * e], v[k][1].h[2 * e + 1]};
-                                const uint32_t al[4] = {v[k][0].l[2 * e], v[k][0].l[2 * e + 1], v[k][1].l[2 * e], v[k][1].l[2 * e + 1]};
-                                mma3(hh, lh, hl, ah, al, bh[2 * k], bh[2 * k + 1], bl[2 * k], bl[2 * k + 1]);
-                            }
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) s.acc[n][2 * i + e][z] += hh[z] + (lh[z] + hl[z]);
-                        }
-                    }
-                }
-            } else if constexpr (!Q4) {
-                uint32_t hi[NT][2], lo[NT][2];
+            for (int tt = 0; tt < TT; ++tt) {
+                const uint32_t sv = st + tt * C::TILE + C::KB;
+                const unsigned char *svp = smem + (sv - smem_u);
+                float p[NT][4];
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t r = pack16<BF>(p[n][2 * h], p[n][2 * h + 1]);
-                        const float2 f = unpack16<BF>(r);
-                        hi[n][h] = movmatrix_trans(r);
-                        lo[n][h] = movmatrix_trans(pack16<BF>(p[n][2 * h] - f.x, p[n][2 * h + 1] - f.y));
+                    for (int e = 0; e < 4; ++e) {
+                        p[n][e] = fast_exp2(x[tt][n][e] - s.msub[n][e & 1]);
+                        s.l[n][e & 1] += p[n][e];
                     }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    uint32_t r[4];
-                    const int row = (lane & 7) + ((lane >> 4) << 3);
-                    ldsm4t(r, sv + row * C::ROWB + (((2 * i + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+                if constexpr (F32) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        mma_16x8x16<BF>(s.acc[n][i], r[0], r[1], r[2], r[3], lo[n][0], lo[n][1]);
-                        mma_16x8x16<BF>(s.acc[n][i], r[0], r[1], r[2], r[3], hi[n][0], hi[n][1]);
+                        // P^T as B operand: row t (+4) of each 8-row half, head g
+                        uint32_t bh[4], bl[4];             // rows t, t+4, 8+t, 12+t
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            const int src = (t + (h & 1) * 4) * 4 + (g >> 1);
+                            const float y0 = __shfl_sync(0xffffffffu, p[n][(h >> 1) * 2], src);
+                            const float y1 = __shfl_sync(0xffffffffu, p[n][(h >> 1) * 2 + 1], src);
+                            const float y = (g & 1) ? y1 : y0;
+                            bh[h] = (__float_as_uint(y) + 0x1000u) & 0xFFFFE000u;
+                            bl[h] = (__float_as_uint(y - __uint_as_float(bh[h])) + 0x1000u) & 0xFFFFE000u;
+                        }
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) {
+                            Split4 v[2][2];
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) {
+                                const int r = t + (h & 1) * 4 + (h >> 1) * 8;
+                                v[h >> 1][h & 1] = split4(*reinterpret_cast<const float4 *>(svp + r * C::ROWB + (((g + 8 * i) ^ ((r & 3) << 1)) << 4)));
+                            }
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {  // output tile 2i + e: features 4(g + 8i) + 2e, + 1
+                                float hh[4] = {}, lh[4] = {}, hl[4] = {};
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const uint32_t ah[4] = {v[k][0].h[2 * e], v[k][0].h[2 * e + 1], v[k][1].h[2 * e], v[k][1].h[2 * e + 1]};
+                                    const uint32_t al[4] = {v[k][0].l[2 * e], v[k][0].l[2 * e + 1], v[k][1].l[2 * e], v[k][1].l[2 * e + 1]};
+                                    mma3(hh, lh, hl, ah, al, bh[2 * k], bh[2 * k + 1], bl[2 * k], bl[2 * k + 1]);
+                                }
+#pragma unroll
+                                for (int z = 0; z < 4; ++z) s.acc[n][2 * i + e][z] += hh[z] + (lh[z] + hl[z]);
+                            }
+                        }
                     }
-                }
-            } else {
-                const float inv = 128.0f / s.ref;          // exact: a power of two; weights reach 2^15 at most
-                const float s0 = vpar[0].x * inv, s1 = vpar[1].x * inv;
-                uint32_t wt[NT][2];
+                } else if constexpr (!Q4) {
+                    uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    wt[n][0] = movmatrix_trans(pack16<false>(p[n][0] * s0, p[n][1] * s0));
-                    wt[n][1] = movmatrix_trans(pack16<false>(p[n][2] * s1, p[n][3] * s1));
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) s.om[n][e] += fmaf(p[n][e], vpar[0].y, p[n][2 + e] * vpar[1].y);
-                }
-                constexpr int NW = D / 64;
-                uint32_t w[4][NW];                         // rows t, 4 + t, 8 + t, 12 + t: what the weights' columns stand for
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t r = pack16<BF>(p[n][2 * h], p[n][2 * h + 1]);
+                            const float2 f = unpack16<BF>(r);
+                            hi[n][h] = movmatrix_trans(r);
+                            lo[n][h] = movmatrix_trans(pack16<BF>(p[n][2 * h] - f.x, p[n][2 * h + 1] - f.y));
+                        }
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const int r = t + 4 * h;
-                    const unsigned char *src = ring + (sv - ring_u) + r * C::ROWB + ((g * (D / 16)) ^ (D == 128 ? ((r >> 1) & 1) << 5 : 0));
-                    if constexpr (NW == 2) *reinterpret_cast<uint2 *>(w[h]) = *reinterpret_cast<const uint2 *>(src);
-                    else w[h][0] = *reinterpret_cast<const uint32_t *>(src);
-                }
+                    for (int i = 0; i < MT; ++i) {
+                        uint32_t r[4];
+                        const int row = (lane & 7) + ((lane >> 4) << 3);
+                        ldsm4t(r, sv + row * C::ROWB + (((2 * i + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
 #pragma unroll
-                for (int i = 0; i < NW; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {          // output tile 4i + e: features 2e and 2e + 1 of the word
-                        uint32_t u0 = __byte_perm(w[0][i], w[1][i], e < 2 ? 0x5410 : 0x7632);
-                        uint32_t u1 = __byte_perm(w[2][i], w[3][i], e < 2 ? 0x5410 : 0x7632);
-                        if (e & 1) { u0 >>= 8; u1 >>= 8; }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            mma_16x8x16<false>(s.acc[n][4 * i + e], u0 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x000f000fu,
-                                               u1 & 0x00f000f0u, wt[n][0], wt[n][1]);
+                        for (int n = 0; n < NT; ++n) {
+                            mma_16x8x16<BF>(s.acc[n][i], r[0], r[1], r[2], r[3], lo[n][0], lo[n][1]);
+                            mma_16x8x16<BF>(s.acc[n][i], r[0], r[1], r[2], r[3], hi[n][0], hi[n][1]);
+                        }
                     }
+                } else {
+                    const float s0 = vpar[tt][0].x * s.inv, s1 = vpar[tt][1].x * s.inv;
+                    uint32_t wt[NT][2], wl[NT][2];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint32_t r0 = pack16<false>(p[n][0] * s0, p[n][1] * s0), r1 = pack16<false>(p[n][2] * s1, p[n][3] * s1);
+                        wt[n][0] = movmatrix_trans(r0);
+                        wt[n][1] = movmatrix_trans(r1);
+                        if (fine) {                        // second terms of the weights
+                            const float2 f0 = unpack16<false>(r0), f1 = unpack16<false>(r1);
+                            wl[n][0] = movmatrix_trans(pack16<false>(fmaf(p[n][0], s0, -f0.x), fmaf(p[n][1], s0, -f0.y)));
+                            wl[n][1] = movmatrix_trans(pack16<false>(fmaf(p[n][2], s1, -f1.x), fmaf(p[n][3], s1, -f1.y)));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) s.om[n][e] = fmaf(p[n][e], vpar[tt][0].y, fmaf(p[n][2 + e], vpar[tt][1].y, s.om[n][e]));
+                    }
+                    constexpr int NW = D / 64;
+                    uint32_t w[4][NW];                     // rows t, 4 + t, 8 + t, 12 + t: what the weights' columns stand for
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const int r = t + 4 * h;
+                        const unsigned char *src = svp + r * C::ROWB + ((g * (D / 16)) ^ (D == 128 ? ((r >> 1) & 1) << 5 : 0));
+                        if constexpr (NW == 2) *reinterpret_cast<uint2 *>(w[h]) = *reinterpret_cast<const uint2 *>(src);
+                        else w[h][0] = *reinterpret_cast<const uint32_t *>(src);
+                    }
+#pragma unroll
+                    for (int i = 0; i < NW; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {      // output tile 4i + e: features 2e and 2e + 1 of the word
+                            uint32_t u0 = __byte_perm(w[0][i], w[1][i], e < 2 ? 0x5410 : 0x7632);
+                            uint32_t u1 = __byte_perm(w[2][i], w[3][i], e < 2 ? 0x5410 : 0x7632);
+                            if (e & 1) { u0 >>= 8; u1 >>= 8; }
+                            const uint32_t a0 = u0 & 0x000f000fu, a1 = u0 & 0x00f000f0u, a2 = u1 & 0x000f000fu, a3 = u1 & 0x00f000f0u;
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][4 * i + e], a0, a1, a2, a3, wt[n][0], wt[n][1]);
+                            if (fine) {
+#pragma unroll
+                                for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][4 * i + e], a0, a1, a2, a3, wl[n][0], wl[n][1]);
+                            }
+                        }
+                }
             }
         };
 
@@ -755,7 +877,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
             if (fresh) { begin_unit(); fresh = false; }
             cp_wait<S - 1>();
             __syncwarp();
-            process(ring_u + stage * C::STAGE, min(16, cc.len - cc.i * 16), (bad_stages >> stage) & 1u);
+            process(ring_u + stage * C::STAGE, cc.len - cc.i * R, (bad_stages >> stage) & 1u);
             __syncwarp();                                  // every lane is done with the stage
             if (++stage == S) stage = 0;
             if (jl < j1) issue();
@@ -776,98 +898,142 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const Paged
                 }
                 if (unit_ends) { unit_lo += cc.ub; fresh = true; }
             }
-            if (j + 1 < j1) tile_advance(a, hv, cc);
+            if (j + 1 < j1) tile_advance<R>(a, hv, cc);
         }
     }
     __syncthreads();
 
     // ---- join the pieces of units that this CTA's warps share -------------------------------
-    if (warp == 0) {
-        const long long u = s_seg[lane];
-        const unsigned valid = __ballot_sync(0xffffffffu, u >= 0);
-        const unsigned below = valid & ((1u << lane) - 1u);
-        const int prev = below ? 31 - __clz(below) : lane;
-        const long long pu = __shfl_sync(0xffffffffu, u, prev);
-        const bool leads = u >= 0 && (below == 0 || pu != u);
-        const unsigned leaders = __ballot_sync(0xffffffffu, leads);
-        if (leads) {
-            const int k = __popc(leaders & ((1u << lane) - 1u));
-            const unsigned above = lane < 31 ? leaders >> (lane + 1) : 0u;
-            s_grp_lo[k] = lane;
-            s_grp_hi[k] = above ? lane + __ffs(above) : 32;
+    // Every warp works out the groups of segments for itself: segment `lane` leads a group when
+    // the valid segment before it belongs to another unit.
+    const long long u = s_seg[lane];
+    const unsigned valid = __ballot_sync(0xffffffffu, u >= 0);
+    if (valid == 0) return;                                // uniform for the CTA: nothing was cut
+    const unsigned below = valid & ((1u << lane) - 1u);
+    const long long pu = __shfl_sync(0xffffffffu, u, below ? 31 - __clz(below) : lane);
+    const unsigned leaders = __ballot_sync(0xffffffffu, u >= 0 && (below == 0 || pu != u));
+    auto members = [&](int lead) -> unsigned {             // segments of the group that segment `lead` leads
+        const unsigned next = lead < 31 ? leaders >> (lead + 1) : 0u;
+        return valid & (next ? (1u << (lead + __ffs(next))) - (1u << lead) : 0u - (1u << lead));
+    };
+    auto seg_slot = [&](int sg) -> float * {
+        const int w = sg >> 1;
+        return (sg & 1) ? reinterpret_cast<float *>(smem + (size_t)w * S * C::STAGE) : first_slots + (size_t)w * C::SLOT;
+    };
+    auto cut = [&](int lead) { return s_seg_lo[lead] < c0 || s_seg_lo[lead] + s_seg_ub[lead] > c1; };
+    constexpr int LPR = D / 4, COLS = G * LPR;
+
+    // Factors: of every segment and head, 2^(m - M), beside the partial; for the leader the sum L too.
+    for (int idx = tid; idx < 2 * W * G; idx += C::THREADS) {
+        const int sg = idx / G, head = idx % G;
+        if (!(valid >> sg & 1u)) continue;
+        const int lead = 31 - __clz(leaders & (0xffffffffu >> (31 - sg)));
+        const unsigned mem = members(lead);
+        float M = -INFINITY;
+        for (unsigned r = mem; r != 0; r &= r - 1) M = fmaxf(M, seg_slot(__ffs(r) - 1)[head * PS + D]);
+        float *p = seg_slot(sg) + head * PS;
+        p[D + 2] = exp2_diff(p[D], M);
+        if (sg == lead) {
+            float L = 0.f;
+            for (unsigned r = mem; r != 0; r &= r - 1) {
+                const float *x = seg_slot(__ffs(r) - 1) + head * PS;
+                L = fmaf(exp2_diff(x[D], M), x[D + 1], L);
+            }
+            p[D + 3] = L;
+            s_top[lead][head] = M;
         }
-        if (lane == 0) s_ngrp = __popc(leaders);
     }
     __syncthreads();
-    constexpr int LPR = D / 4, COLS = G * LPR;
-    auto seg_slot = [&](int sg) -> const float * {
-        const int w = sg >> 1;
-        return (sg & 1) ? reinterpret_cast<const float *>(smem + (size_t)w * S * C::STAGE) : first_slots + (size_t)w * C::SLOT;
-    };
-    const int ngrp = s_ngrp;
-    for (int idx = tid; idx < ngrp * COLS; idx += C::THREADS) {
-        const int k = idx / COLS, col = idx % COLS, head = col / LPR, d = (col % LPR) * 4;
-        const int lo = s_grp_lo[k], hi = s_grp_hi[k];
-        float M = -INFINITY;
-        for (int sg = lo; sg < hi; ++sg)
-            if (s_seg[sg] >= 0) M = fmaxf(M, seg_slot(sg)[head * PS + D]);
+    auto join = [&](int lead, int col) {
+        const int head = col / LPR, d = (col % LPR) * 4;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        float L = 0.f;
-        for (int sg = lo; sg < hi; ++sg) {
-            if (s_seg[sg] < 0) continue;
-            const float *p = seg_slot(sg) + head * PS;
-            const float f = exp2_diff(p[D], M);
+        for (unsigned r = members(lead); r != 0; r &= r - 1) {
+            const float *p = seg_slot(__ffs(r) - 1) + head * PS;
+            const float f = p[D + 2];
             const float4 y = *reinterpret_cast<const float4 *>(p + d);
             o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
-            L = fmaf(f, p[D + 1], L);
         }
-        const long long ulo = s_seg_lo[lo], uhi = ulo + s_seg_ub[lo];
-        if (ulo >= c0 && uhi <= c1) {
-            const int qh = paged_query_head(a, s_seg_b[lo], s_seg_vh[lo], head);
-            const float inv = 1.0f / L;
-            if (qh >= 0)
-                store4(a.out, ((long long)s_seg_b[lo] * a.h_q + qh) * D + d,
-                       make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), dtype);
-        } else {
-            float *p = a.ws + ((size_t)blockIdx.x * 2 + (ulo <= c0 ? 0 : 1)) * C::SLOT + head * PS;
-            *reinterpret_cast<float4 *>(p + d) = o;
-            if (d == 0) { p[D] = M; p[D + 1] = L; }
-        }
-    }
-
-    // ---- units cut between CTAs: whoever delivers the last piece joins them ------------------
-    for (int k = 0; k < ngrp; k += (ngrp > 1 ? ngrp - 1 : 1)) {       // only the first and the last group can be cut
-        const int sg = s_grp_lo[k];
-        const long long ulo = s_seg_lo[sg], uhi = ulo + s_seg_ub[sg];
-        if (ulo >= c0 && uhi <= c1) continue;              // uniform for the CTA
-        const int first = (int)(((ulo + 1) * active - 1) / total), last = (int)((uhi * active - 1) / total);
-        __syncthreads();                                   // the pieces are written; s_last is free
-        if (tid == 0) {
-            __threadfence();
-            const int done = ticket_arrive(&a.tickets[first], a.ticket_tag) == (unsigned)(last - first);
-            if (done) a.tickets[first] = 0ull;
-            s_last = done;
+        return o;
+    };
+    // Units cut between CTAs first (the first group, the last, or both): their partials leave, and
+    // are counted while the whole units are joined.
+    const int lead0 = __ffs(leaders) - 1, lead1 = 31 - __clz(leaders);
+    const bool cut0 = cut(lead0), cut1 = lead1 != lead0 && cut(lead1);
+    if (cut0 || cut1) {
+        for (int idx = tid; idx < 2 * COLS; idx += C::THREADS) {
+            const bool second = idx >= COLS;
+            if (second ? !cut1 : !cut0) continue;
+            const int lead = second ? lead1 : lead0, col = second ? idx - COLS : idx, head = col / LPR, d = (col % LPR) * 4;
+            float *p = a.ws + ((size_t)blockIdx.x * 2 + (s_seg_lo[lead] <= c0 ? 0 : 1)) * C::SLOT + head * PS;
+            *reinterpret_cast<float4 *>(p + d) = join(lead, col);
+            if (d == 0) { p[D] = s_top[lead][head]; p[D + 1] = seg_slot(lead)[head * PS + D + 3]; }
         }
         __syncthreads();
-        if (!s_last) continue;
-        __threadfence();
-        const int b = s_seg_b[sg], vh = s_seg_vh[sg];
+        if (tid < 2) {                                     // one thread per cut unit
+            const int lead = tid ? lead1 : lead0;
+            int done = 0;
+            if (tid ? cut1 : cut0) {
+                const long long ulo = s_seg_lo[lead], uhi = ulo + s_seg_ub[lead];
+                const int first = part_of(total, ulo, active), last = part_of(total, uhi - 1, active);
+                asm volatile("fence.acq_rel.gpu;" ::: "memory");
+                done = ticket_arrive(&a.tickets[first], a.ticket_tag) == (unsigned)(last - first);
+                if (done) a.tickets[first] = 0ull;
+                asm volatile("fence.acq_rel.gpu;" ::: "memory");
+            }
+            s_done[tid] = done;
+        }
+    }
+    for (int idx = tid; idx < __popc(leaders) * COLS; idx += C::THREADS) {
+        unsigned r = leaders;
+        for (int k = idx / COLS; k > 0; --k) r &= r - 1;
+        const int lead = __ffs(r) - 1, col = idx % COLS, head = col / LPR, d = (col % LPR) * 4;
+        if (cut(lead)) continue;
+        const float4 o = join(lead, col);
+        const int b = s_seg_b[lead], qh = paged_query_head(a, b, s_seg_vh[lead], head);
+        const float inv = 1.0f / seg_slot(lead)[head * PS + D + 3];
+        if (qh >= 0)
+            store4(a.out, ((long long)b * a.h_q + qh) * D + d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), dtype);
+    }
+    if (!cut0 && !cut1) return;
+
+    // ---- units cut between CTAs: whoever delivers the last piece joins them, in CTA order -----
+    __syncthreads();
+    for (int k = 0; k < 2; ++k) {
+        if (!s_done[k]) continue;                          // uniform for the CTA
+        const int lead = k ? lead1 : lead0;
+        const long long ulo = s_seg_lo[lead], uhi = ulo + s_seg_ub[lead];
+        const int first = part_of(total, ulo, active), last = part_of(total, uhi - 1, active);
+        const int slot0 = ulo == split_at(total, first, active) ? 0 : 1;      // a CTA's slot 0: the unit that its range begins in
+        const int b = s_seg_b[lead], vh = s_seg_vh[lead];
         for (int col = tid; col < COLS; col += C::THREADS) {
             const int head = col / LPR, d = (col % LPR) * 4;
-            auto slot = [&](int c) -> const float * {      // slot 0 of a CTA: the unit that its range begins in
-                return a.ws + ((size_t)c * 2 + (c > first || ulo == total * c / active ? 0 : 1)) * C::SLOT + head * PS;
-            };
-            float M = -INFINITY;
-#pragma unroll 4
-            for (int c = first; c <= last; ++c) M = fmaxf(M, __ldcg(slot(c) + D));
+            float M = -INFINITY, L = 0.f, Lc = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f), oc = o;
-            float L = 0.f, Lc = 0.f;
-#pragma unroll 4
-            for (int c = first; c <= last; ++c) {
-                const float *p = slot(c);
-                const float f = exp2_diff(__ldcg(p + D), M);
-                comp_fma4(o, oc, __ldcg(reinterpret_cast<const float4 *>(p + d)), f);
-                comp_fma(L, Lc, __ldcg(p + D + 1), f);
+            constexpr int B = 4;                           // partials under way at once
+            for (int c = first; c <= last; c += B) {
+                float4 y[B];
+                float2 ml[B];
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    const float *p = a.ws + ((size_t)min(c + i, last) * 2 + (c + i > first ? 0 : slot0)) * C::SLOT + head * PS;
+                    y[i] = __ldcg(reinterpret_cast<const float4 *>(p + d));
+                    ml[i] = __ldcg(reinterpret_cast<const float2 *>(p + D));
+                    if (c + i > last) ml[i] = make_float2(-INFINITY, 0.f);
+                }
+                float Mn = M;
+#pragma unroll
+                for (int i = 0; i < B; ++i) Mn = fmaxf(Mn, ml[i].x);
+                const float keep = exp2_diff(M, Mn);
+                o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep; L *= keep;
+                oc.x *= keep; oc.y *= keep; oc.z *= keep; oc.w *= keep; Lc *= keep;
+                M = Mn;
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    if (c + i > last) break;
+                    const float f = exp2_diff(ml[i].x, M);
+                    comp_fma4(o, oc, y[i], f);
+                    comp_fma(L, Lc, ml[i].y, f);
+                }
             }
             const int qh = paged_query_head(a, b, vh, head);
             const float inv = 1.0f / L;
