@@ -1027,16 +1027,22 @@ static PagedIoArgs paged_io_args(const moa_paged_cache *c, const long long *ks, 
     return a;
 }
 
+template <int FMT, int DT, int D>
+static cudaError_t launch_append(const PagedIoArgs &a, cudaStream_t st)
+{
+    const long long rows = (long long)a.tokens * (a.q_runs + 2 * a.kv_runs), per_block = 256 / (D / 16);
+    const int blocks = (int)((rows + per_block - 1) / per_block);
+    if (a.rot == 0) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnNone>, blocks, 256, 0, st, a);
+    else if (a.pairs) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnPairs>, blocks, 256, 0, st, a);
+    else if (a.rot % 16 == 0) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnChunks>, blocks, 256, 0, st, a);
+    else launch_dependent(paged_append_kernel<FMT, DT, D, kTurnAny>, blocks, 256, 0, st, a);
+    count_launch();
+    return cudaGetLastError();
+}
 template <int FMT, int DT>
 static cudaError_t launch_append(const PagedIoArgs &a, int d, cudaStream_t st)
 {
-    const int heads = a.h_q + 2 * a.h_kv, runs = (heads + a.heads_per_thread - 1) / a.heads_per_thread;
-    const long long rows = (long long)a.tokens * runs, per_block = 256 / (d / 16);
-    const int blocks = (int)((rows + per_block - 1) / per_block);
-    if (d == 128) launch_dependent(paged_append_kernel<FMT, DT, 128>, blocks, 256, 0, st, a);
-    else launch_dependent(paged_append_kernel<FMT, DT, 64>, blocks, 256, 0, st, a);
-    count_launch();
-    return cudaGetLastError();
+    return d == 128 ? launch_append<FMT, DT, 128>(a, st) : launch_append<FMT, DT, 64>(a, st);
 }
 
 static int paged_append_impl(const moa_paged_cache *c, const void *q, const void *k, const void *v, void *q_out, int dtype,
@@ -1081,7 +1087,12 @@ static int paged_append_impl(const moa_paged_cache *c, const void *q, const void
     a.q_st = s[0]; a.k_st = s[1]; a.v_st = s[2]; a.o_st = s[3];
     a.tokens = tokens; a.h_q = h_q; a.token_start = token_start;
     a.cos_sin = cos_sin; a.rope_rows = rope_rows; a.rot = rot_dim; a.pairs = rope_style == MOA_ROPE_PAIRS;
-    a.heads_per_thread = rows >= 32768 ? 4 : 1;
+    // Heads of one run: 8 share the search for the token's sequence and page and its cosines and sines
+    // where there are rows enough to fill the GPU that way, one where there are not.
+    const long long fill = (long long)dev->sm_count * 1024 / (c->d / 16);
+    a.run = rows >= 8 * fill ? 8 : rows >= 4 * fill ? 4 : rows >= 2 * fill ? 2 : 1;
+    a.q_runs = (h_q + a.run - 1) / a.run;
+    a.kv_runs = (c->h_kv + a.run - 1) / a.run;
     cudaError_t e;
     switch (c->format) {
     case MOA_KV_F32: e = launch_append<MOA_KV_F32, MOA_F32>(a, c->d, st); break;

@@ -4,7 +4,8 @@
 // Both are bound by memory.  A row (one head of one token) belongs to D/16 neighbouring threads of a
 // warp, 16 features each, as two chunks of 8 (16 bytes in 16-bit types): under the rotation of
 // halves the two chunks are each other's partners, so no value crosses threads.  A thread takes
-// several heads of its token in turn and keeps the token's cosines and sines in registers.
+// several heads of its token, all of q, all of k or all of v, in turn: the token's sequence, page,
+// cosines and sines are found once, and the next row is under way while one is turned.
 //
 // Every product, sum and quotient below is rounded on its own (no contraction into fused
 // multiply-adds): what a row holds is then defined by the formulas alone, and equals what any
@@ -29,7 +30,8 @@ struct PagedIoArgs {
     const void *q, *k, *v;
     void *q_out;
     long long q_st, k_st, v_st, o_st;    // elements between consecutive tokens
-    int tokens, h_q, heads_per_thread;
+    int tokens, h_q;
+    int run, q_runs, kv_runs;        // heads that a thread takes; runs of them in q, and in k (as many in v)
     const int32_t *token_start;      // [batch + 1], or null: token t belongs to sequence t
     const float *cos_sin;            // [rope_rows, rot]: rot/2 cosines, rot/2 sines
     int rope_rows, rot;
@@ -84,10 +86,10 @@ __device__ __forceinline__ void turn(float &x, float &y, float c, float s)
 // A row in 4 bits: s = fp16((max - min) / 15), m = fp16(min), code = round((x - m) / s) in 0..15.
 // The quotient by 15 is a product with fp32's nearest to 1/15.  Rows beyond fp16's range are held
 // as if cut off there; a row with a value that is no number or infinite reads back as NaN.
-// lo, hi: this thread's two chunks; the D/16 threads of a row are neighbours.
+// lo, hi: this thread's two chunks; the D/16 threads of a row are neighbours, `mask` their lanes.
 template <int D>
 __device__ __forceinline__ void pack_row(const float (&lo)[8], const float (&hi)[8], uint32_t &c_lo, uint32_t &c_hi,
-                                         uint32_t &params)
+                                         uint32_t &params, unsigned mask)
 {
     float mn = lo[0], mx = lo[0];
     bool odd = false;
@@ -100,9 +102,9 @@ __device__ __forceinline__ void pack_row(const float (&lo)[8], const float (&hi)
     int bad = odd;
 #pragma unroll
     for (int off = 1; off < D / 16; off <<= 1) {
-        mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-        bad |= __shfl_xor_sync(0xffffffffu, bad, off);
+        mn = fminf(mn, __shfl_xor_sync(mask, mn, off));
+        mx = fmaxf(mx, __shfl_xor_sync(mask, mx, off));
+        bad |= __shfl_xor_sync(mask, bad, off);
     }
     const float top = 65504.0f;
     const __half s16 = __float2half_rn(fminf(__fmul_rn(__fsub_rn(mx, mn), 1.0f / 15.0f), top));
@@ -122,129 +124,141 @@ __device__ __forceinline__ void pack_row(const float (&lo)[8], const float (&hi)
     params = (uint32_t)__half_as_ushort(s16) | ((uint32_t)__half_as_ushort(m16) << 16);
 }
 
-// FMT: of the pools; DT: of q, k, v.  The same for 16 and 32 bits.
-template <int FMT, int DT, int D>
-__global__ void __launch_bounds__(256) paged_append_kernel(const PagedIoArgs a)
+// How the pairs that turn together lie: none, in a thread's two chunks (halves, rot a multiple of 16),
+// next to each other, or anywhere (halves of another size: partners are fetched one by one).
+enum PagedTurn { kTurnNone, kTurnChunks, kTurnPairs, kTurnAny };
+
+// Two chunks of a row as they are loaded.
+template <int DT> struct RowPart { uint4 u[DT == MOA_F32 ? 4 : 2]; };
+template <int DT>
+__device__ __forceinline__ void fetch(RowPart<DT> &r, const unsigned char *row, int d_lo, int d_hi)
 {
-    constexpr int TPR = D / 16, SLOTS = 256 / TPR, ES = DT == MOA_F32 ? 4 : 2;
+    constexpr int ES = DT == MOA_F32 ? 4 : 2, N = DT == MOA_F32 ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        r.u[i] = *reinterpret_cast<const uint4 *>(row + d_lo * ES + 16 * i);
+        r.u[N + i] = *reinterpret_cast<const uint4 *>(row + d_hi * ES + 16 * i);
+    }
+}
+
+// FMT: of the pools; DT: of q, k, v.  The same for 16 and 32 bits.
+template <int FMT, int DT, int D, int TURN>
+__global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || FMT == MOA_KV_INT4 ? 3 : 4) paged_append_kernel(const __grid_constant__ PagedIoArgs a)
+{
+    constexpr int TPR = D / 16, SLOTS = 256 / TPR, ES = DT == MOA_F32 ? 4 : 2, N = DT == MOA_F32 ? 2 : 1;
     launch_dependents();
     grid_dependency_wait();
     const int part = threadIdx.x % TPR;
-    const int heads = a.h_q + 2 * a.h_kv;
-    const int runs = (heads + a.heads_per_thread - 1) / a.heads_per_thread;
-    const long long item = (long long)blockIdx.x * SLOTS + threadIdx.x / TPR;
-    const int tok = (int)(item / runs);
-    const int head0 = (int)(item % runs) * a.heads_per_thread;
-    // Every thread stays to the end: the rows of a warp exchange their extremes together.
-    bool live = item < (long long)a.tokens * runs;
+    const unsigned mask = ((1u << TPR) - 1u) << (threadIdx.x & 31 & ~(TPR - 1));
+    const long long item = (long long)blockIdx.x * SLOTS + threadIdx.x / TPR;     // run by run, the tokens of a run in order
+    const int run = item <= 0xffffffffll ? (int)((unsigned)item / (unsigned)a.tokens) : (int)(item / a.tokens);
+    const int tok = (int)(item - (long long)run * a.tokens);
+    if (run >= a.q_runs + 2 * a.kv_runs) return;           // (the threads of a row leave together)
+    const int kind = run < a.q_runs ? 0 : run < a.q_runs + a.kv_runs ? 1 : 2;      // q, k, v
+    const int h0 = (run - (kind == 0 ? 0 : kind == 1 ? a.q_runs : a.q_runs + a.kv_runs)) * a.run;
+    const int h1 = min(h0 + a.run, kind == 0 ? a.h_q : a.h_kv);
+
+    // The token's sequence, position and row.
     int b = tok;
-    long long pos = 0;
-    if (live) {
-        if (a.token_start != nullptr) {
-            int lo = 0, hi = a.batch;                      // last b with token_start[b] <= tok
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (__ldg(a.token_start + mid) <= tok) lo = mid; else hi = mid;
-            }
-            b = lo;
-            const int first = __ldg(a.token_start + b), next = __ldg(a.token_start + b + 1);
-            live = first <= tok && tok < next;             // behind the last sequence: left as it is
-            pos = (long long)__ldg(a.seq_lens + b) - ((long long)next - tok);
-        } else {
-            live = tok < a.batch;
-            if (live) pos = (long long)__ldg(a.seq_lens + b) - 1;
+    long long pos;
+    if (a.token_start != nullptr) {
+        int lo = 0, hi = a.batch;                          // last b with token_start[b] <= tok
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (__ldg(a.token_start + mid) <= tok) lo = mid; else hi = mid;
         }
+        b = lo;
+        const int first = __ldg(a.token_start + b), next = __ldg(a.token_start + b + 1);
+        if (first > tok || tok >= next) return;            // behind the last sequence: left as it is
+        pos = (long long)__ldg(a.seq_lens + b) - ((long long)next - tok);
+    } else {
+        pos = (long long)__ldg(a.seq_lens + b) - 1;
     }
+    const int pi = pos < 0 ? 0 : a.page_shift >= 0 ? (int)pos >> a.page_shift : (int)pos / a.page_size;
+    int status = 0, off = 0;
     long long page = 0;
-    int off = 0;
-    if (live) {
-        int status = 0;
-        const int pi = pos < 0 ? 0 : a.page_shift >= 0 ? (int)pos >> a.page_shift : (int)pos / a.page_size;
-        if (pos < 0 || pi >= a.max_pages || (a.rot > 0 && pos >= a.rope_rows)) status = MOA_STATUS_APPEND_RANGE;
-        else {
-            page = __ldg(a.table + (long long)b * a.max_pages + pi);
-            off = (int)pos - pi * a.page_size;
-            if (page < 0 || page >= a.num_pages) status = MOA_STATUS_PAGE_RANGE;
-        }
-        if (status != 0) {
-            live = false;
-            if (part == 0 && head0 == 0) raise_status(status);
-        }
+    if (pos < 0 || pi >= a.max_pages || (TURN != kTurnNone && pos >= a.rope_rows)) status = MOA_STATUS_APPEND_RANGE;
+    else {
+        page = __ldg(a.table + (long long)b * a.max_pages + pi);
+        off = (int)pos - pi * a.page_size;
+        if (page < 0 || page >= a.num_pages) status = MOA_STATUS_PAGE_RANGE;
     }
+    if (status != 0) {
+        if (part == 0 && run == 0) raise_status(status);
+        return;
+    }
+
     // Places of this thread's two chunks, and its share of the token's cosines and sines.
     const int rot = a.rot, half = rot / 2;
-    const bool by_chunk = !a.pairs && rot % 16 == 0;       // partners are the thread's own chunks
     int d_lo = 16 * part, d_hi = 16 * part + 8;
-    if (by_chunk && 16 * part < rot) { d_lo = 8 * part; d_hi = half + 8 * part; }
-    const bool turns = live && 16 * part < rot;
+    const bool turns = TURN != kTurnNone && kind != 2 && 16 * part < rot;
+    if (TURN == kTurnChunks && turns) { d_lo = 8 * part; d_hi = half + 8 * part; }
     float cs[8], sn[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
     const float *row = a.cos_sin + pos * rot;
-    if (turns && (a.pairs || by_chunk)) {
+    if constexpr (TURN == kTurnChunks || TURN == kTurnPairs) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (8 * part + i < half) { cs[i] = __ldg(row + 8 * part + i); sn[i] = __ldg(row + half + 8 * part + i); }
+        for (int i = 0; i < 8; ++i) {
+            const bool in = turns && (TURN == kTurnChunks || 8 * part + i < half);
+            cs[i] = in ? __ldg(row + 8 * part + i) : 1.f;
+            sn[i] = in ? __ldg(row + half + 8 * part + i) : 0.f;
+        }
     }
-#pragma unroll 2
-    for (int hd = head0; hd < head0 + a.heads_per_thread; ++hd) {
-        const bool on = live && hd < heads;
-        const bool is_q = hd < a.h_q, is_v = hd >= a.h_q + a.h_kv;
-        const int h = is_q ? hd : is_v ? hd - a.h_q - a.h_kv : hd - a.h_q;
-        const unsigned char *src = is_q ? static_cast<const unsigned char *>(a.q) + (tok * a.q_st + (long long)h * D) * ES
-                                 : is_v ? static_cast<const unsigned char *>(a.v) + (tok * a.v_st + (long long)h * D) * ES
-                                        : static_cast<const unsigned char *>(a.k) + (tok * a.k_st + (long long)h * D) * ES;
-        float lo[8] = {}, hi[8] = {};
-        if (on) { load8<DT>(lo, src + d_lo * ES); load8<DT>(hi, src + d_hi * ES); }
-        if (on && turns && !is_v) {
-            if (a.pairs) {
+    const unsigned char *src = kind == 0 ? static_cast<const unsigned char *>(a.q) + tok * a.q_st * ES
+                             : kind == 1 ? static_cast<const unsigned char *>(a.k) + tok * a.k_st * ES
+                                         : static_cast<const unsigned char *>(a.v) + tok * a.v_st * ES;
+    unsigned char *dst = kind == 0 ? static_cast<unsigned char *>(a.q_out) + tok * a.o_st * ES
+                       : kind == 1 ? a.k_pool + page * a.k_sp + off * a.k_sr : a.v_pool + page * a.v_sp + off * a.v_sr;
+    const long long dst_step = kind == 0 ? D * ES : kind == 1 ? a.k_sh : a.v_sh;
+    src += (long long)h0 * D * ES;
+    dst += h0 * dst_step;
+    uint32_t *par = FMT == MOA_KV_INT4 && kind != 0 ? (kind == 1 ? a.kp : a.vp) + (page * a.h_kv + h0) * a.page_size + off : nullptr;
+
+    RowPart<DT> next;
+    fetch<DT>(next, src, d_lo, d_hi);
+#pragma unroll 1
+    for (int h = h0; h < h1; ++h, src += D * ES, dst += dst_step) {
+        const RowPart<DT> now = next;
+        if (h + 1 < h1) fetch<DT>(next, src + D * ES, d_lo, d_hi);
+        float lo[8], hi[8];
+        load8<DT>(lo, &now.u[0]);
+        load8<DT>(hi, &now.u[N]);
+        if constexpr (TURN == kTurnChunks) {
+            if (turns) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) turn(lo[i], hi[i], cs[i], sn[i]);
+            }
+        } else if constexpr (TURN == kTurnPairs) {
+            if (turns) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (d_lo + 2 * i < rot) turn(lo[2 * i], lo[2 * i + 1], cs[i], sn[i]);
                     if (d_hi + 2 * i < rot) turn(hi[2 * i], hi[2 * i + 1], cs[4 + i], sn[4 + i]);
                 }
-            } else if (by_chunk) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) turn(lo[i], hi[i], cs[i], sn[i]);
-            } else {                                       // partners in other threads' chunks: fetched one by one
+            }
+        } else if constexpr (TURN == kTurnAny) {
+            if (turns) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int d = 16 * part + i;
-                    if (d >= rot) continue;
-                    const int pair = d < half ? d : d - half;
-                    const float c = __ldg(row + pair), s = __ldg(row + half + pair);
-                    float x = load_as_float(src, pair, DT), y = load_as_float(src, pair + half, DT);
-                    turn(x, y, c, s);
-                    const float mine = d < half ? x : y;
-                    if (i < 8) lo[i] = mine; else hi[i - 8] = mine;
+                    const int d = 16 * part + i, pair = d < half ? d : d - half;
+                    if (d < rot) {
+                        float x = load_as_float(src, pair, DT), y = load_as_float(src, pair + half, DT);
+                        turn(x, y, __ldg(row + pair), __ldg(row + half + pair));
+                        (i < 8 ? lo[i] : hi[i - 8]) = d < half ? x : y;
+                    }
                 }
             }
+            __syncwarp(mask);                              // q_out may be q: its row is read by now
         }
-        __syncwarp();                                      // q_out may be q: its row is read by now
-        if (is_q) {
-            if (on) {
-                unsigned char *dst = static_cast<unsigned char *>(a.q_out) + (tok * a.o_st + (long long)h * D) * ES;
-                store8<DT>(dst + d_lo * ES, lo);
-                store8<DT>(dst + d_hi * ES, hi);
-            }
-        }
-        if constexpr (FMT != MOA_KV_INT4) {
-            if (on && !is_q) {
-                unsigned char *dst = is_v ? a.v_pool + page * a.v_sp + h * a.v_sh + off * a.v_sr
-                                          : a.k_pool + page * a.k_sp + h * a.k_sh + off * a.k_sr;
-                store8<DT>(dst + d_lo * ES, lo);
-                store8<DT>(dst + d_hi * ES, hi);
-            }
-        } else if (__any_sync(0xffffffffu, on && !is_q)) {
+        if (FMT != MOA_KV_INT4 || kind == 0) {
+            store8<DT>(dst + d_lo * ES, lo);
+            store8<DT>(dst + d_hi * ES, hi);
+        } else {
             uint32_t c_lo, c_hi, params;
-            pack_row<D>(lo, hi, c_lo, c_hi, params);       // (a collective of the warp)
-            if (on && !is_q) {
-                unsigned char *dst = is_v ? a.v_pool + page * a.v_sp + h * a.v_sh + off * a.v_sr
-                                          : a.k_pool + page * a.k_sp + h * a.k_sh + off * a.k_sr;
-                *reinterpret_cast<uint32_t *>(dst + d_lo / 2) = c_lo;
-                *reinterpret_cast<uint32_t *>(dst + d_hi / 2) = c_hi;
-                if (part == 0) (is_v ? a.vp : a.kp)[(page * a.h_kv + h) * a.page_size + off] = params;
-            }
+            pack_row<D>(lo, hi, c_lo, c_hi, params, mask);
+            *reinterpret_cast<uint32_t *>(dst + d_lo / 2) = c_lo;
+            *reinterpret_cast<uint32_t *>(dst + d_hi / 2) = c_hi;
+            if (part == 0) *par = params;
+            par += a.page_size;
         }
     }
 }
@@ -252,7 +266,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const PagedIoArgs a)
 // Rows [row_start, seq_len) of every sequence into [batch, h_kv, n_out, D]; a thread takes eight
 // features of one row of K and of V.
 template <int FMT, int D>
-__global__ void __launch_bounds__(256) paged_gather_kernel(const PagedIoArgs a, int out_dtype)
+__global__ void __launch_bounds__(256) paged_gather_kernel(const __grid_constant__ PagedIoArgs a, int out_dtype)
 {
     constexpr int TPR = D / 8, SLOTS = 256 / TPR;
     launch_dependents();
