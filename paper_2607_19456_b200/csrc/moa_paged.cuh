@@ -23,7 +23,8 @@
 //    so that their rounding (2^-9 for bf16) does not add to the one rounding of the output.
 //  - fp32: both operands split into two tf32 terms, three products (hi*hi, hi*lo, lo*hi), short chains.
 //  - 4 bits: a code c in 0..15 is used as the fp16 bit pattern c, the subnormal c * 2^-24: unpacking
-//    is one AND for two codes (another for the codes four bits up, which come out 16 times as large).
+//    is one AND for two codes (another for the codes four bits up, which come out 16 times as large);
+//    V's bytes are used whole, c0 + 16 c1, beside c0 alone, which takes four instructions for eight codes.
 //    The score of a row is scale * (s * <q, c> + m * sum(q)) with the row's (s, m); in the weighted
 //    sum the weight of a row is p * s, and sum(p * m) is kept beside it.  q is brought to fp16 by a
 //    power of two per head (exact but for terms 2^-38 of the largest); the weights are brought into
@@ -217,9 +218,8 @@ template <class C>
 __device__ __forceinline__ void chunk_place(int r, int c, uint32_t &kd, uint32_t &vd)
 {
     if constexpr (C::FMT == MOA_KV_INT4) {
-        const int slot = (r & 8) | ((r & 3) << 1) | ((r >> 2) & 1);
-        kd = slot * C::ROWB + c * 16;
-        vd = r * C::ROWB + ((c * 16) ^ (C::D == 128 ? ((r >> 1) & 1) << 5 : 0));
+        kd = r * C::ROWB + c * 16;
+        vd = r * C::ROWB + ((c ^ (C::D == 128 ? (r >> 1) & 3 : (r >> 2) & 1)) << 4);
     } else if constexpr (C::FMT == MOA_KV_F32) {
         kd = r * C::ROWB + ((c ^ ((r & 1) << 2)) << 4);
         vd = r * C::ROWB + ((c ^ ((r & 3) << 1)) << 4);
@@ -403,7 +403,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             unit_lo = j0 - cc.i;
         }
         TileCursor lc = cc;
-        long long jl = j0;
+        const int n = (int)(j1 - j0);                      // (2^31 stages of one warp would be 8e13 rows)
+        int loaded = 0;
         int load_stage = 0;
         unsigned bad_stages = 0;
         // Of the unit under `lc`: its K/V head's part of the pools, its row of the table.
@@ -431,6 +432,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         };
         load_unit();
         fetch_pages();
+        uint32_t kd0, vd0;
+        chunk_place<C>(lane / C::CPR, lane % C::CPR, kd0, vd0);
         const long long k_step = (32 / C::CPR) * a.k_sr, v_step = (32 / C::CPR) * a.v_sr;
 
         auto issue = [&]() {                               // copies of the stage under `lc`, then on to the next
@@ -445,10 +448,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     const unsigned char *vr = vh + page[tt] * a.v_sp + off0 * a.v_sr;
 #pragma unroll
                     for (int i = 0; i < C::NCH; ++i) {
-                        uint32_t kd, vd;
-                        chunk_place<C>(lane / C::CPR + i * (32 / C::CPR), lane % C::CPR, kd, vd);
-                        cp16(dst + kd, kr);
-                        cp16(dst + C::KB + vd, vr);
+                        // the place of row r + i * (32 / CPR), from the place of row r: the swizzle's bits and the row's are apart
+                        constexpr int RS = 32 / C::CPR;
+                        const uint32_t kx = Q4 ? 0 : F32 ? ((i * RS) & 1) << 6 : ((i * RS) & 7) << 4;
+                        const uint32_t vx = Q4 ? 0 : F32 ? ((i * RS) & 3) << 5 : ((i * RS) & 7) << 4;
+                        cp16(dst + (kd0 ^ kx) + i * RS * C::ROWB, kr);
+                        cp16(dst + C::KB + (vd0 ^ vx) + i * RS * C::ROWB, vr);
                         kr += k_step; vr += v_step;
                     }
                     if (Q4) cp4(dst + 2 * C::KB + lane * 4, ph + ((long long)page[tt] * a.h_stored * a.page_size + off0));
@@ -459,15 +464,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             if (bad) bad_stages |= 1u << load_stage;
             else bad_stages &= ~(1u << load_stage);
             if (++load_stage == S) load_stage = 0;
-            ++jl;
-            if (jl < j1) {
+            if (++loaded < n) {
                 if (tile_advance<R>(a, hv, lc)) load_unit();
                 fetch_pages();
             }
         };
 #pragma unroll 1
         for (int i = 0; i < S; ++i) {
-            if (jl < j1) issue();
+            if (loaded < n) issue();
             cp_commit();
         }
 
@@ -556,7 +560,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         auto process = [&](uint32_t st, int nr, bool bad) {
             float x[TT][NT][4];
             float2 vpar[TT][2];                            // 4 bits: V's (scale, least) of this lane's two rows
-            const int tok = Q4 ? ((g & 1) << 2) | (g >> 1) : g;    // the row that score row g stands for (score row g + 8: 8 more)
 #pragma unroll
             for (int tt = 0; tt < TT; ++tt) {
                 const uint32_t sk = st + tt * C::TILE;
@@ -619,9 +622,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                         *reinterpret_cast<uint2 *>(w1) = *reinterpret_cast<const uint2 *>(p + 8 * C::ROWB);
                     }
                     const __half2 *par = reinterpret_cast<const __half2 *>(skp + 2 * C::KB);
-                    const float2 k0 = __half22float2(par[tok]), k1 = __half22float2(par[tok + 8]);
-                    vpar[tt][0] = __half22float2(par[16 + tok]);
-                    vpar[tt][1] = __half22float2(par[16 + tok + 8]);
+                    const float2 k0 = __half22float2(par[g]), k1 = __half22float2(par[g + 8]);
+                    vpar[tt][0] = __half22float2(par[16 + g]);
+                    vpar[tt][1] = __half22float2(par[24 + g]);
                     float c[NT][4] = {};
 #pragma unroll
                     for (int w = 0; w < NW; ++w)
@@ -648,8 +651,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            if (16 * tt + tok >= nr) x[tt][n][e] = -INFINITY;
-                            if (16 * tt + tok + 8 >= nr) x[tt][n][2 + e] = -INFINITY;
+                            if (16 * tt + g >= nr) x[tt][n][e] = -INFINITY;
+                            if (16 * tt + g + 8 >= nr) x[tt][n][2 + e] = -INFINITY;
                         }
             }
             // The reference maximum moves only when a score exceeds it by more than 8 (a factor of
@@ -794,37 +797,36 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
                         for (int e = 0; e < 2; ++e) s.om[n][e] = fmaf(p[n][e], vpar[tt][0].y, fmaf(p[n][2 + e], vpar[tt][1].y, s.om[n][e]));
                     }
-                    constexpr int NW = D / 64;
-                    uint32_t w[4][NW];                     // rows t, 4 + t, 8 + t, 12 + t: what the weights' columns stand for
+                    // A transposed load hands a lane the 16-bit units (four codes) of two neighbouring rows in
+                    // one register.  Low features of a byte: code & 15; both together, c0 + 16 c1, stand in the
+                    // rows of the high ones, whose sums are taken apart at the end of the unit.
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const int r = t + 4 * h;
-                        const unsigned char *src = svp + r * C::ROWB + ((g * (D / 16)) ^ (D == 128 ? ((r >> 1) & 1) << 5 : 0));
-                        if constexpr (NW == 2) *reinterpret_cast<uint2 *>(w[h]) = *reinterpret_cast<const uint2 *>(src);
-                        else w[h][0] = *reinterpret_cast<const uint32_t *>(src);
-                    }
+                    for (int j = 0; j < D / 64; ++j) {
+                        uint32_t r[4];                     // columns 16j.. of 16-bit units: rows 0-7, 8-15; columns 16j + 8..: the same
+                        const int row = (lane & 7) + (((lane >> 3) & 1) << 3), ch = 2 * j + (lane >> 4);
+                        ldsm4t(r, sv + row * C::ROWB + ((ch ^ (D == 128 ? (row >> 1) & 3 : (row >> 2) & 1)) << 4));
 #pragma unroll
-                    for (int i = 0; i < NW; ++i)
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {      // output tile 4i + e: features 2e and 2e + 1 of the word
-                            uint32_t u0 = __byte_perm(w[0][i], w[1][i], e < 2 ? 0x5410 : 0x7632);
-                            uint32_t u1 = __byte_perm(w[2][i], w[3][i], e < 2 ? 0x5410 : 0x7632);
-                            if (e & 1) { u0 >>= 8; u1 >>= 8; }
-                            const uint32_t a0 = u0 & 0x000f000fu, a1 = u0 & 0x00f000f0u, a2 = u1 & 0x000f000fu, a3 = u1 & 0x00f000f0u;
+                            for (int e = 0; e < 2; ++e) {  // output tile 4j + 2i + e: features 4(8(2j + i) + g) + 2e, + 1
+                                const uint32_t a1 = e ? __byte_perm(r[2 * i], 0u, 0x4341) : r[2 * i] & 0x00ff00ffu;
+                                const uint32_t a3 = e ? __byte_perm(r[2 * i + 1], 0u, 0x4341) : r[2 * i + 1] & 0x00ff00ffu;
+                                const uint32_t a0 = a1 & 0x000f000fu, a2 = a3 & 0x000f000fu;
+                                const int to = 4 * j + 2 * i + e;
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][4 * i + e], a0, a1, a2, a3, wt[n][0], wt[n][1]);
-                            if (fine) {
+                                for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][to], a0, a1, a2, a3, wt[n][0], wt[n][1]);
+                                if (fine) {
 #pragma unroll
-                                for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][4 * i + e], a0, a1, a2, a3, wl[n][0], wl[n][1]);
+                                    for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][to], a0, a1, a2, a3, wl[n][0], wl[n][1]);
+                                }
                             }
-                        }
+                    }
                 }
             }
         };
 
         // ---- end of a unit, or of this warp's part of it ------------------------------------
-        // Feature of accumulator (i, half h): 16-bit: 16i + 8h + g; fp32: 4(g + 8(i/2)) + 2(i%2) + h;
-        // 4 bits: g * D/8 + 8(i/4) + 2(i%4) + h.  dst: a partial slot, or null for the output row.
+        // Feature of accumulator (i, half h): 16-bit: 16i + 8h + g; fp32 and 4 bits: 4(g + 8(i/2)) + 2(i%2) + h.  dst: a partial slot, or null for the output row.
         auto close = [&](float *dst) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -837,8 +839,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                         if (Q4) om += __shfl_xor_sync(0xffffffffu, om, off);
                     }
                     const int head = 8 * n + 2 * t + e;
-                    float f0 = 1.f, f1 = 1.f, add = 0.f;   // of the features that come from the low and the high codes
-                    if (Q4) { f0 = s.ref * 131072.0f; f1 = s.ref * 8192.0f; add = om; }
+                    float f0 = 1.f, f1 = 1.f, add = 0.f;   // of even and of odd features
+                    if (Q4) { f0 = s.ref * 131072.0f; f1 = s.ref * 8192.0f; add = om; }      // 2^24 / 128, and a 16th
                     long long at = -1;
                     if (dst != nullptr) {
                         if (g == 0) { dst[head * PS + D] = s.m[n][e]; dst[head * PS + D + 1] = l; }
@@ -848,12 +850,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                         const float inv = 1.0f / l;
                         f0 *= inv; f1 *= inv; add *= inv;
                     }
-                    auto val = [&](int i, int h) { return fmaf(s.acc[n][i][2 * h + e], h ? f1 : f0, add); };
+                    auto val = [&](int i, int h) {
+                        return fmaf(Q4 && h ? s.acc[n][i][2 + e] - s.acc[n][i][e] : s.acc[n][i][2 * h + e], h ? f1 : f0, add);
+                    };
                     if (Q4 || F32) {
 #pragma unroll
                         for (int i = 0; i < MT; i += 2) {
                             const float4 v4 = make_float4(val(i, 0), val(i, 1), val(i + 1, 0), val(i + 1, 1));
-                            const int d = Q4 ? g * (D / 8) + 2 * i : 4 * (g + 4 * i);
+                            const int d = 4 * (g + 4 * i);
                             if (dst != nullptr) *reinterpret_cast<float4 *>(dst + head * PS + d) = v4;
                             else if (at >= 0) store4(a.out, at + d, v4, dtype);
                         }
@@ -873,21 +877,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         int stage = 0;
         bool fresh = true;
 #pragma unroll 1
-        for (long long j = j0; j < j1; ++j) {
+        for (int j = 0; j < n; ++j) {
             if (fresh) { begin_unit(); fresh = false; }
             cp_wait<S - 1>();
             __syncwarp();
             process(ring_u + stage * C::STAGE, cc.len - cc.i * R, (bad_stages >> stage) & 1u);
             __syncwarp();                                  // every lane is done with the stage
             if (++stage == S) stage = 0;
-            if (jl < j1) issue();
+            if (loaded < n) issue();
             cp_commit();
             const bool unit_ends = cc.i + 1 == cc.ub;
-            if (unit_ends || j + 1 == j1) {
+            if (unit_ends || j + 1 == n) {
                 const bool whole = unit_ends && unit_lo >= j0;
                 if (whole) close(nullptr);
                 else {
-                    const int which = j + 1 == j1 ? 1 : 0; // a cut unit that ends before the range does is its first
+                    const int which = j + 1 == n ? 1 : 0; // a cut unit that ends before the range does is its first
                     if (which) { cp_wait<0>(); __syncwarp(); }
                     close(which ? reinterpret_cast<float *>(ring) : first_slots + (size_t)warp * C::SLOT);
                     if (lane == 0) {
@@ -898,7 +902,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                 }
                 if (unit_ends) { unit_lo += cc.ub; fresh = true; }
             }
-            if (j + 1 < j1) tile_advance<R>(a, hv, cc);
+            if (j + 1 < n) tile_advance<R>(a, hv, cc);
         }
     }
     __syncthreads();
