@@ -918,6 +918,7 @@ static int paged_grid(const DeviceState &s)
     return g_num_ctas > 0 ? (g_num_ctas < kTicketCtas ? g_num_ctas : kTicketCtas) : (s.sm_count < kTicketCtas ? s.sm_count : kTicketCtas);
 }
 
+static size_t paged_ticket_bytes(int grid, int heads) { return (size_t)grid * heads * sizeof(unsigned long long); }
 static size_t paged_slot_bytes(int grid, int heads, int d)
 {
     return ((size_t)grid * 2 * heads * (d + 4) * sizeof(float) + 255) / 256 * 256;
@@ -956,7 +957,11 @@ static cudaError_t launch_paged(int format, int heads, const PagedArgs &a, int g
         if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 1, 8, wide ? 2 : 4, 1>>(a, grid, st);
         return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 2, 8, wide ? 2 : 4, 1>>(a, grid, st);
     default:
-        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 16, wide ? 2 : 3, 2>>(a, grid, st);
+        if (a.dtype == MOA_F16) {
+            if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 12, 2, 2, true>>(a, grid, st);
+            return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 8, wide ? 3 : 4, 2, true>>(a, grid, st);
+        }
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 12, 2, 2>>(a, grid, st);
         return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 8, wide ? 3 : 4, 2>>(a, grid, st);
     }
 }
@@ -986,14 +991,21 @@ static int paged_decode_impl(const moa_paged_cache *c, const void *q, void *out,
     if (rc != MOA_OK) return rc;
     const int g = h_q / c->h_kv, heads = paged_heads(c->format, g), grid = paged_grid(*dev);
     const size_t slots = paged_slot_bytes(grid, heads, c->d);
-    if (ws_bytes < slots + kTicketBytes) return MOA_ERR_WORKSPACE;
+    if (ws_bytes < slots + paged_ticket_bytes(grid, heads)) return MOA_ERR_WORKSPACE;
 
     a.k = static_cast<const unsigned char *>(c->k); a.v = static_cast<const unsigned char *>(c->v);
     a.kp = static_cast<const uint32_t *>(c->k_params); a.vp = static_cast<const uint32_t *>(c->v_params);
     a.k_sp = ks[0]; a.k_sh = ks[1]; a.k_sr = ks[2];
     a.v_sp = vs[0]; a.v_sh = vs[1]; a.v_sr = vs[2];
     a.num_pages = c->num_pages; a.page_size = c->page_size;
-    a.page_shift = page_shift_of(c->page_size); a.one_page = c->page_size % 16 == 0;
+    a.page_shift = page_shift_of(c->page_size);
+    const long long pairs = (long long)c->h_kv * c->page_size, top = 0xffffffffLL;
+    a.one_page = a.page_shift >= 4 && ks[0] <= top && ks[2] <= top && vs[0] <= top && vs[2] <= top && pairs <= top;
+    if (a.one_page) {
+        a.k_sp32 = (uint32_t)ks[0]; a.k_sr32 = (uint32_t)ks[2];
+        a.v_sp32 = (uint32_t)vs[0]; a.v_sr32 = (uint32_t)vs[2];
+        a.p_sp32 = (uint32_t)pairs;
+    }
     a.table = page_table; a.max_pages = max_pages; a.seq_lens = seq_lens;
     const long long cap = (long long)max_pages * c->page_size;
     a.len_max = cap < 0x7fffffffLL - 16 ? (int)cap : 0x7fffffff - 16;
@@ -1450,7 +1462,8 @@ size_t moa_paged_workspace_bytes(int batch, int h_q, int h_kv, int d)
     DeviceState plain;
     plain.sm_count = 256;                  // no device: an upper bound
     const int grid = paged_grid(current_device(&dev) == MOA_OK ? *dev : plain);
-    return paged_slot_bytes(grid, paged_heads(MOA_KV_BF16, h_q / h_kv), d) + (kTicketBytes + 255) / 256 * 256;
+    const int heads = paged_heads(MOA_KV_BF16, h_q / h_kv);
+    return paged_slot_bytes(grid, heads, d) + (paged_ticket_bytes(grid, heads) + 255) / 256 * 256;
 }
 
 int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int dtype, int batch, int n_out,

@@ -46,7 +46,10 @@ struct PagedArgs {
     long long v_sp, v_sh, v_sr;
     int num_pages, page_size;
     int page_shift;                  // log2(page_size), or -1
-    int one_page;                    // page_size % 16 == 0: a tile lies in one page
+    // A tile of 16 rows lies in one page (page_size a power of two, 16 at least), and these byte strides
+    // (page and row; pairs of a page) fit 32 bits: the copies' addresses are two multiply-adds each.
+    int one_page;
+    uint32_t k_sp32, k_sr32, v_sp32, v_sr32, p_sp32;
     const int32_t *table;            // [batch, max_pages]
     int max_pages;
     const int32_t *seq_lens;         // [batch]
@@ -61,14 +64,17 @@ struct PagedArgs {
     int g_total;                     // query heads per stored kv head
     float qscale;                    // scale * log2(e)
     float *ws;                       // two partial slots per CTA
-    unsigned long long *tickets;
+    unsigned long long *tickets;     // G for every CTA: counters of the pieces of the unit that is cut at its end
     unsigned long long ticket_tag;
 };
 
 // W warps, S ring stages of TT tiles of 16 rows (K and V) each.  The ring and the slots of the first cut unit
 // share the 227 KB of an SM; the slot of the last cut unit is the ring itself, empty by then.
-template <int FMT_, int D_, int NT_, int W_, int S_, int TT_>
+// FINE: the weights of 4-bit rows in two fp16 terms, for fp16 outputs (one term: 6.0e-4 off the definition
+// where the rounding of the output alone is 2.0e-4; bf16 outputs, 1.7e-3, gain nothing from it).
+template <int FMT_, int D_, int NT_, int W_, int S_, int TT_, bool FINE_ = false>
 struct PagedCfg {
+    static constexpr bool FINE = FINE_;
     static constexpr int FMT = FMT_, D = D_, NT = NT_, W = W_, S = S_, TT = TT_;
     static constexpr int THREADS = W * 32, R = 16 * TT;    // rows of a stage
     static constexpr int ROWB = FMT == MOA_KV_F32 ? 4 * D : FMT == MOA_KV_INT4 ? D / 2 : 2 * D;   // bytes of a row
@@ -87,11 +93,11 @@ struct PagedCfg {
     static constexpr int QREGS = FMT == MOA_KV_F32 ? 4 : 2;    // B registers per k-step (fp32: two terms)
     static constexpr size_t OFF_FIRST = (size_t)W * S * STAGE;
     static constexpr size_t OFF_PREF = OFF_FIRST + sizeof(float) * (size_t)W * SLOT;
-    static constexpr size_t SMEM_BYTES = OFF_PREF + sizeof(long long) * (THREADS + 1);
+    static constexpr size_t SMEM_BYTES = OFF_PREF + sizeof(long long) * THREADS;
     static_assert(W <= 16, "two segments per warp have to fit a warp's lanes");
     static_assert((size_t)S * STAGE >= sizeof(float) * SLOT, "the ring holds the last partial");
     static_assert(OFF_FIRST % 16 == 0 && OFF_PREF % 16 == 0, "alignment of the regions");
-    static_assert(SMEM_BYTES <= 227 * 1024 - 3328, "shared memory of an SM, less the static part");
+    static_assert(SMEM_BYTES <= 227 * 1024 - 1280, "shared memory of an SM, less the static part");
 };
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool full)
@@ -294,178 +300,220 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
     __shared__ long long s_warp[16];
     __shared__ bool s_large[16];
     __shared__ long long s_seg[32];                        // unit of segment 2 * warp + (0: first, 1: last), or -1
-    __shared__ long long s_seg_lo[32];                     // flat index of that unit's first tile
-    __shared__ int s_seg_ub[32], s_seg_vh[32];             // its tiles, its virtual kv head (with the sequence in s_seg_b)
-    __shared__ int s_seg_b[32];
-    __shared__ float s_top[32][G];                         // reference maximum of the group that a segment leads
-    __shared__ int s_done[2];
+    __shared__ long long s_seg_lo[32];                     // flat index of that unit's first stage
+    __shared__ int s_seg_ub[32], s_seg_vh[32], s_seg_b[32];    // its stages, virtual kv head, sequence
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int hv = a.h_stored * a.share;
     const int dtype = F32 ? MOA_F32 : FMT == MOA_KV_BF16 ? MOA_BF16 : FMT == MOA_KV_F16 ? MOA_F16 : a.dtype;
 
     launch_dependents();
+    if (lane < 2) s_seg[2 * warp + lane] = -1;             // (read behind the barrier at the end)
+    if (warp == 0 && lane >= 2 * W) s_seg[lane] = -1;
     grid_dependency_wait();
 
-    // ---- lengths: tiles per sequence, prefix over the threads' runs of sequences -----------
-    const int per_thread = (a.batch + C::THREADS - 1) / C::THREADS;
+    // ---- lengths: stages per sequence and their prefix ---------------------------------------
+    // Up to 128 sequences every warp does this for itself, four to a lane; more go through shared
+    // memory, a run of sequences to a thread.
+    const bool few = a.batch <= 128;
+    const int per_thread = few ? 4 : (a.batch + C::THREADS - 1) / C::THREADS;
+    int ln[4];                                             // few: lengths of sequences 4 * lane..., 0 where out of range
     long long mine = 0;
-    bool empty = false, large = false;
-    for (int i = 0; i < per_thread; ++i) {
-        const int b = tid * per_thread + i;
-        if (b >= a.batch) break;
-        const int len = a.seq_lens[b];
-        const bool here = (unsigned)b % gridDim.x == blockIdx.x;
-        if (len < 0 || len > a.len_max) { if (here) raise_status(MOA_STATUS_SEQLEN_RANGE); }
-        else {
-            mine += (len + R - 1) / R;
-            empty |= (len == 0 && here);
-            large |= len > C::WHOLE * R;
+    bool large = false;
+    auto zero_out = [&](int b) {                           // a sequence without rows
+        const long long row_bytes = (long long)a.h_q * D * (dtype == MOA_F32 ? 4 : 2);
+        for (long long i = tid; i < row_bytes / 16; i += C::THREADS)
+            reinterpret_cast<uint4 *>(static_cast<unsigned char *>(a.out) + (long long)b * row_bytes)[i] = make_uint4(0u, 0u, 0u, 0u);
+    };
+    if (few) {
+        unsigned zero = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ln[i] = 4 * lane + i < a.batch ? a.seq_lens[4 * lane + i] : -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = 4 * lane + i;
+            const bool here = b < a.batch && (unsigned)b % gridDim.x == blockIdx.x;
+            if (here && ln[i] == 0) zero |= 1u << i;
+            if (ln[i] < 0 || ln[i] > a.len_max) {
+                if (here && warp == 0) raise_status(MOA_STATUS_SEQLEN_RANGE);
+                ln[i] = 0;
+            }
+            mine += (ln[i] + R - 1) / R;
+            large |= ln[i] > C::WHOLE * R;
+        }
+        if (__any_sync(0xffffffffu, zero != 0)) {
+#pragma unroll 1
+            for (int b = 0; b < a.batch; ++b)
+                if (__shfl_sync(0xffffffffu, zero, b >> 2) >> (b & 3) & 1u) zero_out(b);
+        }
+    } else {
+        bool empty = false;
+#pragma unroll 1
+        for (int i = 0; i < per_thread; ++i) {
+            const int b = tid * per_thread + i;
+            if (b >= a.batch) break;
+            const int len = a.seq_lens[b];
+            const bool here = (unsigned)b % gridDim.x == blockIdx.x;
+            if (len < 0 || len > a.len_max) { if (here) raise_status(MOA_STATUS_SEQLEN_RANGE); }
+            else { mine += (len + R - 1) / R; empty |= len == 0 && here; large |= len > C::WHOLE * R; }
+        }
+        if (__syncthreads_or(empty)) {
+            for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
+                if (a.seq_lens[b] == 0) zero_out(b);
         }
     }
-    long long inc = mine;
+    large = __any_sync(0xffffffffu, large);
+    long long pre = mine;                                  // stages per head of the sequences before this lane's (this thread's)
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const long long x = __shfl_up_sync(0xffffffffu, inc, off);
-        if (lane >= off) inc += x;
+        const long long x = __shfl_up_sync(0xffffffffu, pre, off);
+        if (lane >= off) pre += x;
     }
-    large = __any_sync(0xffffffffu, large);
-    if (lane == 31) { s_warp[warp] = inc; s_large[warp] = large; }
-    if (tid < 32) s_seg[tid] = -1;
-    const int any_empty = __syncthreads_or(empty);
-    long long before = 0, total1 = 0;
+    long long total = __shfl_sync(0xffffffffu, pre, 31);
+    pre -= mine;
+    if (!few) {
+        if (lane == 0) { s_warp[warp] = total; s_large[warp] = large; }
+        __syncthreads();
+        total = 0;
+#pragma unroll 1
+        for (int w = 0; w < W; ++w) {
+            if (w < warp) pre += s_warp[w];
+            total += s_warp[w];
+            large |= s_large[w];
+        }
+        s_pref[tid] = pre;
+        __syncthreads();
+    }
+    total *= hv;
+
+    // ---- this CTA's range [c0, c1) of the flat list, this warp's [j0, j1), and the unit it begins in --
+    // Few and small units: one for each CTA, none is cut, the list is the unit's own.  Else a CTA takes at
+    // least W stages: a cut costs a partial, a counter round trip and a merge, about 3 us.
+    const bool whole = few && !large && (long long)a.batch * hv <= gridDim.x;
+    const int active = total < (long long)W * gridDim.x ? (int)((unsigned)(total + W - 1) / W) : (int)gridDim.x;
+    TileCursor cc;
+    cc.b = cc.h = cc.i = cc.len = 0;
+    cc.ub = 1;
+    long long c0, c1, j0, j1, unit_lo = 0;                 // unit_lo: flat index of the current unit's first stage
+    if (whole) {
+        cc.b = blockIdx.x / hv; cc.h = blockIdx.x % hv;
+        if (cc.b >= a.batch) return;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        if (w < warp) before += s_warp[w];
-        total1 += s_warp[w];
-        large |= s_large[w];
-    }
-    s_pref[tid] = before + inc - mine;
-    if (tid == 0) s_pref[C::THREADS] = total1;
-    if (any_empty) {                                       // a sequence without rows: zeros
-        const long long row_bytes = (long long)a.h_q * D * (dtype == MOA_F32 ? 4 : 2);
-        for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
-            if (a.seq_lens[b] == 0)
-                for (long long i = tid; i < row_bytes / 16; i += C::THREADS)
-                    reinterpret_cast<uint4 *>(static_cast<unsigned char *>(a.out) + (long long)b * row_bytes)[i] =
-                        make_uint4(0u, 0u, 0u, 0u);
-    }
-    __syncthreads();
-    const long long total = total1 * hv;
-    // A CTA takes at least W stages: a cut costs a partial, a counter round trip and a merge, about 3 us.
-    int active = total < (long long)W * gridDim.x ? (int)((unsigned)(total + W - 1) / W) : (int)gridDim.x;
-    long long c0, c1;
-    if (!large && per_thread == 1 && (long long)a.batch * hv <= gridDim.x) {      // small and few: a unit for each CTA, nothing is cut
-        const int b = blockIdx.x / hv, h = blockIdx.x % hv;
-        if (b >= a.batch) return;
-        const long long ub = s_pref[b + 1] - s_pref[b];
-        c0 = s_pref[b] * hv + h * ub;
-        c1 = c0 + ub;
-        if (ub == 0) return;
+        for (int i = 0; i < 4; ++i) {
+            const int x = __shfl_sync(0xffffffffu, ln[i], cc.b >> 2);
+            if ((cc.b & 3) == i) cc.len = x;
+        }
+        if (cc.len == 0) return;
+        cc.ub = (cc.len + R - 1) / R;
+        c0 = 0; c1 = cc.ub;
+        j0 = split_at(c1, warp, W); j1 = split_at(c1, warp + 1, W);
+        cc.i = (int)j0;
     } else {
         if (blockIdx.x >= active) return;                  // (also when there is nothing to do)
-        c0 = split_at(total, blockIdx.x, active);
-        c1 = split_at(total, blockIdx.x + 1, active);
+        c0 = split_at(total, blockIdx.x, active); c1 = split_at(total, blockIdx.x + 1, active);
+        j0 = c0 + split_at(c1 - c0, warp, W); j1 = c0 + split_at(c1 - c0, warp + 1, W);
+        if (j0 < j1) {
+            long long at;
+            int b, len = 0, ub = 0;
+            if (few) {
+                const int from = 31 - __clz(__ballot_sync(0xffffffffu, mine > 0 && pre * hv <= j0));
+                at = __shfl_sync(0xffffffffu, pre, from) * hv;
+                b = 4 * from - 1;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int x = __shfl_sync(0xffffffffu, ln[i], from);
+                    if (j0 < at + (long long)ub * hv) continue;        // found
+                    at += (long long)ub * hv;
+                    ++b; len = x; ub = (x + R - 1) / R;
+                }
+            } else {
+                int lo = 0, hi = C::THREADS;
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (s_pref[mid] * hv <= j0) lo = mid; else hi = mid;
+                }
+                at = s_pref[lo] * hv;
+#pragma unroll 1
+                for (b = lo * per_thread; b < a.batch; ++b) {          // ends before: j0 < total
+                    len = paged_len(a, b);
+                    ub = (len + R - 1) / R;
+                    if (j0 < at + (long long)ub * hv) break;
+                    at += (long long)ub * hv;
+                }
+            }
+            if (b < a.batch && ub > 0) {                   // (else the lengths have changed meanwhile: no rows, no output)
+                const long long in = j0 - at;
+                cc.b = b; cc.len = len; cc.ub = ub;
+                cc.h = in <= 0x7fffffff ? (int)((unsigned)in / (unsigned)ub) : (int)(in / ub);
+                cc.i = (int)(in - (long long)cc.h * ub);
+            } else cc.b = a.batch;
+            unit_lo = j0 - cc.i;
+        }
     }
-    const long long j0 = c0 + split_at(c1 - c0, warp, W), j1 = c0 + split_at(c1 - c0, warp + 1, W);
 
     unsigned char *ring = smem + (size_t)warp * S * C::STAGE;
     const uint32_t smem_u = smem_u32(smem), ring_u = smem_u + warp * S * C::STAGE;
-    // fp16 output: the weights of 4-bit rows in two fp16 terms (one term: 6.0e-4 off the definition where
-    // the rounding of the output alone is 2.0e-4; bf16 outputs, 1.7e-3, gain nothing from it).
-    const bool fine = Q4 && dtype == MOA_F16;
 
     if (j0 < j1) {
-        // ---- the tile that the range begins with ------------------------------------------
-        TileCursor cc;
-        long long unit_lo;                                 // flat index of the current unit's first tile
-        {
-            int lo = 0, hi = C::THREADS;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (s_pref[mid] * hv <= j0) lo = mid; else hi = mid;
-            }
-            long long at = s_pref[lo] * hv;
-            int b = lo * per_thread, ub = 0, len = 0;
-            for (; b < a.batch; ++b) {                     // ends before: j0 < total
-                len = paged_len(a, b);
-                ub = (len + R - 1) / R;
-                if (j0 < at + (long long)ub * hv) break;
-                at += (long long)ub * hv;
-            }
-            cc.b = b; cc.len = len; cc.ub = ub; cc.h = cc.i = 0;
-            if (b < a.batch) {
-                const long long in = j0 - at;
-                cc.h = in <= 0x7fffffff ? (int)((unsigned)in / (unsigned)ub) : (int)(in / ub);
-                cc.i = (int)(in - (long long)cc.h * ub);
-            }
-            else cc.len = 0, cc.ub = 1;                    // (lengths that changed meanwhile: no rows, no output)
-            unit_lo = j0 - cc.i;
-        }
         TileCursor lc = cc;
         const int n = (int)(j1 - j0);                      // (2^31 stages of one warp would be 8e13 rows)
         int loaded = 0;
-        int load_stage = 0;
-        unsigned bad_stages = 0;
-        // Of the unit under `lc`: its K/V head's part of the pools, its row of the table.
+        uint32_t load_at = ring_u;
+        unsigned bad_stages = 0, load_bit = 1;
+        // Of the unit under `lc`: its K/V head's part of the pools, its row of the table, and up to where
+        // its rows go a tile at a time.
         const unsigned char *kh, *vh;
         const uint32_t *ph;                                // this lane's operand of the pairs
         const int32_t *trow;
-        int hs;
+        int hs, row0, fast_end;
         auto load_unit = [&]() {
             hs = a.share == 1 ? lc.h : lc.h / a.share;
             kh = a.k + hs * a.k_sh + (lane / C::CPR) * a.k_sr + (lane % C::CPR) * 16;
             vh = a.v + hs * a.v_sh + (lane / C::CPR) * a.v_sr + (lane % C::CPR) * 16;
             if (Q4) ph = (lane < 16 ? a.kp : a.vp) + (long long)hs * a.page_size + (lane & 15);
             trow = a.table + (long long)lc.b * a.max_pages;
+            row0 = lc.i * R;
+            fast_end = a.one_page ? lc.len - 15 : 0;
         };
-        // Page numbers of the stage's tiles, one ahead of their copies; -1: the tile goes by row
-        // (it ends behind the sequence, or pages are no multiple of 16 rows).
+        // Page numbers of the stage's tiles, one ahead of their copies; -1: the tile goes by row.
         int page[TT];
         auto fetch_pages = [&]() {
 #pragma unroll
-            for (int tt = 0; tt < TT; ++tt) {
-                const int row0 = lc.i * R + 16 * tt;
-                page[tt] = -1;
-                if (a.one_page && row0 + 16 <= lc.len) page[tt] = __ldg(trow + (a.page_shift >= 0 ? row0 >> a.page_shift : row0 / a.page_size));
-            }
+            for (int tt = 0; tt < TT; ++tt) page[tt] = row0 + 16 * tt < fast_end ? __ldg(trow + ((row0 + 16 * tt) >> a.page_shift)) : -1;
         };
         load_unit();
         fetch_pages();
         uint32_t kd0, vd0;
         chunk_place<C>(lane / C::CPR, lane % C::CPR, kd0, vd0);
-        const long long k_step = (32 / C::CPR) * a.k_sr, v_step = (32 / C::CPR) * a.v_sr;
 
         auto issue = [&]() {                               // copies of the stage under `lc`, then on to the next
             bool bad = false;
 #pragma unroll
             for (int tt = 0; tt < TT; ++tt) {
-                const uint32_t dst = ring_u + load_stage * C::STAGE + tt * C::TILE;
-                const int row0 = lc.i * R + 16 * tt;
+                const uint32_t dst = load_at + tt * C::TILE;
                 if ((unsigned)page[tt] < (unsigned)a.num_pages) {
-                    const int off0 = a.page_shift >= 0 ? row0 & (a.page_size - 1) : row0 % a.page_size;
-                    const unsigned char *kr = kh + page[tt] * a.k_sp + off0 * a.k_sr;
-                    const unsigned char *vr = vh + page[tt] * a.v_sp + off0 * a.v_sr;
+                    const uint32_t pg = page[tt], off = (row0 + 16 * tt) & (a.page_size - 1);
+                    const unsigned char *kr = kh + (unsigned long long)pg * a.k_sp32 + (unsigned long long)off * a.k_sr32;
+                    const unsigned char *vr = vh + (unsigned long long)pg * a.v_sp32 + (unsigned long long)off * a.v_sr32;
 #pragma unroll
                     for (int i = 0; i < C::NCH; ++i) {
                         // the place of row r + i * (32 / CPR), from the place of row r: the swizzle's bits and the row's are apart
                         constexpr int RS = 32 / C::CPR;
                         const uint32_t kx = Q4 ? 0 : F32 ? ((i * RS) & 1) << 6 : ((i * RS) & 7) << 4;
                         const uint32_t vx = Q4 ? 0 : F32 ? ((i * RS) & 3) << 5 : ((i * RS) & 7) << 4;
-                        cp16(dst + (kd0 ^ kx) + i * RS * C::ROWB, kr);
-                        cp16(dst + C::KB + (vd0 ^ vx) + i * RS * C::ROWB, vr);
-                        kr += k_step; vr += v_step;
+                        cp16(dst + (kd0 ^ kx) + i * RS * C::ROWB, kr + (unsigned long long)(i * RS) * a.k_sr32);
+                        cp16(dst + C::KB + (vd0 ^ vx) + i * RS * C::ROWB, vr + (unsigned long long)(i * RS) * a.v_sr32);
                     }
-                    if (Q4) cp4(dst + 2 * C::KB + lane * 4, ph + ((long long)page[tt] * a.h_stored * a.page_size + off0));
+                    if (Q4) cp4(dst + 2 * C::KB + lane * 4, ph + ((unsigned long long)pg * a.p_sp32 + off));
                 } else {
-                    bad |= copy_ragged_tile<C>(a, dst, lc.b, hs, row0, lc.len);
+                    bad |= copy_ragged_tile<C>(a, dst, lc.b, hs, row0 + 16 * tt, lc.len);
                 }
             }
-            if (bad) bad_stages |= 1u << load_stage;
-            else bad_stages &= ~(1u << load_stage);
-            if (++load_stage == S) load_stage = 0;
+            bad_stages = bad ? bad_stages | load_bit : bad_stages & ~load_bit;
+            load_at += C::STAGE; load_bit <<= 1;
+            if (load_bit == 1u << S) { load_at = ring_u; load_bit = 1; }
             if (++loaded < n) {
-                if (tile_advance<R>(a, hv, lc)) load_unit();
+                if (tile_advance<R>(a, hv, lc)) load_unit(); else row0 += R;
                 fetch_pages();
             }
         };
@@ -789,7 +837,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                         const uint32_t r0 = pack16<false>(p[n][0] * s0, p[n][1] * s0), r1 = pack16<false>(p[n][2] * s1, p[n][3] * s1);
                         wt[n][0] = movmatrix_trans(r0);
                         wt[n][1] = movmatrix_trans(r1);
-                        if (fine) {                        // second terms of the weights
+                        if constexpr (C::FINE) {                        // second terms of the weights
                             const float2 f0 = unpack16<false>(r0), f1 = unpack16<false>(r1);
                             wl[n][0] = movmatrix_trans(pack16<false>(fmaf(p[n][0], s0, -f0.x), fmaf(p[n][1], s0, -f0.y)));
                             wl[n][1] = movmatrix_trans(pack16<false>(fmaf(p[n][2], s1, -f1.x), fmaf(p[n][3], s1, -f1.y)));
@@ -815,7 +863,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                                 const int to = 4 * j + 2 * i + e;
 #pragma unroll
                                 for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][to], a0, a1, a2, a3, wt[n][0], wt[n][1]);
-                                if (fine) {
+                                if constexpr (C::FINE) {
 #pragma unroll
                                     for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][to], a0, a1, a2, a3, wl[n][0], wl[n][1]);
                                 }
@@ -874,16 +922,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                 }
         };
 
-        int stage = 0;
+        uint32_t stage_at = ring_u;
+        unsigned stage_bit = 1;
         bool fresh = true;
 #pragma unroll 1
         for (int j = 0; j < n; ++j) {
             if (fresh) { begin_unit(); fresh = false; }
             cp_wait<S - 1>();
             __syncwarp();
-            process(ring_u + stage * C::STAGE, cc.len - cc.i * R, (bad_stages >> stage) & 1u);
+            process(stage_at, cc.len - cc.i * R, (bad_stages & stage_bit) != 0);
             __syncwarp();                                  // every lane is done with the stage
-            if (++stage == S) stage = 0;
+            stage_at += C::STAGE; stage_bit <<= 1;
+            if (stage_bit == 1u << S) { stage_at = ring_u; stage_bit = 1; }
             if (loaded < n) issue();
             cp_commit();
             const bool unit_ends = cc.i + 1 == cc.ub;
@@ -908,141 +958,166 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
     __syncthreads();
 
     // ---- join the pieces of units that this CTA's warps share -------------------------------
-    // Every warp works out the groups of segments for itself: segment `lane` leads a group when
-    // the valid segment before it belongs to another unit.
+    // Every warp works out the groups of segments for itself, a segment to a lane: one leads a group
+    // when the valid segment before it belongs to another unit.  Then a warp takes a head (or two): the
+    // segments' factors by shuffles, the features by its lanes.
     const long long u = s_seg[lane];
     const unsigned valid = __ballot_sync(0xffffffffu, u >= 0);
     if (valid == 0) return;                                // uniform for the CTA: nothing was cut
     const unsigned below = valid & ((1u << lane) - 1u);
     const long long pu = __shfl_sync(0xffffffffu, u, below ? 31 - __clz(below) : lane);
     const unsigned leaders = __ballot_sync(0xffffffffu, u >= 0 && (below == 0 || pu != u));
+    const unsigned upto = leaders & (0xffffffffu >> (31 - lane)), after = lane < 31 ? leaders >> (lane + 1) : 0u;
+    const int my_lead = upto ? 31 - __clz(upto) : 0, my_end = after ? lane + __ffs(after) - 1 : 31;
     auto members = [&](int lead) -> unsigned {             // segments of the group that segment `lead` leads
         const unsigned next = lead < 31 ? leaders >> (lead + 1) : 0u;
         return valid & (next ? (1u << (lead + __ffs(next))) - (1u << lead) : 0u - (1u << lead));
     };
-    auto seg_slot = [&](int sg) -> float * {
-        const int w = sg >> 1;
-        return (sg & 1) ? reinterpret_cast<float *>(smem + (size_t)w * S * C::STAGE) : first_slots + (size_t)w * C::SLOT;
+    auto seg_slot = [&](int sg) -> const float * {
+        return reinterpret_cast<const float *>((sg & 1) ? smem + (sg >> 1) * (S * C::STAGE)
+                                                        : smem + C::OFF_FIRST + (sg >> 1) * (C::SLOT * 4));
     };
-    auto cut = [&](int lead) { return s_seg_lo[lead] < c0 || s_seg_lo[lead] + s_seg_ub[lead] > c1; };
-    constexpr int LPR = D / 4, COLS = G * LPR;
-
-    // Factors: of every segment and head, 2^(m - M), beside the partial; for the leader the sum L too.
-    for (int idx = tid; idx < 2 * W * G; idx += C::THREADS) {
-        const int sg = idx / G, head = idx % G;
-        if (!(valid >> sg & 1u)) continue;
-        const int lead = 31 - __clz(leaders & (0xffffffffu >> (31 - sg)));
-        const unsigned mem = members(lead);
-        float M = -INFINITY;
-        for (unsigned r = mem; r != 0; r &= r - 1) M = fmaxf(M, seg_slot(__ffs(r) - 1)[head * PS + D]);
-        float *p = seg_slot(sg) + head * PS;
-        p[D + 2] = exp2_diff(p[D], M);
-        if (sg == lead) {
-            float L = 0.f;
-            for (unsigned r = mem; r != 0; r &= r - 1) {
-                const float *x = seg_slot(__ffs(r) - 1) + head * PS;
-                L = fmaf(exp2_diff(x[D], M), x[D + 1], L);
-            }
-            p[D + 3] = L;
-            s_top[lead][head] = M;
+    constexpr int LPR = D / 4, HPW = (G + W - 1) / W;
+    const int d = (lane % LPR) * 4;
+    float f[HPW], M[HPW], L[HPW];                          // of this lane's segment; M and L of its group
+#pragma unroll
+    for (int k = 0; k < HPW; ++k) {
+        const int head = warp + k * W;
+        float m = -INFINITY, l = 0.f;
+        if ((valid >> lane & 1u) && head < G) {
+            const float2 ml = *reinterpret_cast<const float2 *>(seg_slot(lane) + head * PS + D);
+            m = ml.x; l = ml.y;
         }
+        M[k] = m;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const float x = __shfl_up_sync(0xffffffffu, M[k], off);
+            if (lane - off >= my_lead) M[k] = fmaxf(M[k], x);
+        }
+        M[k] = __shfl_sync(0xffffffffu, M[k], my_end);
+        f[k] = exp2_diff(m, M[k]);
+        L[k] = f[k] * l;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const float x = __shfl_up_sync(0xffffffffu, L[k], off);
+            if (lane - off >= my_lead) L[k] += x;
+        }
+        L[k] = __shfl_sync(0xffffffffu, L[k], my_end);
     }
-    __syncthreads();
-    auto join = [&](int lead, int col) {
-        const int head = col / LPR, d = (col % LPR) * 4;
+    auto join = [&](int lead, int head, float fk) {        // this lane's four features of a group's sum
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
         for (unsigned r = members(lead); r != 0; r &= r - 1) {
-            const float *p = seg_slot(__ffs(r) - 1) + head * PS;
-            const float f = p[D + 2];
-            const float4 y = *reinterpret_cast<const float4 *>(p + d);
-            o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
+            const int sg = __ffs(r) - 1;
+            const float x = __shfl_sync(0xffffffffu, fk, sg);
+            const float4 y = *reinterpret_cast<const float4 *>(seg_slot(sg) + head * PS + d);
+            o.x = fmaf(x, y.x, o.x); o.y = fmaf(x, y.y, o.y); o.z = fmaf(x, y.z, o.z); o.w = fmaf(x, y.w, o.w);
         }
         return o;
     };
-    // Units cut between CTAs first (the first group, the last, or both): their partials leave, and
-    // are counted while the whole units are joined.
-    const int lead0 = __ffs(leaders) - 1, lead1 = 31 - __clz(leaders);
-    const bool cut0 = cut(lead0), cut1 = lead1 != lead0 && cut(lead1);
-    if (cut0 || cut1) {
-        for (int idx = tid; idx < 2 * COLS; idx += C::THREADS) {
-            const bool second = idx >= COLS;
-            if (second ? !cut1 : !cut0) continue;
-            const int lead = second ? lead1 : lead0, col = second ? idx - COLS : idx, head = col / LPR, d = (col % LPR) * 4;
-            float *p = a.ws + ((size_t)blockIdx.x * 2 + (s_seg_lo[lead] <= c0 ? 0 : 1)) * C::SLOT + head * PS;
-            *reinterpret_cast<float4 *>(p + d) = join(lead, col);
-            if (d == 0) { p[D] = s_top[lead][head]; p[D + 1] = seg_slot(lead)[head * PS + D + 3]; }
-        }
-        __syncthreads();
-        if (tid < 2) {                                     // one thread per cut unit
-            const int lead = tid ? lead1 : lead0;
-            int done = 0;
-            if (tid ? cut1 : cut0) {
-                const long long ulo = s_seg_lo[lead], uhi = ulo + s_seg_ub[lead];
-                const int first = part_of(total, ulo, active), last = part_of(total, uhi - 1, active);
-                asm volatile("fence.acq_rel.gpu;" ::: "memory");
-                done = ticket_arrive(&a.tickets[first], a.ticket_tag) == (unsigned)(last - first);
-                if (done) a.tickets[first] = 0ull;
-                asm volatile("fence.acq_rel.gpu;" ::: "memory");
-            }
-            s_done[tid] = done;
-        }
-    }
-    for (int idx = tid; idx < __popc(leaders) * COLS; idx += C::THREADS) {
-        unsigned r = leaders;
-        for (int k = idx / COLS; k > 0; --k) r &= r - 1;
-        const int lead = __ffs(r) - 1, col = idx % COLS, head = col / LPR, d = (col % LPR) * 4;
-        if (cut(lead)) continue;
-        const float4 o = join(lead, col);
-        const int b = s_seg_b[lead], qh = paged_query_head(a, b, s_seg_vh[lead], head);
-        const float inv = 1.0f / seg_slot(lead)[head * PS + D + 3];
-        if (qh >= 0)
+    auto emit = [&](int b, int vh, int head, const float4 &o, float sum) {
+        const int qh = paged_query_head(a, b, vh, head);
+        const float inv = 1.0f / sum;
+        if (qh >= 0 && lane < LPR)
             store4(a.out, ((long long)b * a.h_q + qh) * D + d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), dtype);
+    };
+    // Units cut between CTAs first (the first group, the last, or both): their partials leave and are
+    // counted, head by head, while the whole units are joined.
+    int lead_of[2] = {__ffs(leaders) - 1, 31 - __clz(leaders)}, first[2], last[2];
+    bool cut[2];
+    unsigned long long seen[HPW];                          // lanes 0 and 1: the counter of head k for cut unit `lane`
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int lead = lead_of[i];
+        const long long lo = s_seg_lo[lead], hi = lo + s_seg_ub[lead];
+        cut[i] = !whole && (lo < c0 || hi > c1) && (i == 0 || lead != lead_of[0]);
+        first[i] = last[i] = 0;
+        if (cut[i]) { first[i] = part_of(total, lo, active); last[i] = part_of(total, hi - 1, active); }
     }
-    if (!cut0 && !cut1) return;
+    if (cut[0] || cut[1]) {
+#pragma unroll
+        for (int k = 0; k < HPW; ++k) {
+            const int head = warp + k * W;
+            if (head >= G) break;
+#pragma unroll 1
+            for (int i = 0; i < 2; ++i) {
+                if (!(i ? cut[1] : cut[0])) continue;
+                const int lead = i ? lead_of[1] : lead_of[0];
+                float *p = a.ws + ((size_t)blockIdx.x * 2 + (s_seg_lo[lead] <= c0 ? 0 : 1)) * C::SLOT + head * PS;
+                const float4 o = join(lead, head, f[k]);
+                const float m = __shfl_sync(0xffffffffu, M[k], lead), l = __shfl_sync(0xffffffffu, L[k], lead);
+                if (lane < LPR) *reinterpret_cast<float4 *>(p + d) = o;
+                if (lane == 0) *reinterpret_cast<float2 *>(p + D) = make_float2(m, l);
+            }
+        }
+        __syncwarp();
+        if (lane < 2 && (lane ? cut[1] : cut[0])) {
+            asm volatile("fence.acq_rel.gpu;" ::: "memory");
+#pragma unroll
+            for (int k = 0; k < HPW; ++k)
+                if (warp + k * W < G) seen[k] = atomicAdd(a.tickets + (lane ? first[1] : first[0]) * G + warp + k * W, a.ticket_tag);
+        }
+    }
+#pragma unroll 1
+    for (unsigned r = leaders; r != 0; r &= r - 1) {
+        const int lead = __ffs(r) - 1;
+        if ((cut[0] && lead == lead_of[0]) || (cut[1] && lead == lead_of[1])) continue;
+#pragma unroll
+        for (int k = 0; k < HPW; ++k) {
+            const int head = warp + k * W;
+            if (head < G) emit(s_seg_b[lead], s_seg_vh[lead], head, join(lead, head, f[k]), __shfl_sync(0xffffffffu, L[k], lead));
+        }
+    }
+    if (!cut[0] && !cut[1]) return;
 
-    // ---- units cut between CTAs: whoever delivers the last piece joins them, in CTA order -----
-    __syncthreads();
-    for (int k = 0; k < 2; ++k) {
-        if (!s_done[k]) continue;                          // uniform for the CTA
-        const int lead = k ? lead1 : lead0;
-        const long long ulo = s_seg_lo[lead], uhi = ulo + s_seg_ub[lead];
-        const int first = part_of(total, ulo, active), last = part_of(total, uhi - 1, active);
-        const int slot0 = ulo == split_at(total, first, active) ? 0 : 1;      // a CTA's slot 0: the unit that its range begins in
-        const int b = s_seg_b[lead], vh = s_seg_vh[lead];
-        for (int col = tid; col < COLS; col += C::THREADS) {
-            const int head = col / LPR, d = (col % LPR) * 4;
-            float M = -INFINITY, L = 0.f, Lc = 0.f;
+    // ---- units cut between CTAs: the warp that delivers a head's last piece joins them, in CTA order --
+#pragma unroll
+    for (int k = 0; k < HPW; ++k) {
+        const int head = warp + k * W;
+        if (head >= G) break;
+        bool done = false;
+        if (lane < 2 && (lane ? cut[1] : cut[0])) {
+            unsigned long long *word = a.tickets + (lane ? first[1] : first[0]) * G + head;
+            done = ticket_count(word, a.ticket_tag, seen[k]) == (unsigned)(lane ? last[1] - first[1] : last[0] - first[0]);
+            if (done) *word = 0ull;
+            asm volatile("fence.acq_rel.gpu;" ::: "memory");
+        }
+        const unsigned dones = __ballot_sync(0xffffffffu, done);
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) {
+            if (!(dones >> i & 1u)) continue;
+            const int lead = i ? lead_of[1] : lead_of[0], c_first = i ? first[1] : first[0], c_last = i ? last[1] : last[0];
+            const int slot0 = s_seg_lo[lead] == split_at(total, c_first, active) ? 0 : 1;      // a CTA's slot 0: the unit that its range begins in
+            float top = -INFINITY, sum = 0.f, sumc = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f), oc = o;
-            constexpr int B = 4;                           // partials under way at once
-            for (int c = first; c <= last; c += B) {
+            constexpr int B = 8;                           // partials under way at once
+#pragma unroll 1
+            for (int c = c_first; c <= c_last; c += B) {
                 float4 y[B];
                 float2 ml[B];
 #pragma unroll
-                for (int i = 0; i < B; ++i) {
-                    const float *p = a.ws + ((size_t)min(c + i, last) * 2 + (c + i > first ? 0 : slot0)) * C::SLOT + head * PS;
-                    y[i] = __ldcg(reinterpret_cast<const float4 *>(p + d));
-                    ml[i] = __ldcg(reinterpret_cast<const float2 *>(p + D));
-                    if (c + i > last) ml[i] = make_float2(-INFINITY, 0.f);
+                for (int z = 0; z < B; ++z) {
+                    const float *p = a.ws + ((size_t)min(c + z, c_last) * 2 + (min(c + z, c_last) > c_first ? 0 : slot0)) * C::SLOT + head * PS;
+                    y[z] = __ldcg(reinterpret_cast<const float4 *>(p + d));
+                    ml[z] = __ldcg(reinterpret_cast<const float2 *>(p + D));
+                    if (c + z > c_last) ml[z] = make_float2(-INFINITY, 0.f);
                 }
-                float Mn = M;
+                float top_new = top;
 #pragma unroll
-                for (int i = 0; i < B; ++i) Mn = fmaxf(Mn, ml[i].x);
-                const float keep = exp2_diff(M, Mn);
-                o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep; L *= keep;
-                oc.x *= keep; oc.y *= keep; oc.z *= keep; oc.w *= keep; Lc *= keep;
-                M = Mn;
+                for (int z = 0; z < B; ++z) top_new = fmaxf(top_new, ml[z].x);
+                const float keep = exp2_diff(top, top_new);
+                o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep; sum *= keep;
+                oc.x *= keep; oc.y *= keep; oc.z *= keep; oc.w *= keep; sumc *= keep;
+                top = top_new;
 #pragma unroll
-                for (int i = 0; i < B; ++i) {
-                    if (c + i > last) break;
-                    const float f = exp2_diff(ml[i].x, M);
-                    comp_fma4(o, oc, y[i], f);
-                    comp_fma(L, Lc, ml[i].y, f);
+                for (int z = 0; z < B; ++z) {
+                    if (c + z > c_last) break;
+                    const float x = exp2_diff(ml[z].x, top);
+                    comp_fma4(o, oc, y[z], x);
+                    comp_fma(sum, sumc, ml[z].y, x);
                 }
             }
-            const int qh = paged_query_head(a, b, vh, head);
-            const float inv = 1.0f / L;
-            if (qh >= 0)
-                store4(a.out, ((long long)b * a.h_q + qh) * D + d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), dtype);
+            emit(s_seg_b[lead], s_seg_vh[lead], head, o, sum);
         }
     }
 }
