@@ -998,9 +998,13 @@ static int paged_decode_impl(const moa_paged_cache *c, const void *q, void *out,
     a.k_sp = ks[0]; a.k_sh = ks[1]; a.k_sr = ks[2];
     a.v_sp = vs[0]; a.v_sh = vs[1]; a.v_sr = vs[2];
     a.num_pages = c->num_pages; a.page_size = c->page_size;
-    a.page_shift = page_shift_of(c->page_size);
+    // exact for rows below 2^31: page_mul * page_size exceeds 2^page_sh by less than 2^(page_sh - 31)
+    int log2_up = 0;
+    while ((1LL << log2_up) < c->page_size) ++log2_up;
+    a.page_sh = 31 + log2_up;
+    a.page_mul = (uint32_t)(((1ULL << a.page_sh) + c->page_size - 1) / c->page_size);
     const long long pairs = (long long)c->h_kv * c->page_size, top = 0xffffffffLL;
-    a.one_page = a.page_shift >= 4 && ks[0] <= top && ks[2] <= top && vs[0] <= top && vs[2] <= top && pairs <= top;
+    a.one_page = c->page_size >= 16 && (c->page_size & (c->page_size - 1)) == 0 && ks[0] <= top && ks[2] <= top && vs[0] <= top && vs[2] <= top && pairs <= top;
     if (a.one_page) {
         a.k_sp32 = (uint32_t)ks[0]; a.k_sr32 = (uint32_t)ks[2];
         a.v_sp32 = (uint32_t)vs[0]; a.v_sr32 = (uint32_t)vs[2];

@@ -45,7 +45,8 @@ struct PagedArgs {
     long long k_sp, k_sh, k_sr;      // byte strides: page, kv head, row
     long long v_sp, v_sh, v_sr;
     int num_pages, page_size;
-    int page_shift;                  // log2(page_size), or -1
+    uint32_t page_mul;               // row / page_size = row * page_mul >> page_sh, for rows below 2^31
+    int page_sh;
     // A tile of 16 rows lies in one page (page_size a power of two, 16 at least), and these byte strides
     // (page and row; pairs of a page) fit 32 bits: the copies' addresses are two multiply-adds each.
     int one_page;
@@ -163,6 +164,12 @@ __device__ __forceinline__ float2 unpack16(uint32_t r)
     if (BF16) return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u));
     return __half22float2(*reinterpret_cast<const __half2 *>(&r));
 }
+__device__ __forceinline__ float4 lds4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 // One element of a tensor of `dtype` as a float, and four floats into one.
 __device__ __forceinline__ float load_as_float(const void *p, long long i, int dtype)
 {
@@ -184,6 +191,11 @@ __device__ __forceinline__ void store1(void *p, long long i, float v, int dtype)
     if (dtype == MOA_F32) static_cast<float *>(p)[i] = v;
     else if (dtype == MOA_BF16) static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
     else static_cast<__half *>(p)[i] = __float2half_rn(v);
+}
+
+__device__ __forceinline__ int page_index(const PagedArgs &a, int row)
+{
+    return (int)(((unsigned long long)(unsigned)row * a.page_mul) >> a.page_sh);
 }
 
 __device__ __forceinline__ int paged_len(const PagedArgs &a, int b)       // 0: nothing to attend to
@@ -235,22 +247,22 @@ __device__ __forceinline__ void chunk_place(int r, int c, uint32_t &kd, uint32_t
 }
 
 // Copies of one tile whose rows may lie in several pages, end behind the sequence (zero-filled), or
-// have pages that do not exist (zero-filled, reported).  One row per lane (lanes 16..31 repeat); out of
-// line, so that the common case (16 rows of one page) has the loop to itself.
+// have pages that do not exist (zero-filled, reported).  A row per lane (lanes 16..31 repeat): `page` is
+// that of row row0 + lane % 16.  Out of line, so that the common case (16 rows of one page) has the
+// loop to itself.  True: a page does not exist.
 template <class C>
-__device__ __noinline__ bool copy_ragged_tile(const PagedArgs &a, uint32_t dst, int b, int hs, int row0, int len)
+__device__ __noinline__ bool copy_ragged_tile(const PagedArgs &a, uint32_t dst, int page, int hs, int row0, int len)
 {
     const int lane = threadIdx.x & 31, row = row0 + (lane & 15);
     long long ko = -1, vo = 0, po = 0;
     bool bad = false;
     if (row < len) {
-        const int pi = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size, off = row - pi * a.page_size;
-        const long long page = __ldg(a.table + (long long)b * a.max_pages + pi);
+        const int off = row - page_index(a, row) * a.page_size;
         bad = page < 0 || page >= a.num_pages;
         if (!bad) {
             ko = page * a.k_sp + hs * a.k_sh + off * a.k_sr;
             vo = page * a.v_sp + hs * a.v_sh + off * a.v_sr;
-            po = (page * a.h_stored + hs) * a.page_size + off;
+            po = ((long long)page * a.h_stored + hs) * a.page_size + off;
         }
     }
     const int c = lane % C::CPR;
@@ -310,6 +322,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
     launch_dependents();
     if (lane < 2) s_seg[2 * warp + lane] = -1;             // (read behind the barrier at the end)
     if (warp == 0 && lane >= 2 * W) s_seg[lane] = -1;
+    // Into L2 while the kernel before this one ends: what the first copies depend on (lengths, page table,
+    // queries).  A hint, no access: what that kernel still writes is read from L2 as it stands then.
+    {
+        const long long id = (long long)blockIdx.x * C::THREADS + tid, lens_n = (a.batch + 31) / 32,
+                        table_n = ((long long)a.batch * a.max_pages + 31) / 32,
+                        q_n = ((long long)(a.batch - 1) * a.q_sb + a.h_q * D) * (dtype == MOA_F32 ? 4 : 2) / 128;
+        const unsigned char *p = nullptr;
+        if (id < lens_n) p = reinterpret_cast<const unsigned char *>(a.seq_lens) + id * 128;
+        else if (id < lens_n + q_n) p = static_cast<const unsigned char *>(a.q) + (id - lens_n) * 128;
+        else if (id < lens_n + q_n + table_n) p = reinterpret_cast<const unsigned char *>(a.table) + (id - lens_n - q_n) * 128;
+        if (p != nullptr) asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+    }
     grid_dependency_wait();
 
     // ---- lengths: stages per sequence and their prefix ---------------------------------------
@@ -475,11 +499,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             row0 = lc.i * R;
             fast_end = a.one_page ? lc.len - 15 : 0;
         };
-        // Page numbers of the stage's tiles, one ahead of their copies; -1: the tile goes by row.
+        // Page numbers of the stage's tiles, one stage ahead of their copies: of the tile, or of the lane's row
+        // where the tile goes by row.
         int page[TT];
         auto fetch_pages = [&]() {
 #pragma unroll
-            for (int tt = 0; tt < TT; ++tt) page[tt] = row0 + 16 * tt < fast_end ? __ldg(trow + ((row0 + 16 * tt) >> a.page_shift)) : -1;
+            for (int tt = 0; tt < TT; ++tt) {
+                const int r0 = row0 + 16 * tt, row = r0 < fast_end ? r0 : r0 + (lane & 15);
+                page[tt] = row < lc.len ? __ldg(trow + page_index(a, row)) : -1;
+            }
         };
         load_unit();
         fetch_pages();
@@ -491,7 +519,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
             for (int tt = 0; tt < TT; ++tt) {
                 const uint32_t dst = load_at + tt * C::TILE;
-                if ((unsigned)page[tt] < (unsigned)a.num_pages) {
+                if (row0 + 16 * tt < fast_end && (unsigned)page[tt] < (unsigned)a.num_pages) {
                     const uint32_t pg = page[tt], off = (row0 + 16 * tt) & (a.page_size - 1);
                     const unsigned char *kr = kh + (unsigned long long)pg * a.k_sp32 + (unsigned long long)off * a.k_sr32;
                     const unsigned char *vr = vh + (unsigned long long)pg * a.v_sp32 + (unsigned long long)off * a.v_sr32;
@@ -506,7 +534,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     }
                     if (Q4) cp4(dst + 2 * C::KB + lane * 4, ph + ((unsigned long long)pg * a.p_sp32 + off));
                 } else {
-                    bad |= copy_ragged_tile<C>(a, dst, lc.b, hs, row0 + 16 * tt, lc.len);
+                    bad |= copy_ragged_tile<C>(a, dst, page[tt], hs, row0 + 16 * tt, lc.len);
                 }
             }
             bad_stages = bad ? bad_stages | load_bit : bad_stages & ~load_bit;
@@ -973,9 +1001,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         const unsigned next = lead < 31 ? leaders >> (lead + 1) : 0u;
         return valid & (next ? (1u << (lead + __ffs(next))) - (1u << lead) : 0u - (1u << lead));
     };
-    auto seg_slot = [&](int sg) -> const float * {
-        return reinterpret_cast<const float *>((sg & 1) ? smem + (sg >> 1) * (S * C::STAGE)
-                                                        : smem + C::OFF_FIRST + (sg >> 1) * (C::SLOT * 4));
+    auto seg_slot = [&](int sg) -> uint32_t {              // shared address of its partial
+        return smem_u + ((sg & 1) ? (sg >> 1) * (S * C::STAGE) : (int)C::OFF_FIRST + (sg >> 1) * (C::SLOT * 4));
     };
     constexpr int LPR = D / 4, HPW = (G + W - 1) / W;
     const int d = (lane % LPR) * 4;
@@ -985,7 +1012,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         const int head = warp + k * W;
         float m = -INFINITY, l = 0.f;
         if ((valid >> lane & 1u) && head < G) {
-            const float2 ml = *reinterpret_cast<const float2 *>(seg_slot(lane) + head * PS + D);
+            const float4 ml = lds4(seg_slot(lane) + (head * PS + D) * 4);
             m = ml.x; l = ml.y;
         }
         M[k] = m;
@@ -1010,7 +1037,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         for (unsigned r = members(lead); r != 0; r &= r - 1) {
             const int sg = __ffs(r) - 1;
             const float x = __shfl_sync(0xffffffffu, fk, sg);
-            const float4 y = *reinterpret_cast<const float4 *>(seg_slot(sg) + head * PS + d);
+            const float4 y = lds4(seg_slot(sg) + (head * PS + d) * 4);
             o.x = fmaf(x, y.x, o.x); o.y = fmaf(x, y.y, o.y); o.z = fmaf(x, y.z, o.z); o.w = fmaf(x, y.w, o.w);
         }
         return o;
@@ -1090,7 +1117,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             const int slot0 = s_seg_lo[lead] == split_at(total, c_first, active) ? 0 : 1;      // a CTA's slot 0: the unit that its range begins in
             float top = -INFINITY, sum = 0.f, sumc = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f), oc = o;
-            constexpr int B = 8;                           // partials under way at once
+            constexpr int B = 4;                           // partials under way at once
 #pragma unroll 1
             for (int c = c_first; c <= c_last; c += B) {
                 float4 y[B];
