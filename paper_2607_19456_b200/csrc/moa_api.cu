@@ -918,7 +918,7 @@ static int paged_grid(const DeviceState &s)
     return g_num_ctas > 0 ? (g_num_ctas < kTicketCtas ? g_num_ctas : kTicketCtas) : (s.sm_count < kTicketCtas ? s.sm_count : kTicketCtas);
 }
 
-static size_t paged_ticket_bytes(int grid, int heads) { return (size_t)grid * heads * sizeof(unsigned long long); }
+static size_t paged_ticket_bytes(int grid) { return (size_t)grid * sizeof(unsigned long long); }
 static size_t paged_slot_bytes(int grid, int heads, int d)
 {
     return ((size_t)grid * 2 * heads * (d + 4) * sizeof(float) + 255) / 256 * 256;
@@ -951,10 +951,10 @@ static cudaError_t launch_paged(int format, int heads, const PagedArgs &a, int g
     switch (format) {
     case MOA_KV_F32: return launch_paged_cfg<PagedCfg<MOA_KV_F32, D, 1, wide ? 6 : 8, 2, 1>>(a, grid, st);
     case MOA_KV_BF16:
-        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 1, 8, wide ? 2 : 4, 1>>(a, grid, st);
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 1, wide ? 8 : 12, 2, wide ? 1 : 2>>(a, grid, st);
         return launch_paged_cfg<PagedCfg<MOA_KV_BF16, D, 2, 8, wide ? 2 : 4, 1>>(a, grid, st);
     case MOA_KV_F16:
-        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 1, 8, wide ? 2 : 4, 1>>(a, grid, st);
+        if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 1, wide ? 8 : 12, 2, wide ? 1 : 2>>(a, grid, st);
         return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 2, 8, wide ? 2 : 4, 1>>(a, grid, st);
     default:
         if (a.dtype == MOA_F16) {
@@ -991,7 +991,7 @@ static int paged_decode_impl(const moa_paged_cache *c, const void *q, void *out,
     if (rc != MOA_OK) return rc;
     const int g = h_q / c->h_kv, heads = paged_heads(c->format, g), grid = paged_grid(*dev);
     const size_t slots = paged_slot_bytes(grid, heads, c->d);
-    if (ws_bytes < slots + paged_ticket_bytes(grid, heads)) return MOA_ERR_WORKSPACE;
+    if (ws_bytes < slots + paged_ticket_bytes(grid)) return MOA_ERR_WORKSPACE;
 
     a.k = static_cast<const unsigned char *>(c->k); a.v = static_cast<const unsigned char *>(c->v);
     a.kp = static_cast<const uint32_t *>(c->k_params); a.vp = static_cast<const uint32_t *>(c->v_params);
@@ -1467,7 +1467,7 @@ size_t moa_paged_workspace_bytes(int batch, int h_q, int h_kv, int d)
     plain.sm_count = 256;                  // no device: an upper bound
     const int grid = paged_grid(current_device(&dev) == MOA_OK ? *dev : plain);
     const int heads = paged_heads(MOA_KV_BF16, h_q / h_kv);
-    return paged_slot_bytes(grid, heads, d) + (paged_ticket_bytes(grid, heads) + 255) / 256 * 256;
+    return paged_slot_bytes(grid, heads, d) + (paged_ticket_bytes(grid) + 255) / 256 * 256;
 }
 
 int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int dtype, int batch, int n_out,

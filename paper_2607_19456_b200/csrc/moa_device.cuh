@@ -249,11 +249,10 @@ constexpr int kTicketStride = kTicketCtas + 1;
 constexpr size_t kTicketBytes = (size_t)kTicketStride * sizeof(unsigned long long);
 constexpr unsigned long long kTicketCountMask = (1ull << 20) - 1ull;
 
-// `old` is what adding `inc` to `word` found there; returns the number of arrivals of this
-// launch before this one.
-__device__ __forceinline__ unsigned ticket_count(unsigned long long *word, unsigned long long inc,
-                                                 unsigned long long old)
+// Count one arrival on `word`; returns the number of arrivals of this launch before this one.
+__device__ __forceinline__ unsigned ticket_arrive(unsigned long long *word, unsigned long long inc)
 {
+    unsigned long long old = atomicAdd(word, inc);
     for (;;) {
         const unsigned long long j = old & kTicketCountMask;
         if (old == j * inc) return (unsigned)j;
@@ -265,12 +264,6 @@ __device__ __forceinline__ unsigned ticket_count(unsigned long long *word, unsig
         if (atomicCAS(word, seen, inc) == seen) return 0u;
         old = ~0ull;                            // lost the race: look again
     }
-}
-
-// Count one arrival on `word`; returns the number of arrivals of this launch before this one.
-__device__ __forceinline__ unsigned ticket_arrive(unsigned long long *word, unsigned long long inc)
-{
-    return ticket_count(word, inc, atomicAdd(word, inc));
 }
 
 // Length of sequence b as the kernels see it; 0 for an out-of-range length (the item is

@@ -65,7 +65,7 @@ struct PagedArgs {
     int g_total;                     // query heads per stored kv head
     float qscale;                    // scale * log2(e)
     float *ws;                       // two partial slots per CTA
-    unsigned long long *tickets;     // G for every CTA: counters of the pieces of the unit that is cut at its end
+    unsigned long long *tickets;     // for every CTA: counter of the pieces of the unit that is cut at its end
     unsigned long long ticket_tag;
 };
 
@@ -314,6 +314,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
     __shared__ long long s_seg[32];                        // unit of segment 2 * warp + (0: first, 1: last), or -1
     __shared__ long long s_seg_lo[32];                     // flat index of that unit's first stage
     __shared__ int s_seg_ub[32], s_seg_vh[32], s_seg_b[32];    // its stages, virtual kv head, sequence
+    __shared__ int s_done[2];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int hv = a.h_stored * a.share;
@@ -1049,10 +1050,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             store4(a.out, ((long long)b * a.h_q + qh) * D + d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), dtype);
     };
     // Units cut between CTAs first (the first group, the last, or both): their partials leave and are
-    // counted, head by head, while the whole units are joined.
+    // counted while the whole units are joined.  One release and one count per CTA and cut unit: fences of
+    // several warps of an SM wait for one another (a count per head and warp took 30 us on 16 heads).
     int lead_of[2] = {__ffs(leaders) - 1, 31 - __clz(leaders)}, first[2], last[2];
     bool cut[2];
-    unsigned long long seen[HPW];                          // lanes 0 and 1: the counter of head k for cut unit `lane`
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int lead = lead_of[i];
@@ -1061,7 +1062,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         first[i] = last[i] = 0;
         if (cut[i]) { first[i] = part_of(total, lo, active); last[i] = part_of(total, hi - 1, active); }
     }
-    if (cut[0] || cut[1]) {
+    const bool any_cut = cut[0] || cut[1];
+    if (any_cut) {
 #pragma unroll
         for (int k = 0; k < HPW; ++k) {
             const int head = warp + k * W;
@@ -1077,12 +1079,19 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                 if (lane == 0) *reinterpret_cast<float2 *>(p + D) = make_float2(m, l);
             }
         }
-        __syncwarp();
-        if (lane < 2 && (lane ? cut[1] : cut[0])) {
-            asm volatile("fence.acq_rel.gpu;" ::: "memory");
-#pragma unroll
-            for (int k = 0; k < HPW; ++k)
-                if (warp + k * W < G) seen[k] = atomicAdd(a.tickets + (lane ? first[1] : first[0]) * G + warp + k * W, a.ticket_tag);
+        __syncthreads();
+        if (tid < 2) {
+            int done = 0;
+            if (tid ? cut[1] : cut[0]) {
+                unsigned long long *word = a.tickets + (tid ? first[1] : first[0]);
+                asm volatile("fence.acq_rel.gpu;" ::: "memory");
+                done = ticket_arrive(word, a.ticket_tag) == (unsigned)(tid ? last[1] - first[1] : last[0] - first[0]);
+                if (done) {
+                    *word = 0ull;
+                    asm volatile("fence.acq_rel.gpu;" ::: "memory");
+                }
+            }
+            s_done[tid] = done;
         }
     }
 #pragma unroll 1
@@ -1095,53 +1104,51 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             if (head < G) emit(s_seg_b[lead], s_seg_vh[lead], head, join(lead, head, f[k]), __shfl_sync(0xffffffffu, L[k], lead));
         }
     }
-    if (!cut[0] && !cut[1]) return;
+    if (!any_cut) return;
 
-    // ---- units cut between CTAs: the warp that delivers a head's last piece joins them, in CTA order --
-#pragma unroll
-    for (int k = 0; k < HPW; ++k) {
-        const int head = warp + k * W;
-        if (head >= G) break;
-        bool done = false;
-        if (lane < 2 && (lane ? cut[1] : cut[0])) {
-            unsigned long long *word = a.tickets + (lane ? first[1] : first[0]) * G + head;
-            done = ticket_count(word, a.ticket_tag, seen[k]) == (unsigned)(lane ? last[1] - first[1] : last[0] - first[0]);
-            if (done) *word = 0ull;
-            asm volatile("fence.acq_rel.gpu;" ::: "memory");
-        }
-        const unsigned dones = __ballot_sync(0xffffffffu, done);
+    // ---- units cut between CTAs: the CTA that delivers the last piece joins them, in CTA order --------
+    __syncthreads();
 #pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-            if (!(dones >> i & 1u)) continue;
-            const int lead = i ? lead_of[1] : lead_of[0], c_first = i ? first[1] : first[0], c_last = i ? last[1] : last[0];
-            const int slot0 = s_seg_lo[lead] == split_at(total, c_first, active) ? 0 : 1;      // a CTA's slot 0: the unit that its range begins in
-            float top = -INFINITY, sum = 0.f, sumc = 0.f;
+    for (int i = 0; i < 2; ++i) {
+        if (!s_done[i]) continue;
+        const int lead = i ? lead_of[1] : lead_of[0], c_first = i ? first[1] : first[0], c_last = i ? last[1] : last[0];
+        const int slot0 = s_seg_lo[lead] == split_at(total, c_first, active) ? 0 : 1;      // a CTA's slot 0: the unit that its range begins in
+#pragma unroll 1
+        for (int head = warp; head < G; head += W) {
+            float top = -INFINITY, sum = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f), oc = o;
-            constexpr int B = 4;                           // partials under way at once
 #pragma unroll 1
-            for (int c = c_first; c <= c_last; c += B) {
+            for (int c = c_first; c <= c_last; c += 32) {  // 32 partials' factors at once, one to a lane
+                const int n = min(32, c_last - c + 1);
+                const float *p = a.ws + ((size_t)(c + min(lane, n - 1)) * 2 + (c + lane > c_first ? 0 : slot0)) * C::SLOT + head * PS;
+                float2 ml = __ldcg(reinterpret_cast<const float2 *>(p + D));
+                constexpr int B = 8;                       // rows under way at once, the first beside the factors
                 float4 y[B];
-                float2 ml[B];
+                auto fetch = [&](int z0) {
 #pragma unroll
-                for (int z = 0; z < B; ++z) {
-                    const float *p = a.ws + ((size_t)min(c + z, c_last) * 2 + (min(c + z, c_last) > c_first ? 0 : slot0)) * C::SLOT + head * PS;
-                    y[z] = __ldcg(reinterpret_cast<const float4 *>(p + d));
-                    ml[z] = __ldcg(reinterpret_cast<const float2 *>(p + D));
-                    if (c + z > c_last) ml[z] = make_float2(-INFINITY, 0.f);
-                }
-                float top_new = top;
+                    for (int z = 0; z < B; ++z)
+                        if (z0 + z < n) y[z] = __ldcg(reinterpret_cast<const float4 *>(
+                            a.ws + ((size_t)(c + z0 + z) * 2 + (c + z0 + z > c_first ? 0 : slot0)) * C::SLOT + head * PS + d));
+                };
+                fetch(0);
+                if (lane >= n) ml = make_float2(-INFINITY, 0.f);
+                float top_new = fmaxf(top, ml.x);
 #pragma unroll
-                for (int z = 0; z < B; ++z) top_new = fmaxf(top_new, ml[z].x);
-                const float keep = exp2_diff(top, top_new);
-                o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep; sum *= keep;
-                oc.x *= keep; oc.y *= keep; oc.z *= keep; oc.w *= keep; sumc *= keep;
+                for (int off = 1; off < 32; off <<= 1) top_new = fmaxf(top_new, __shfl_xor_sync(0xffffffffu, top_new, off));
+                const float keep = exp2_diff(top, top_new), x = exp2_diff(ml.x, top_new);
+                float add = x * ml.y;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) add += __shfl_xor_sync(0xffffffffu, add, off);
+                sum = fmaf(sum, keep, add);
+                o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+                oc.x *= keep; oc.y *= keep; oc.z *= keep; oc.w *= keep;
                 top = top_new;
+#pragma unroll 1
+                for (int z0 = 0; z0 < n; z0 += B) {
+                    if (z0 > 0) fetch(z0);
 #pragma unroll
-                for (int z = 0; z < B; ++z) {
-                    if (c + z > c_last) break;
-                    const float x = exp2_diff(ml[z].x, top);
-                    comp_fma4(o, oc, y[z], x);
-                    comp_fma(sum, sumc, ml[z].y, x);
+                    for (int z = 0; z < B; ++z)
+                        if (z0 + z < n) comp_fma4(o, oc, y[z], __shfl_sync(0xffffffffu, x, z0 + z));
                 }
             }
             emit(s_seg_b[lead], s_seg_vh[lead], head, o, sum);
