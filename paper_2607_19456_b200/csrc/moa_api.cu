@@ -1103,10 +1103,10 @@ static int paged_append_impl(const moa_paged_cache *c, const void *q, const void
     a.q_st = s[0]; a.k_st = s[1]; a.v_st = s[2]; a.o_st = s[3];
     a.tokens = tokens; a.h_q = h_q; a.token_start = token_start;
     a.cos_sin = cos_sin; a.rope_rows = rope_rows; a.rot = rot_dim; a.pairs = rope_style == MOA_ROPE_PAIRS;
-    // Heads of one run: 8 share the search for the token's sequence and page and its cosines and sines
+    // Heads of one run: 4 share the search for the token's sequence and page and its cosines and sines
     // where there are rows enough to fill the GPU that way, one where there are not.
     const long long fill = (long long)dev->sm_count * 1024 / (c->d / 16);
-    a.run = rows >= 8 * fill ? 8 : rows >= 4 * fill ? 4 : rows >= 2 * fill ? 2 : 1;
+    a.run = rows >= 4 * fill ? 4 : rows >= 2 * fill ? 2 : 1;
     a.q_runs = (h_q + a.run - 1) / a.run;
     a.kv_runs = (c->h_kv + a.run - 1) / a.run;
     cudaError_t e;
@@ -1123,8 +1123,7 @@ static int paged_append_impl(const moa_paged_cache *c, const void *q, const void
 template <int D>
 static cudaError_t launch_gather(int format, const PagedIoArgs &a, int dtype, cudaStream_t st)
 {
-    const long long rows = (long long)a.batch * a.h_kv * a.n_out, per_block = 256 / (D / 8);
-    const int blocks = (int)((rows + per_block - 1) / per_block);
+    const int blocks = (int)((long long)a.batch * a.h_kv * ((a.n_out - 1) / kGatherRows + 1));
     switch (format) {
     case MOA_KV_F32: launch_dependent(paged_gather_kernel<MOA_KV_F32, D>, blocks, 256, 0, st, a, dtype); break;
     case MOA_KV_BF16: launch_dependent(paged_gather_kernel<MOA_KV_BF16, D>, blocks, 256, 0, st, a, dtype); break;
@@ -1147,7 +1146,7 @@ static int paged_gather_impl(const moa_paged_cache *c, void *k_out, void *v_out,
     if (!aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(seq_lens, 4) || !aligned(page_table, 4) ||
         (row_start && !aligned(row_start, 4)))
         return MOA_ERR_ALIGN;
-    if ((double)batch * c->h_kv * n_out > 2147483647.0 * 16) return MOA_ERR_CAPACITY;
+    if ((double)batch * c->h_kv * ((n_out - 1) / kGatherRows + 1) > 2147483647.0) return MOA_ERR_CAPACITY;
     DeviceState *dev = nullptr;
     rc = current_device(&dev);
     if (rc != MOA_OK) return rc;

@@ -113,13 +113,32 @@ __device__ __forceinline__ void pack_row(const float (&lo)[8], const float (&hi)
     c_lo = c_hi = 0u;
     if (bad) { params = 0x7fff7fffu; return; }
     if (s > 0.f) {
+        // round((x - m) / s): with the reciprocal, which is within 2^-22 of the quotient's 15 at most; a thread
+        // that comes nearer than 2^-16 to a border between two codes divides.
+        const float r = __frcp_rn(s);
+        float c[16];
+        bool near = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float a = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(lo[i], m), s)), 0.f), 15.f);
-            const float b = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(hi[i], m), s)), 0.f), 15.f);
-            c_lo |= (uint32_t)a << (4 * i);
-            c_hi |= (uint32_t)b << (4 * i);
+        for (int i = 0; i < 16; ++i) {
+            const float x = i < 8 ? lo[i] : hi[i - 8];
+            const float q = fminf(fmaxf(__fmul_rn(__fsub_rn(x, m), r), 0.f), 15.f);
+            c[i] = rintf(q);
+            near |= fabsf(q - c[i]) > 0.5f - 1.0f / 65536.0f;
         }
+        if (near) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float x = i < 8 ? lo[i] : hi[i - 8];
+                c[i] = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x, m), s)), 0.f), 15.f);
+            }
+        }
+        // Four codes make an exact number below 2^16, whose bits a float of 2^23 more shows.
+        uint32_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            h[i] = __float_as_uint(fmaf(4096.f, c[4 * i + 3], fmaf(256.f, c[4 * i + 2], fmaf(16.f, c[4 * i + 1], c[4 * i]))) + 8388608.0f) & 0xffffu;
+        c_lo = h[0] | h[1] << 16;
+        c_hi = h[2] | h[3] << 16;
     }
     params = (uint32_t)__half_as_ushort(s16) | ((uint32_t)__half_as_ushort(m16) << 16);
 }
@@ -158,6 +177,17 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
     const int h0 = (run - (kind == 0 ? 0 : kind == 1 ? a.q_runs : a.q_runs + a.kv_runs)) * a.run;
     const int h1 = min(h0 + a.run, kind == 0 ? a.h_q : a.h_kv);
 
+    // The first row is under way while its place is found.
+    int d_lo = 16 * part, d_hi = 16 * part + 8;
+    const bool turns = TURN != kTurnNone && kind != 2 && 16 * part < a.rot;
+    if (TURN == kTurnChunks && turns) { d_lo = 8 * part; d_hi = a.rot / 2 + 8 * part; }
+    const unsigned char *src = kind == 0 ? static_cast<const unsigned char *>(a.q) + tok * a.q_st * ES
+                             : kind == 1 ? static_cast<const unsigned char *>(a.k) + tok * a.k_st * ES
+                                         : static_cast<const unsigned char *>(a.v) + tok * a.v_st * ES;
+    src += (long long)h0 * D * ES;
+    RowPart<DT> next;
+    fetch<DT>(next, src, d_lo, d_hi);
+
     // The token's sequence, position and row.
     int b = tok;
     long long pos;
@@ -188,11 +218,8 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
         return;
     }
 
-    // Places of this thread's two chunks, and its share of the token's cosines and sines.
+    // This thread's share of the token's cosines and sines.
     const int rot = a.rot, half = rot / 2;
-    int d_lo = 16 * part, d_hi = 16 * part + 8;
-    const bool turns = TURN != kTurnNone && kind != 2 && 16 * part < rot;
-    if (TURN == kTurnChunks && turns) { d_lo = 8 * part; d_hi = half + 8 * part; }
     float cs[8], sn[8];
     const float *row = a.cos_sin + pos * rot;
     if constexpr (TURN == kTurnChunks || TURN == kTurnPairs) {
@@ -203,18 +230,12 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
             sn[i] = in ? __ldg(row + half + 8 * part + i) : 0.f;
         }
     }
-    const unsigned char *src = kind == 0 ? static_cast<const unsigned char *>(a.q) + tok * a.q_st * ES
-                             : kind == 1 ? static_cast<const unsigned char *>(a.k) + tok * a.k_st * ES
-                                         : static_cast<const unsigned char *>(a.v) + tok * a.v_st * ES;
     unsigned char *dst = kind == 0 ? static_cast<unsigned char *>(a.q_out) + tok * a.o_st * ES
                        : kind == 1 ? a.k_pool + page * a.k_sp + off * a.k_sr : a.v_pool + page * a.v_sp + off * a.v_sr;
     const long long dst_step = kind == 0 ? D * ES : kind == 1 ? a.k_sh : a.v_sh;
-    src += (long long)h0 * D * ES;
     dst += h0 * dst_step;
     uint32_t *par = FMT == MOA_KV_INT4 && kind != 0 ? (kind == 1 ? a.kp : a.vp) + (page * a.h_kv + h0) * a.page_size + off : nullptr;
 
-    RowPart<DT> next;
-    fetch<DT>(next, src, d_lo, d_hi);
 #pragma unroll 1
     for (int h = h0; h < h1; ++h, src += D * ES, dst += dst_step) {
         const RowPart<DT> now = next;
@@ -263,60 +284,65 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
     }
 }
 
-// Rows [row_start, seq_len) of every sequence into [batch, h_kv, n_out, D]; a thread takes eight
-// features of one row of K and of V.
+// Rows [row_start, seq_len) of every sequence into [batch, h_kv, n_out, D].  A block takes 64 rows of one
+// slab, a thread eight features of K and of V in four of them.
+constexpr int kGatherRows = 64;
 template <int FMT, int D>
 __global__ void __launch_bounds__(256) paged_gather_kernel(const __grid_constant__ PagedIoArgs a, int out_dtype)
 {
-    constexpr int TPR = D / 8, SLOTS = 256 / TPR;
+    constexpr int TPR = D / 8, SLOTS = 256 / TPR, PASSES = kGatherRows / SLOTS;
     launch_dependents();
     grid_dependency_wait();
-    const int d = (threadIdx.x % TPR) * 8;
-    const long long item = (long long)blockIdx.x * SLOTS + threadIdx.x / TPR;     // (b, h, i)
-    if (item >= (long long)a.batch * a.h_kv * a.n_out) return;
-    const int i = (int)(item % a.n_out);
-    const int b = (int)(item / a.n_out / a.h_kv), h = (int)(item / a.n_out % a.h_kv);
+    const unsigned chunks = (a.n_out - 1) / kGatherRows + 1;
+    const unsigned slab = blockIdx.x / chunks;
+    const int i0 = (int)(blockIdx.x - slab * chunks) * kGatherRows;
+    const int b = (int)(slab / a.h_kv), h = (int)(slab - (unsigned)b * a.h_kv);
     const int len = __ldg(a.seq_lens + b), from = a.row_start != nullptr ? __ldg(a.row_start + b) : 0;
     if (from < 0 || len < from || (long long)len - from > a.n_out || len > (long long)a.max_pages * a.page_size) {
-        if (i == 0 && h == 0 && d == 0) raise_status(MOA_STATUS_SEQLEN_RANGE);
+        if (i0 == 0 && h == 0 && threadIdx.x == 0) raise_status(MOA_STATUS_SEQLEN_RANGE);
         return;
     }
-    const int row = from + i;
-    if (i >= len - from) return;
-    const int pi = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size;
-    const int off = row - pi * a.page_size;
-    const long long page = __ldg(a.table + (long long)b * a.max_pages + pi);
-    if (page < 0 || page >= a.num_pages) {
-        if (d == 0) raise_status(MOA_STATUS_PAGE_RANGE);
-        return;
-    }
-    const unsigned char *ks = a.k_pool + page * a.k_sp + h * a.k_sh + off * a.k_sr;
-    const unsigned char *vs = a.v_pool + page * a.v_sp + h * a.v_sh + off * a.v_sr;
-    float x[8], y[8];
-    if constexpr (FMT == MOA_KV_INT4) {
-        const long long at = (page * a.h_kv + h) * a.page_size + off;
-        const uint32_t kc = *reinterpret_cast<const uint32_t *>(ks + d / 2), vc = *reinterpret_cast<const uint32_t *>(vs + d / 2);
-        const float2 kf = unpack16<false>(a.kp[at]), vf = unpack16<false>(a.vp[at]);
+    const int d = (threadIdx.x % TPR) * 8;
+    constexpr int ES = FMT == MOA_KV_F32 ? 4 : 2;
+    const unsigned char *kh = a.k_pool + h * a.k_sh + (FMT == MOA_KV_INT4 ? d / 2 : d * ES);
+    const unsigned char *vh = a.v_pool + h * a.v_sh + (FMT == MOA_KV_INT4 ? d / 2 : d * ES);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = fmaf(kf.x, (float)((kc >> (4 * e)) & 15u), kf.y);
-            y[e] = fmaf(vf.x, (float)((vc >> (4 * e)) & 15u), vf.y);
+    for (int p = 0; p < PASSES; ++p) {
+        const int i = i0 + p * SLOTS + threadIdx.x / TPR, row = from + i;
+        if (i >= len - from) return;                       // (and so are the rows of later passes)
+        const int pi = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size;
+        const int off = row - pi * a.page_size;
+        const long long page = __ldg(a.table + (long long)b * a.max_pages + pi);
+        if (page < 0 || page >= a.num_pages) {
+            if (d == 0) raise_status(MOA_STATUS_PAGE_RANGE);
+            continue;
         }
-    } else {
-        constexpr int ES = FMT == MOA_KV_F32 ? 4 : 2;
-        load8<FMT>(x, ks + d * ES);
-        load8<FMT>(y, vs + d * ES);
-    }
-    const long long to = item * D + d;
-    if (out_dtype == MOA_F32) {
-        store8<MOA_F32>(static_cast<float *>(a.k_out) + to, x);
-        store8<MOA_F32>(static_cast<float *>(a.v_out) + to, y);
-    } else if (out_dtype == MOA_BF16) {
-        store8<MOA_BF16>(static_cast<uint16_t *>(a.k_out) + to, x);
-        store8<MOA_BF16>(static_cast<uint16_t *>(a.v_out) + to, y);
-    } else {
-        store8<MOA_F16>(static_cast<uint16_t *>(a.k_out) + to, x);
-        store8<MOA_F16>(static_cast<uint16_t *>(a.v_out) + to, y);
+        const unsigned char *ks = kh + page * a.k_sp + off * a.k_sr, *vs = vh + page * a.v_sp + off * a.v_sr;
+        float x[8], y[8];
+        if constexpr (FMT == MOA_KV_INT4) {
+            const long long at = (page * a.h_kv + h) * a.page_size + off;
+            const uint32_t kc = *reinterpret_cast<const uint32_t *>(ks), vc = *reinterpret_cast<const uint32_t *>(vs);
+            const float2 kf = unpack16<false>(a.kp[at]), vf = unpack16<false>(a.vp[at]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {                  // a code as the low bits of 2^23 + code
+                x[e] = fmaf(kf.x, __uint_as_float(((kc >> (4 * e)) & 15u) | 0x4b000000u) - 8388608.0f, kf.y);
+                y[e] = fmaf(vf.x, __uint_as_float(((vc >> (4 * e)) & 15u) | 0x4b000000u) - 8388608.0f, vf.y);
+            }
+        } else {
+            load8<FMT>(x, ks);
+            load8<FMT>(y, vs);
+        }
+        const long long to = ((long long)slab * a.n_out + i) * D + d;
+        if (out_dtype == MOA_F32) {
+            store8<MOA_F32>(static_cast<float *>(a.k_out) + to, x);
+            store8<MOA_F32>(static_cast<float *>(a.v_out) + to, y);
+        } else if (out_dtype == MOA_BF16) {
+            store8<MOA_BF16>(static_cast<uint16_t *>(a.k_out) + to, x);
+            store8<MOA_BF16>(static_cast<uint16_t *>(a.v_out) + to, y);
+        } else {
+            store8<MOA_F16>(static_cast<uint16_t *>(a.k_out) + to, x);
+            store8<MOA_F16>(static_cast<uint16_t *>(a.v_out) + to, y);
+        }
     }
 }
 
