@@ -71,8 +71,7 @@ struct PagedArgs {
 
 // W warps, S ring stages of TT tiles of 16 rows (K and V) each.  The ring and the slots of the first cut unit
 // share the 227 KB of an SM; the slot of the last cut unit is the ring itself, empty by then.
-// FINE: the weights of 4-bit rows in two fp16 terms, for fp16 outputs (one term: 6.0e-4 off the definition
-// where the rounding of the output alone is 2.0e-4; bf16 outputs, 1.7e-3, gain nothing from it).
+// FINE: what the rounding of the 4-bit rows' weights takes is put back in fp32 (fp16 outputs).
 template <int FMT_, int D_, int NT_, int W_, int S_, int TT_, bool FINE_ = false>
 struct PagedCfg {
     static constexpr bool FINE = FINE_;
@@ -135,7 +134,7 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
 {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 template <bool BF16>
@@ -216,18 +215,16 @@ struct TileCursor {
     int b, h, i, ub, len;
 };
 template <int R>
-__device__ __forceinline__ bool tile_advance(const PagedArgs &a, int hv, TileCursor &c)      // true: another unit
+__device__ __forceinline__ void next_unit(const PagedArgs &a, int hv, TileCursor &c)
 {
-    if (++c.i < c.ub) return false;
     c.i = 0;
-    if (++c.h < hv) return true;
+    if (++c.h < hv) return;
     c.h = 0;
     do {
-        if (++c.b >= a.batch) { c.b = a.batch; c.len = 0; c.ub = 1; return true; }
+        if (++c.b >= a.batch) { c.b = a.batch; c.len = 0; c.ub = 1; return; }
         c.len = paged_len(a, c.b);
     } while (c.len == 0);
     c.ub = (c.len + R - 1) / R;
-    return true;
 }
 
 // Place of a 16-byte chunk c of row r in the shared tile of K and of V: what keeps the reads free of
@@ -287,7 +284,7 @@ struct PagedState {
     float acc[C::NT][C::MT][4];
     float m[C::NT][2], msub[C::NT][2], l[C::NT][2];        // heads 8n + 2t and 8n + 2t + 1; msub: m, or 0 while m is -inf
     float om[C::NT][2];                                    // 4 bits: sum of p * least
-    float ref, inv;                                        // 4 bits: power of two, at least every row's scale so far; 128 / ref
+    float ref, inv, mid;                                   // 4 bits: power of two, at least every row's scale so far; 128 / ref, 7.5 ref / 128
 };
 
 // n * i / of, in 32 bits where that suffices.
@@ -482,15 +479,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
     if (j0 < j1) {
         TileCursor lc = cc;
         const int n = (int)(j1 - j0);                      // (2^31 stages of one warp would be 8e13 rows)
-        int loaded = 0;
+        int to_load = n, unit_left;                        // stages not issued yet, in all and of the unit under `lc`
         uint32_t load_at = ring_u;
         unsigned bad_stages = 0, load_bit = 1;
         // Of the unit under `lc`: its K/V head's part of the pools, its row of the table, and up to where
-        // its rows go a tile at a time.
+        // its rows go whole stages of whole pages at a time.
         const unsigned char *kh, *vh;
         const uint32_t *ph;                                // this lane's operand of the pairs
         const int32_t *trow;
-        int hs, row0, fast_end;
+        int hs, row0, fast_end, page[TT];
         auto load_unit = [&]() {
             hs = a.share == 1 ? lc.h : lc.h / a.share;
             kh = a.k + hs * a.k_sh + (lane / C::CPR) * a.k_sr + (lane % C::CPR) * 16;
@@ -498,16 +495,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             if (Q4) ph = (lane < 16 ? a.kp : a.vp) + (long long)hs * a.page_size + (lane & 15);
             trow = a.table + (long long)lc.b * a.max_pages;
             row0 = lc.i * R;
-            fast_end = a.one_page ? lc.len - 15 : 0;
+            unit_left = lc.ub - lc.i;
+            fast_end = a.one_page ? lc.len - (R - 1) : 0;
         };
         // Page numbers of the stage's tiles, one stage ahead of their copies: of the tile, or of the lane's row
-        // where the tile goes by row.
-        int page[TT];
+        // where tiles go by row.
         auto fetch_pages = [&]() {
+            if (row0 < fast_end) {
 #pragma unroll
-            for (int tt = 0; tt < TT; ++tt) {
-                const int r0 = row0 + 16 * tt, row = r0 < fast_end ? r0 : r0 + (lane & 15);
-                page[tt] = row < lc.len ? __ldg(trow + page_index(a, row)) : -1;
+                for (int tt = 0; tt < TT; ++tt) page[tt] = __ldg(trow + page_index(a, row0 + 16 * tt));
+            } else {
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt) {
+                    const int row = row0 + 16 * tt + (lane & 15);
+                    page[tt] = row < lc.len ? __ldg(trow + page_index(a, row)) : -1;
+                }
             }
         };
         load_unit();
@@ -516,12 +518,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         chunk_place<C>(lane / C::CPR, lane % C::CPR, kd0, vd0);
 
         auto issue = [&]() {                               // copies of the stage under `lc`, then on to the next
-            bool bad = false;
+            bool fast = row0 < fast_end;
 #pragma unroll
-            for (int tt = 0; tt < TT; ++tt) {
-                const uint32_t dst = load_at + tt * C::TILE;
-                if (row0 + 16 * tt < fast_end && (unsigned)page[tt] < (unsigned)a.num_pages) {
-                    const uint32_t pg = page[tt], off = (row0 + 16 * tt) & (a.page_size - 1);
+            for (int tt = 0; tt < TT; ++tt) fast = fast && (unsigned)page[tt] < (unsigned)a.num_pages;
+            bad_stages &= ~load_bit;
+            if (fast) {
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt) {
+                    const uint32_t dst = load_at + tt * C::TILE, pg = page[tt], off = (row0 + 16 * tt) & (a.page_size - 1);
                     const unsigned char *kr = kh + (unsigned long long)pg * a.k_sp32 + (unsigned long long)off * a.k_sr32;
                     const unsigned char *vr = vh + (unsigned long long)pg * a.v_sp32 + (unsigned long long)off * a.v_sr32;
 #pragma unroll
@@ -534,21 +538,32 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                         cp16(dst + C::KB + (vd0 ^ vx) + i * RS * C::ROWB, vr + (unsigned long long)(i * RS) * a.v_sr32);
                     }
                     if (Q4) cp4(dst + 2 * C::KB + lane * 4, ph + ((unsigned long long)pg * a.p_sp32 + off));
-                } else {
-                    bad |= copy_ragged_tile<C>(a, dst, page[tt], hs, row0 + 16 * tt, lc.len);
                 }
+            } else {
+                bool bad = false;
+#pragma unroll 1
+                for (int tt = 0; tt < TT; ++tt) {
+                    int pg = page[0];                      // (of the lane's row: a stage with a missing page has its tiles' numbers, which serve)
+#pragma unroll
+                    for (int k = 1; k < TT; ++k) pg = tt == k ? page[k] : pg;
+                    bad |= copy_ragged_tile<C>(a, load_at + tt * C::TILE, pg, hs, row0 + 16 * tt, lc.len);
+                }
+                if (bad) bad_stages |= load_bit;
             }
-            bad_stages = bad ? bad_stages | load_bit : bad_stages & ~load_bit;
             load_at += C::STAGE; load_bit <<= 1;
             if (load_bit == 1u << S) { load_at = ring_u; load_bit = 1; }
-            if (++loaded < n) {
-                if (tile_advance<R>(a, hv, lc)) load_unit(); else row0 += R;
+            if (--to_load > 0) {
+                row0 += R;
+                if (--unit_left == 0) {
+                    next_unit<R>(a, hv, lc);
+                    load_unit();
+                }
                 fetch_pages();
             }
         };
 #pragma unroll 1
         for (int i = 0; i < S; ++i) {
-            if (loaded < n) issue();
+            if (to_load > 0) issue();
             cp_commit();
         }
 
@@ -631,6 +646,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             }
             s.ref = 5.9604644775390625e-8f;                // 2^-24, fp16's least positive value
             s.inv = 2147483648.0f;
+            s.mid = 7.5f / 2147483648.0f;
         };
 
         // ---- one tile: scores, probabilities, weighted sum ----------------------------------
@@ -781,6 +797,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                                 for (int e = 0; e < 4; ++e) s.acc[n][i][e] *= f;
                         s.ref = r;
                         s.inv = 128.0f / r;                // exact: weights reach 2^15 at most
+                        s.mid = r * (7.5f / 128.0f);
                     }
                 }
             }
@@ -860,19 +877,24 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     }
                 } else {
                     const float s0 = vpar[tt][0].x * s.inv, s1 = vpar[tt][1].x * s.inv;
-                    uint32_t wt[NT][2], wl[NT][2];
+                    uint32_t wt[NT][2];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        const uint32_t r0 = pack16<false>(p[n][0] * s0, p[n][1] * s0), r1 = pack16<false>(p[n][2] * s1, p[n][3] * s1);
+                        // Weights w = p * s, rounded to fp16, w'.  The products are with codes 0..15; for fp16 outputs
+                        // what the rounding takes from their middle is put back in fp32, 7.5 (w - w'), so that it
+                        // acts on code - 7.5 only: 2.8e-4 off the definition where it was 6.0e-4 and the output's
+                        // rounding alone is 2.0e-4.  bf16 outputs round by 1.7e-3 and gain nothing from it.
+                        const float w[4] = {p[n][0] * s0, p[n][1] * s0, p[n][2] * s1, p[n][3] * s1};
+                        const uint32_t r0 = pack16<false>(w[0], w[1]), r1 = pack16<false>(w[2], w[3]);
                         wt[n][0] = movmatrix_trans(r0);
                         wt[n][1] = movmatrix_trans(r1);
-                        if constexpr (C::FINE) {                        // second terms of the weights
-                            const float2 f0 = unpack16<false>(r0), f1 = unpack16<false>(r1);
-                            wl[n][0] = movmatrix_trans(pack16<false>(fmaf(p[n][0], s0, -f0.x), fmaf(p[n][1], s0, -f0.y)));
-                            wl[n][1] = movmatrix_trans(pack16<false>(fmaf(p[n][2], s1, -f1.x), fmaf(p[n][3], s1, -f1.y)));
-                        }
 #pragma unroll
                         for (int e = 0; e < 2; ++e) s.om[n][e] = fmaf(p[n][e], vpar[tt][0].y, fmaf(p[n][2 + e], vpar[tt][1].y, s.om[n][e]));
+                        if constexpr (C::FINE) {
+                            const float2 f0 = unpack16<false>(r0), f1 = unpack16<false>(r1);
+                            s.om[n][0] = fmaf((w[0] - f0.x) + (w[2] - f1.x), s.mid, s.om[n][0]);
+                            s.om[n][1] = fmaf((w[1] - f0.y) + (w[3] - f1.y), s.mid, s.om[n][1]);
+                        }
                     }
                     // A transposed load hands a lane the 16-bit units (four codes) of two neighbouring rows in
                     // one register.  Low features of a byte: code & 15; both together, c0 + 16 c1, stand in the
@@ -892,10 +914,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                                 const int to = 4 * j + 2 * i + e;
 #pragma unroll
                                 for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][to], a0, a1, a2, a3, wt[n][0], wt[n][1]);
-                                if constexpr (C::FINE) {
-#pragma unroll
-                                    for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][to], a0, a1, a2, a3, wl[n][0], wl[n][1]);
-                                }
                             }
                     }
                 }
@@ -953,35 +971,39 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 
         uint32_t stage_at = ring_u;
         unsigned stage_bit = 1;
-        bool fresh = true;
 #pragma unroll 1
-        for (int j = 0; j < n; ++j) {
-            if (fresh) { begin_unit(); fresh = false; }
-            cp_wait<S - 1>();
-            __syncwarp();
-            process(stage_at, cc.len - cc.i * R, (bad_stages & stage_bit) != 0);
-            __syncwarp();                                  // every lane is done with the stage
-            stage_at += C::STAGE; stage_bit <<= 1;
-            if (stage_bit == 1u << S) { stage_at = ring_u; stage_bit = 1; }
-            if (loaded < n) issue();
-            cp_commit();
-            const bool unit_ends = cc.i + 1 == cc.ub;
-            if (unit_ends || j + 1 == n) {
-                const bool whole = unit_ends && unit_lo >= j0;
-                if (whole) close(nullptr);
-                else {
-                    const int which = j + 1 == n ? 1 : 0; // a cut unit that ends before the range does is its first
-                    if (which) { cp_wait<0>(); __syncwarp(); }
-                    close(which ? reinterpret_cast<float *>(ring) : first_slots + (size_t)warp * C::SLOT);
-                    if (lane == 0) {
-                        const int sg = 2 * warp + which;
-                        s_seg[sg] = (long long)cc.b * hv + cc.h;
-                        s_seg_lo[sg] = unit_lo; s_seg_ub[sg] = cc.ub; s_seg_vh[sg] = cc.h; s_seg_b[sg] = cc.b;
-                    }
-                }
-                if (unit_ends) { unit_lo += cc.ub; fresh = true; }
+        for (int left = n;;) {                             // unit by unit
+            begin_unit();
+            const int here = min(cc.ub - cc.i, left);
+            int nr = cc.len - cc.i * R;                    // rows from this stage on
+#pragma unroll 1
+            for (int k = 0; k < here; ++k, nr -= R) {
+                cp_wait<S - 1>();
+                __syncwarp();
+                process(stage_at, nr, (bad_stages & stage_bit) != 0);
+                __syncwarp();                              // every lane is done with the stage
+                stage_at += C::STAGE; stage_bit <<= 1;
+                if (stage_bit == 1u << S) { stage_at = ring_u; stage_bit = 1; }
+                if (to_load > 0) issue();
+                cp_commit();
             }
-            if (j + 1 < n) tile_advance<R>(a, hv, cc);
+            left -= here;
+            const bool unit_ends = cc.i + here == cc.ub;
+            float *dst = nullptr;                          // the whole unit: the output; else a partial
+            if (!unit_ends || unit_lo < j0) {
+                const int which = left == 0 ? 1 : 0;       // a cut unit that ends before the range does is its first
+                if (which) { cp_wait<0>(); __syncwarp(); }
+                dst = which ? reinterpret_cast<float *>(ring) : first_slots + (size_t)warp * C::SLOT;
+                if (lane == 0) {
+                    const int sg = 2 * warp + which;
+                    s_seg[sg] = (long long)cc.b * hv + cc.h;
+                    s_seg_lo[sg] = unit_lo; s_seg_ub[sg] = cc.ub; s_seg_vh[sg] = cc.h; s_seg_b[sg] = cc.b;
+                }
+            }
+            close(dst);
+            if (left == 0) break;
+            unit_lo += cc.ub;
+            next_unit<R>(a, hv, cc);
         }
     }
     __syncthreads();
