@@ -957,10 +957,6 @@ static cudaError_t launch_paged(int format, int heads, const PagedArgs &a, int g
         if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 1, wide ? 8 : 12, 2, wide ? 1 : 2>>(a, grid, st);
         return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 2, 8, wide ? 2 : 4, 1>>(a, grid, st);
     default:
-        if (a.dtype == MOA_F16) {
-            if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 12, 2, 2, true>>(a, grid, st);
-            return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 8, wide ? 3 : 4, 2, true>>(a, grid, st);
-        }
         if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 12, 2, 2>>(a, grid, st);
         return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 8, wide ? 3 : 4, 2>>(a, grid, st);
     }

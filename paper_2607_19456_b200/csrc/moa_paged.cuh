@@ -24,9 +24,9 @@
 //  - fp32: both operands split into two tf32 terms, three products (hi*hi, hi*lo, lo*hi), short chains.
 //  - 4 bits: a code c in 0..15 is used as the fp16 bit pattern c, the subnormal c * 2^-24: unpacking
 //    is one AND for two codes (another for the codes four bits up, which come out 16 times as large);
-//    V's bytes are used whole, c0 + 16 c1, beside c0 alone, which takes four instructions for eight codes.
+//    V's bytes are used whole, c0 + 16 c1, beside c0 alone: four instructions for eight codes.
 //    The score of a row is scale * (s * <q, c> + m * sum(q)) with the row's (s, m); in the weighted
-//    sum the weight of a row is p * s, and sum(p * m) is kept beside it.  q is brought to fp16 by a
+//    sum the weight of a row is p * s, and sum(p * (m + 8 s)) is kept beside it.  q is brought to fp16 by a
 //    power of two per head (exact but for terms 2^-38 of the largest); the weights are brought into
 //    fp16's range by a power of two that follows the largest s seen.
 #pragma once
@@ -71,10 +71,8 @@ struct PagedArgs {
 
 // W warps, S ring stages of TT tiles of 16 rows (K and V) each.  The ring and the slots of the first cut unit
 // share the 227 KB of an SM; the slot of the last cut unit is the ring itself, empty by then.
-// FINE: what the rounding of the 4-bit rows' weights takes is put back in fp32 (fp16 outputs).
-template <int FMT_, int D_, int NT_, int W_, int S_, int TT_, bool FINE_ = false>
+template <int FMT_, int D_, int NT_, int W_, int S_, int TT_>
 struct PagedCfg {
-    static constexpr bool FINE = FINE_;
     static constexpr int FMT = FMT_, D = D_, NT = NT_, W = W_, S = S_, TT = TT_;
     static constexpr int THREADS = W * 32, R = 16 * TT;    // rows of a stage
     static constexpr int ROWB = FMT == MOA_KV_F32 ? 4 * D : FMT == MOA_KV_INT4 ? D / 2 : 2 * D;   // bytes of a row
@@ -283,8 +281,8 @@ template <class C>
 struct PagedState {
     float acc[C::NT][C::MT][4];
     float m[C::NT][2], msub[C::NT][2], l[C::NT][2];        // heads 8n + 2t and 8n + 2t + 1; msub: m, or 0 while m is -inf
-    float om[C::NT][2];                                    // 4 bits: sum of p * least
-    float ref, inv, mid;                                   // 4 bits: power of two, at least every row's scale so far; 128 / ref, 7.5 ref / 128
+    float om[C::NT][2];                                    // 4 bits: sum of p * (least + 8 scale)
+    float ref, inv;                                        // 4 bits: power of two, at least every row's scale so far; 128 / ref
 };
 
 // n * i / of, in 32 bits where that suffices.
@@ -646,7 +644,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             }
             s.ref = 5.9604644775390625e-8f;                // 2^-24, fp16's least positive value
             s.inv = 2147483648.0f;
-            s.mid = 7.5f / 2147483648.0f;
         };
 
         // ---- one tile: scores, probabilities, weighted sum ----------------------------------
@@ -797,7 +794,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                                 for (int e = 0; e < 4; ++e) s.acc[n][i][e] *= f;
                         s.ref = r;
                         s.inv = 128.0f / r;                // exact: weights reach 2^15 at most
-                        s.mid = r * (7.5f / 128.0f);
                     }
                 }
             }
@@ -805,6 +801,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
                 for (int n = 0; n < NT; ++n) s.l[n][0] = s.l[n][1] = __int_as_float(0x7fffffff);
             }
+            uint32_t wt[TT][NT][2];                        // 4 bits: weights p * s as B operand
 #pragma unroll
             for (int tt = 0; tt < TT; ++tt) {
                 const uint32_t sv = st + tt * C::TILE + C::KB;
@@ -877,45 +874,72 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     }
                 } else {
                     const float s0 = vpar[tt][0].x * s.inv, s1 = vpar[tt][1].x * s.inv;
-                    uint32_t wt[NT][2];
+                    const float mid0 = fmaf(8.f, vpar[tt][0].x, vpar[tt][0].y), mid1 = fmaf(8.f, vpar[tt][1].x, vpar[tt][1].y);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        // Weights w = p * s, rounded to fp16, w'.  The products are with codes 0..15; for fp16 outputs
-                        // what the rounding takes from their middle is put back in fp32, 7.5 (w - w'), so that it
-                        // acts on code - 7.5 only: 2.8e-4 off the definition where it was 6.0e-4 and the output's
-                        // rounding alone is 2.0e-4.  bf16 outputs round by 1.7e-3 and gain nothing from it.
-                        const float w[4] = {p[n][0] * s0, p[n][1] * s0, p[n][2] * s1, p[n][3] * s1};
-                        const uint32_t r0 = pack16<false>(w[0], w[1]), r1 = pack16<false>(w[2], w[3]);
-                        wt[n][0] = movmatrix_trans(r0);
-                        wt[n][1] = movmatrix_trans(r1);
+                        wt[tt][n][0] = movmatrix_trans(pack16<false>(p[n][0] * s0, p[n][1] * s0));
+                        wt[tt][n][1] = movmatrix_trans(pack16<false>(p[n][2] * s1, p[n][3] * s1));
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) s.om[n][e] = fmaf(p[n][e], vpar[tt][0].y, fmaf(p[n][2 + e], vpar[tt][1].y, s.om[n][e]));
-                        if constexpr (C::FINE) {
-                            const float2 f0 = unpack16<false>(r0), f1 = unpack16<false>(r1);
-                            s.om[n][0] = fmaf((w[0] - f0.x) + (w[2] - f1.x), s.mid, s.om[n][0]);
-                            s.om[n][1] = fmaf((w[1] - f0.y) + (w[3] - f1.y), s.mid, s.om[n][1]);
-                        }
+                        for (int e = 0; e < 2; ++e) s.om[n][e] = fmaf(p[n][e], mid0, fmaf(p[n][2 + e], mid1, s.om[n][e]));
                     }
-                    // A transposed load hands a lane the 16-bit units (four codes) of two neighbouring rows in
-                    // one register.  Low features of a byte: code & 15; both together, c0 + 16 c1, stand in the
-                    // rows of the high ones, whose sums are taken apart at the end of the unit.
+                }
+            }
+            if constexpr (Q4) {
+                // Weighted sum of the stage's codes, from zero, then added to the unit's in fp32.  The sums are of c - 8:
+                // with codes from 0 they would carry 7.5 steps of every row, which over 1e5 rows are 500 times
+                // the result, and the rounding of the accumulation and of the weights would act on them (7.4e-4 off the
+                // definition at 131072 rows with fp16 outputs, whose own rounding is 2.0e-4; this way 3.0e-4).
+                // What is to be taken off, 8 * sum of the rounded weights, comes as a product of its own with a
+                // constant operand, which the sums start from.  Low features of a byte: its low code; the rows of
+                // the high ones hold c0 + 16 c1 (so 136 comes off), taken apart at the end of the unit.
+                float off[NT][4];
 #pragma unroll
-                    for (int j = 0; j < D / 64; ++j) {
-                        uint32_t r[4];                     // columns 16j.. of 16-bit units: rows 0-7, 8-15; columns 16j + 8..: the same
-                        const int row = (lane & 7) + (((lane >> 3) & 1) << 3), ch = 2 * j + (lane >> 4);
-                        ldsm4t(r, sv + row * C::ROWB + ((ch ^ (D == 128 ? (row >> 1) & 3 : (row >> 2) & 1)) << 4));
+                for (int n = 0; n < NT; ++n) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
+                    for (int e = 0; e < 4; ++e) off[n][e] = 0.f;
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {  // output tile 4j + 2i + e: features 4(8(2j + i) + g) + 2e, + 1
-                                const uint32_t a1 = e ? __byte_perm(r[2 * i], 0u, 0x4341) : r[2 * i] & 0x00ff00ffu;
-                                const uint32_t a3 = e ? __byte_perm(r[2 * i + 1], 0u, 0x4341) : r[2 * i + 1] & 0x00ff00ffu;
-                                const uint32_t a0 = a1 & 0x000f000fu, a2 = a3 & 0x000f000fu;
-                                const int to = 4 * j + 2 * i + e;
+                    for (int tt = 0; tt < TT; ++tt)
+                        mma_16x8x16<false>(off[n], 0x80088008u, 0x80888088u, 0x80088008u, 0x80888088u, wt[tt][n][0], wt[tt][n][1]);
+                }
 #pragma unroll
-                                for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s.acc[n][to], a0, a1, a2, a3, wt[n][0], wt[n][1]);
+                for (int j = 0; j < D / 64; ++j) {
+                    // A transposed load hands a lane the 16-bit units (four codes) of two neighbouring rows in one
+                    // register: columns 16j.. of units, rows 0-7, 8-15; columns 16j + 8..: the same.
+                    uint32_t r[TT][4];
+                    const int row = (lane & 7) + (((lane >> 3) & 1) << 3), ch = 2 * j + (lane >> 4);
+#pragma unroll
+                    for (int tt = 0; tt < TT; ++tt)
+                        ldsm4t(r[tt], st + tt * C::TILE + C::KB + row * C::ROWB + ((ch ^ (D == 128 ? (row >> 1) & 3 : (row >> 2) & 1)) << 4));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {      // output tile 4j + 2i + e: features 4(8(2j + i) + g) + 2e, + 1
+                            float sum[NT][4];
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int z = 0; z < 4; ++z) sum[n][z] = off[n][z];
+#pragma unroll
+                            for (int tt = 0; tt < TT; ++tt) {
+                                const uint32_t a1 = e ? __byte_perm(r[tt][2 * i], 0u, 0x4341) : r[tt][2 * i] & 0x00ff00ffu;
+                                const uint32_t a3 = e ? __byte_perm(r[tt][2 * i + 1], 0u, 0x4341) : r[tt][2 * i + 1] & 0x00ff00ffu;
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+                                    mma_16x8x16<false>(sum[n], a1 & 0x000f000fu, a1, a3 & 0x000f000fu, a3, wt[tt][n][0], wt[tt][n][1]);
                             }
-                    }
+                            const int to = 4 * j + 2 * i + e;
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int z = 0; z < 4; z += 2) {
+                                    const uint64_t x = add2(pack2(__float_as_uint(s.acc[n][to][z]), __float_as_uint(s.acc[n][to][z + 1])),
+                                                            pack2(__float_as_uint(sum[n][z]), __float_as_uint(sum[n][z + 1])));
+                                    uint32_t x0, x1;
+                                    unpack2(x, x0, x1);
+                                    s.acc[n][to][z] = __uint_as_float(x0);
+                                    s.acc[n][to][z + 1] = __uint_as_float(x1);
+                                }
+                        }
                 }
             }
         };
