@@ -688,18 +688,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[tt][n][e] = (x[tt][n][e] + (lh[n][e] + hl[n][e])) * a.qscale;
                 } else if constexpr (!Q4) {
-                    float c[NT][4] = {};
+                    float c[2][NT][4] = {};                // two chains: half the products wait for one another
 #pragma unroll
                     for (int i = 0; i < C::KSTEPS; ++i) {
                         uint32_t r[4];
                         ldsm4(r, sk + (lane & 15) * C::ROWB + (((2 * i + (lane >> 4)) ^ (lane & 7)) << 4));
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma_16x8x16<BF>(c[n], r[0], r[1], r[2], r[3], qf[n][i][0], qf[n][i][1]);
+                        for (int n = 0; n < NT; ++n) mma_16x8x16<BF>(c[i & 1][n], r[0], r[1], r[2], r[3], qf[n][i][0], qf[n][i][1]);
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[tt][n][e] = c[n][e] * a.qscale;
+                        for (int e = 0; e < 4; ++e) x[tt][n][e] = (c[0][n][e] + c[1][n][e]) * a.qscale;
                 } else {
                     constexpr int NW = D / 32;
                     uint32_t w0[NW], w1[NW];
@@ -1081,11 +1081,24 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
     auto join = [&](int lead, int head, float fk) {        // this lane's four features of a group's sum
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-        for (unsigned r = members(lead); r != 0; r &= r - 1) {
-            const int sg = __ffs(r) - 1;
-            const float x = __shfl_sync(0xffffffffu, fk, sg);
-            const float4 y = lds4(seg_slot(sg) + (head * PS + d) * 4);
-            o.x = fmaf(x, y.x, o.x); o.y = fmaf(x, y.y, o.y); o.z = fmaf(x, y.z, o.z); o.w = fmaf(x, y.w, o.w);
+        for (unsigned r = members(lead); r != 0;) {        // four under way at once (the last one again, unused, where there are fewer)
+            float4 y[4];
+            float x[4];
+            int sg = 0;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                const bool on = r != 0;
+                sg = on ? __ffs(r) - 1 : sg;
+                x[z] = __shfl_sync(0xffffffffu, fk, sg);
+                if (!on) x[z] = 0.f;
+                y[z] = lds4(seg_slot(sg) + (head * PS + d) * 4);
+                if (!on) y[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+                r &= r - 1;
+            }
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                o.x = fmaf(x[z], y[z].x, o.x); o.y = fmaf(x[z], y[z].y, o.y); o.z = fmaf(x[z], y[z].z, o.z); o.w = fmaf(x[z], y[z].w, o.w);
+            }
         }
         return o;
     };
