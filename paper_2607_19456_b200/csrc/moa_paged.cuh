@@ -1172,46 +1172,58 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         if (!s_done[i]) continue;
         const int lead = i ? lead_of[1] : lead_of[0], c_first = i ? first[1] : first[0], c_last = i ? last[1] : last[0];
         const int slot0 = s_seg_lo[lead] == split_at(total, c_first, active) ? 0 : 1;      // a CTA's slot 0: the unit that its range begins in
+        float top[HPW], sum[HPW], x[HPW];
+        float4 o[HPW], oc[HPW];
+#pragma unroll
+        for (int k = 0; k < HPW; ++k) { top[k] = -INFINITY; sum[k] = 0.f; o[k] = oc[k] = make_float4(0.f, 0.f, 0.f, 0.f); }
 #pragma unroll 1
-        for (int head = warp; head < G; head += W) {
-            float top = -INFINITY, sum = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f), oc = o;
-#pragma unroll 1
-            for (int c = c_first; c <= c_last; c += 32) {  // 32 partials' factors at once, one to a lane
-                const int n = min(32, c_last - c + 1);
-                const float *p = a.ws + ((size_t)(c + min(lane, n - 1)) * 2 + (c + lane > c_first ? 0 : slot0)) * C::SLOT + head * PS;
-                float2 ml = __ldcg(reinterpret_cast<const float2 *>(p + D));
-                constexpr int B = 8;                       // rows under way at once, the first beside the factors
-                float4 y[B];
-                auto fetch = [&](int z0) {
+        for (int c = c_first; c <= c_last; c += 32) {      // 32 partials' factors at once, one to a lane
+            const int n = min(32, c_last - c + 1);
+            auto part = [&](int z, int k) {                // partial of CTA c + z for this warp's head k
+                return a.ws + ((size_t)(c + z) * 2 + (c + z > c_first ? 0 : slot0)) * C::SLOT + min(warp + k * W, G - 1) * PS;
+            };
+            constexpr int B = 8;                           // rows of a head under way at once, the first beside the factors
+            float4 y[HPW][B];
+            float2 ml[HPW];
+            auto fetch = [&](int z0) {
+#pragma unroll
+                for (int k = 0; k < HPW; ++k)
 #pragma unroll
                     for (int z = 0; z < B; ++z)
-                        if (z0 + z < n) y[z] = __ldcg(reinterpret_cast<const float4 *>(
-                            a.ws + ((size_t)(c + z0 + z) * 2 + (c + z0 + z > c_first ? 0 : slot0)) * C::SLOT + head * PS + d));
-                };
-                fetch(0);
-                if (lane >= n) ml = make_float2(-INFINITY, 0.f);
-                float top_new = fmaxf(top, ml.x);
+                        if (z0 + z < n) y[k][z] = __ldcg(reinterpret_cast<const float4 *>(part(z0 + z, k) + d));
+            };
+#pragma unroll
+            for (int k = 0; k < HPW; ++k) ml[k] = __ldcg(reinterpret_cast<const float2 *>(part(min(lane, n - 1), k) + D));
+            fetch(0);
+#pragma unroll
+            for (int k = 0; k < HPW; ++k) {
+                if (lane >= n) ml[k] = make_float2(-INFINITY, 0.f);
+                float top_new = fmaxf(top[k], ml[k].x);
 #pragma unroll
                 for (int off = 1; off < 32; off <<= 1) top_new = fmaxf(top_new, __shfl_xor_sync(0xffffffffu, top_new, off));
-                const float keep = exp2_diff(top, top_new), x = exp2_diff(ml.x, top_new);
-                float add = x * ml.y;
+                const float keep = exp2_diff(top[k], top_new);
+                x[k] = exp2_diff(ml[k].x, top_new);
+                float add = x[k] * ml[k].y;
 #pragma unroll
                 for (int off = 1; off < 32; off <<= 1) add += __shfl_xor_sync(0xffffffffu, add, off);
-                sum = fmaf(sum, keep, add);
-                o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
-                oc.x *= keep; oc.y *= keep; oc.z *= keep; oc.w *= keep;
-                top = top_new;
+                sum[k] = fmaf(sum[k], keep, add);
+                o[k].x *= keep; o[k].y *= keep; o[k].z *= keep; o[k].w *= keep;
+                oc[k].x *= keep; oc[k].y *= keep; oc[k].z *= keep; oc[k].w *= keep;
+                top[k] = top_new;
+            }
 #pragma unroll 1
-                for (int z0 = 0; z0 < n; z0 += B) {
-                    if (z0 > 0) fetch(z0);
+            for (int z0 = 0; z0 < n; z0 += B) {
+                if (z0 > 0) fetch(z0);
+#pragma unroll
+                for (int k = 0; k < HPW; ++k)
 #pragma unroll
                     for (int z = 0; z < B; ++z)
-                        if (z0 + z < n) comp_fma4(o, oc, y[z], __shfl_sync(0xffffffffu, x, z0 + z));
-                }
+                        if (z0 + z < n) comp_fma4(o[k], oc[k], y[k][z], __shfl_sync(0xffffffffu, x[k], z0 + z));
             }
-            emit(s_seg_b[lead], s_seg_vh[lead], head, o, sum);
         }
+#pragma unroll
+        for (int k = 0; k < HPW; ++k)
+            if (warp + k * W < G) emit(s_seg_b[lead], s_seg_vh[lead], warp + k * W, o[k], sum[k]);
     }
 }
 
