@@ -243,10 +243,9 @@ __device__ __forceinline__ void chunk_place(int r, int c, uint32_t &kd, uint32_t
 
 // Copies of one tile whose rows may lie in several pages, end behind the sequence (zero-filled), or
 // have pages that do not exist (zero-filled, reported).  A row per lane (lanes 16..31 repeat): `page` is
-// that of row row0 + lane % 16.  Out of line, so that the common case (16 rows of one page) has the
-// loop to itself.  True: a page does not exist.
+// that of row row0 + lane % 16.  True: a page does not exist.
 template <class C>
-__device__ __noinline__ bool copy_ragged_tile(const PagedArgs &a, uint32_t dst, int page, int hs, int row0, int len)
+__device__ __forceinline__ bool copy_ragged_tile(const PagedArgs &a, uint32_t dst, int page, int hs, int row0, int len)
 {
     const int lane = threadIdx.x & 31, row = row0 + (lane & 15);
     long long ko = -1, vo = 0, po = 0;
