@@ -227,7 +227,7 @@ int moa_decode_step_strided(const float *q, float *K, float *V, const float *k_n
  * Formats.  MOA_KV_F32, MOA_KV_BF16, MOA_KV_F16: rows of d elements of that type.
  * MOA_KV_INT4: rows of d codes 0..15, two to a byte, feature 2i in the low half of byte i; strides
  * count codes.  Every row has a pair of fp16 values (scale, least) beside it, at
- * params[((page * h_kv + h) * page_size + r) * 2], and stands for  scale * code + least.
+ * params[((page * h_kv + h) * page_size + r) * 2], and stands for  scale * code + least; scale >= 0.
  *
  * d is 64 or 128, for K and V alike; page_size and num_pages are any positive numbers.  Pools are
  * 16-byte aligned, strides non-negative multiples of 16 bytes (32 codes), at most 2^40, the row
@@ -259,10 +259,12 @@ typedef struct moa_paged_cache {
  *       cache's own for 16 and 32 bits, MOA_BF16 or MOA_F16 for MOA_KV_INT4.
  *   token_strides: HOST array of four element counts {q, k, v, q_out} between consecutive tokens (the heads of
  *       a token are dense: slices of one projection's output are taken as they are), or NULL: dense.
- *   h_q may be 0: then q and q_out are not touched (and may be NULL).  q_out may be q, with the same stride.
+ *   h_q is a multiple of h_kv.  It may be 0: then q and q_out are not touched (and may be NULL).  q_out may be q,
+ *       with the same stride.
  *   token_start: device int32[batch + 1], token_start[0] = 0, ascending: tokens [token_start[b],
  *       token_start[b+1]) belong to sequence b; tokens behind token_start[batch] are left alone
- *       (a padded batch).  NULL: token t is the one new token of sequence t (tokens == batch).
+ *       (a padded batch).  NULL: token t is the one new token of sequence t (tokens == batch), and a
+ *       length of 0 means that there is none.
  *   seq_lens: device int32[batch], the lengths WITH the new rows (what moa_paged_decode_attn is
  *       then given): sequence b's token i of n lands in row seq_lens[b] - n + i, its position.
  *   page_table: device int32[batch][max_pages].  Entries of pages that a call has no rows in are

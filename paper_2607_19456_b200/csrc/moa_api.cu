@@ -1008,7 +1008,7 @@ static int paged_decode_impl(const moa_paged_cache *c, const void *q, void *out,
     }
     a.table = page_table; a.max_pages = max_pages; a.seq_lens = seq_lens;
     const long long cap = (long long)max_pages * c->page_size;
-    a.len_max = cap < 0x7fffffffLL - 16 ? (int)cap : 0x7fffffff - 16;
+    a.len_max = cap < 0x7fffffffLL - 64 ? (int)cap : 0x7fffffff - 64;      // (row numbers of the last stage stay ints)
     a.q = q; a.out = out; a.q_sb = q_stride; a.dtype = dtype;
     a.batch = batch; a.h_q = h_q; a.h_stored = c->h_kv;
     a.share = (g + heads - 1) / heads;

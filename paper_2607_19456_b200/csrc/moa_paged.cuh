@@ -54,7 +54,7 @@ struct PagedArgs {
     const int32_t *table;            // [batch, max_pages]
     int max_pages;
     const int32_t *seq_lens;         // [batch]
-    int len_max;                     // min(max_pages * page_size, INT_MAX)
+    int len_max;                     // min(max_pages * page_size, INT_MAX - 64)
     const void *q;
     void *out;
     long long q_sb;                  // elements between the queries of consecutive sequences

@@ -42,9 +42,6 @@ struct PagedIoArgs {
     int n_out;
 };
 
-template <int FMT> struct PagedElem { using type = uint16_t; };
-template <> struct PagedElem<MOA_KV_F32> { using type = float; };
-
 // Eight consecutive elements of a row as floats, and back.
 template <int DT>
 __device__ __forceinline__ void load8(float (&x)[8], const void *p)
@@ -203,6 +200,7 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
         pos = (long long)__ldg(a.seq_lens + b) - ((long long)next - tok);
     } else {
         pos = (long long)__ldg(a.seq_lens + b) - 1;
+        if (pos == -1) return;                             // a padded batch: no token
     }
     const int pi = pos < 0 ? 0 : a.page_shift >= 0 ? (int)pos >> a.page_shift : (int)pos / a.page_size;
     int status = 0, off = 0;

@@ -95,6 +95,25 @@ def test_one_token_each_without_starts_and_in_place(fmt, in_place):
         assert all(np.array_equal(raw(p.pools[n]), raw(pools[n])) for n in "kv") and moa.moa_device_status() == 0
 
 
+@pytest.mark.parametrize("fmt", FORMATS, ids=lambda f: NAMES[f])
+def test_a_padded_batch_of_single_tokens(fmt):
+    """Length 0 and no token starts: that token is left alone, without a status, and the attention gives zeros for it."""
+    rng = np.random.default_rng(67 + fmt)
+    p = Paged(rng, fmt, [9, 0, 40], 1, 128, 16)
+    dtype = dtype_of(fmt)
+    wide, (q, k, v), (qf, kf, vf) = tensors(rng, 3, 2, 1, 128, dtype)
+    table = rope_table(64, 128)
+    live = [0, 2]
+    pools, params, want_q = expected(p, [(0, 8), (2, 39)], kf[live], vf[live], qf[live], table, 128, 0, dtype)
+    q_out = torch.full((3, 2, 128), 9.0, dtype=TYPES[dtype], device="cuda")
+    st = wide.shape[1]
+    moa.moa_paged_append(p.cache, q, k, v, q_out, dtype, (st, st, st, 256), 3, 2, 3, None, p.lens_dev, p.table, p.max_pages,
+                         torch.from_numpy(table).cuda(), 64, 128, 0)
+    assert np.array_equal(raw(q_out[live]), raw(want_q)) and bool((q_out[1] == 9).all())
+    assert all(np.array_equal(raw(p.pools[n]), raw(pools[n])) for n in "kv")
+    assert bool((attend(p, q_out, dtype, 0.1)[1] == 0).all()) and moa.moa_device_status() == 0
+
+
 def test_many_tokens_and_no_queries():
     rng = np.random.default_rng(11)
     for fmt in FORMATS:
