@@ -910,7 +910,8 @@ static int page_shift_of(int page_size)
 
 // Query heads of one pass over a unit's rows: 8, or 16 for the larger groups of the 16- and 4-bit
 // formats (fp32 keeps its query in 64 registers per 8 heads, so it takes 8 at a time and reads the
-// rows of a larger group again, from L2).
+// rows of a larger group again, from L2).  4 bits, 16 heads: 135 us in one pass of 32 x 60001..131072 rows, 158 in
+// two passes (at a quarter of that, where the joining of 16 heads counts, 60 and 54).
 static int paged_heads(int format, int g) { return format != MOA_KV_F32 && g > 8 ? 16 : 8; }
 
 static int paged_grid(const DeviceState &s)
@@ -944,6 +945,13 @@ static cudaError_t launch_paged_cfg(const PagedArgs &a, int grid, cudaStream_t s
     return cudaGetLastError();
 }
 
+// Warps, ring stages and tiles per stage by format, row length and heads, as measured (us; d = 128: bf16 on 32 x 512..2048
+// rows, 4 bits on 64 x 1024..8192, both 32/8 heads, fp32 on 16 x 1000..4096; d = 64: fp16 on 47 x 0..4999, 24/4 heads):
+//   16 bits, d = 128: 8 warps, 2 stages 39; 10 warps, 2 stages 40; 7 warps, 3 stages 44
+//   16 bits, d = 64:  12 warps, 2 stages of two tiles 35; 8 warps, 4 stages of one tile 45; 16 warps, 2 of one 36
+//   fp32,    d = 128: 6 warps 69; 5 warps 76 (7 do not fit)
+//   4 bits:           12 warps of 168 registers 77; 16 of 128 82; 10 of 204 89; 12 with a third stage 81
+// 16 heads: 8 warps, whose 255 registers hold two column tiles (4 bits, 8 x 60001..131072 rows: 60; 10 warps 78).
 template <int D>
 static cudaError_t launch_paged(int format, int heads, const PagedArgs &a, int grid, cudaStream_t st)
 {
@@ -1100,7 +1108,8 @@ static int paged_append_impl(const moa_paged_cache *c, const void *q, const void
     a.tokens = tokens; a.h_q = h_q; a.token_start = token_start;
     a.cos_sin = cos_sin; a.rope_rows = rope_rows; a.rot = rot_dim; a.pairs = rope_style == MOA_ROPE_PAIRS;
     // Heads of one run: 4 share the search for the token's sequence and page and its cosines and sines
-    // where there are rows enough to fill the GPU that way, one where there are not.
+    // where there are rows enough to fill the GPU that way, one where there are not (7.9k tokens of 48 heads in bf16:
+    // 38.5 us with runs of 4, 38.8 with 8, 42.7 with 2).
     const long long fill = (long long)dev->sm_count * 1024 / (c->d / 16);
     a.run = rows >= 4 * fill ? 4 : rows >= 2 * fill ? 2 : 1;
     a.q_runs = (h_q + a.run - 1) / a.run;
