@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoa.so")
@@ -25,8 +26,9 @@ F32, BF16, F16 = 0, 1, 2                               # element types of tensor
 KV_F32, KV_BF16, KV_F16, KV_INT4 = 0, 1, 2, 3          # formats of a paged cache
 ROPE_HALVES, ROPE_PAIRS = 0, 1
 
-_Strides4 = C.c_longlong * 4
+_strides4 = struct.Struct("4q").pack                    # four long longs (as bytes, a quarter of a ctypes array's time)
 _lib = None
+_current_stream = None
 
 
 class PagedCache(C.Structure):
@@ -117,8 +119,12 @@ def _ptr(x):
 
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        global _current_stream
+        if _current_stream is None:
+            import torch
+            device, raw = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+            _current_stream = lambda: raw(device())
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -241,18 +247,21 @@ def moa_paged_append(cache, q, k, v, q_out, dtype, token_strides, tokens, h_q, b
     if token_strides is not None:
         if len(token_strides) != 4:
             raise ValueError("token strides are (q, k, v, q_out) element counts")
-        token_strides = _Strides4(*token_strides)
-    _check(lib().moa_paged_append(cache, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), dtype, token_strides, tokens, h_q,
-                                  batch, _ptr(token_start), _ptr(seq_lens), _ptr(page_table), max_pages,
-                                  _ptr(cos_sin), rope_rows, rot_dim, rope_style, _stream(stream)),
-           "moa_paged_append")
+        token_strides = _strides4(*token_strides)
+    code = (_lib or lib()).moa_paged_append(cache, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), dtype, token_strides, tokens,
+                                            h_q, batch, _ptr(token_start), _ptr(seq_lens), _ptr(page_table), max_pages,
+                                            _ptr(cos_sin), rope_rows, rot_dim, rope_style, _stream(stream))
+    if code != OK:
+        raise MoaError(code, "moa_paged_append")
 
 
 def moa_paged_decode_attn(cache, q, out, dtype, q_stride, batch, h_q, seq_lens, page_table, max_pages, scale,
                           workspace, workspace_bytes, stream=None):
-    _check(lib().moa_paged_decode_attn(cache, _ptr(q), _ptr(out), dtype, q_stride, batch, h_q, _ptr(seq_lens),
-                                       _ptr(page_table), max_pages, scale, _ptr(workspace), workspace_bytes,
-                                       _stream(stream)), "moa_paged_decode_attn")
+    code = (_lib or lib()).moa_paged_decode_attn(cache, _ptr(q), _ptr(out), dtype, q_stride, batch, h_q, _ptr(seq_lens),
+                                                 _ptr(page_table), max_pages, scale, _ptr(workspace), workspace_bytes,
+                                                 _stream(stream))
+    if code != OK:
+        raise MoaError(code, "moa_paged_decode_attn")
 
 
 def moa_paged_workspace_bytes(batch, h_q, h_kv, d) -> int:
@@ -262,8 +271,10 @@ def moa_paged_workspace_bytes(batch, h_q, h_kv, d) -> int:
 def moa_paged_gather(cache, k_out, v_out, dtype, batch, n_out, row_start, seq_lens, page_table, max_pages,
                      stream=None):
     """Rows [row_start[b], seq_lens[b]) of every sequence into k_out, v_out [batch, h_kv, n_out, d]."""
-    _check(lib().moa_paged_gather(cache, _ptr(k_out), _ptr(v_out), dtype, batch, n_out, _ptr(row_start),
-                                  _ptr(seq_lens), _ptr(page_table), max_pages, _stream(stream)), "moa_paged_gather")
+    code = (_lib or lib()).moa_paged_gather(cache, _ptr(k_out), _ptr(v_out), dtype, batch, n_out, _ptr(row_start),
+                                            _ptr(seq_lens), _ptr(page_table), max_pages, _stream(stream))
+    if code != OK:
+        raise MoaError(code, "moa_paged_gather")
 
 
 def moa_decode_attn_host(q, K, V, out, batch, h_q, h_kv, n, d_k, d_v, scale):
