@@ -70,3 +70,22 @@ def test_calls_of_different_kinds_back_to_back():
         for p, q, o in zip(caches, qs, outs):
             close(p, q, o, 0.1)
     assert moa.moa_device_status() == 0
+
+
+@pytest.mark.parametrize("batch", [1, 5, 200])
+@pytest.mark.parametrize("fmt", range(4), ids=lambda f: NAMES[f])
+def test_nothing_but_empty_sequences(fmt, batch):
+    p = Paged(np.random.default_rng(batch), fmt, [0] * batch, 2, 64, 16)
+    dtype = dtype_of(fmt)
+    out = attend(p, torch.ones((batch, 4, 64), dtype=TYPES[dtype], device="cuda"), dtype, 0.1)
+    assert bool((out == 0).all()) and moa.moa_device_status() == 0
+
+
+@pytest.mark.parametrize("fmt", range(4), ids=lambda f: NAMES[f])
+def test_one_kv_head_for_128_query_heads(fmt):
+    rng = np.random.default_rng(97 + fmt)
+    p = Paged(rng, fmt, [1000, 7], 1, 128, 16)
+    dtype = dtype_of(fmt, moa.F16)
+    q = torch.from_numpy(rng.standard_normal((2, 128, 128)).astype(np.float32)).cuda().to(TYPES[dtype])
+    close(p, q, attend(p, q, dtype, 0.09), 0.09)
+    assert moa.moa_device_status() == 0
