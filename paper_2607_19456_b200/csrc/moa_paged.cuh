@@ -20,7 +20,9 @@
 // Number formats of the products:
 //  - bf16, fp16: the stored values are the A operand; q is the B operand as it is (the scale is
 //    applied to the fp32 score).  The probabilities are split into two 16-bit terms, p = hi + lo,
-//    so that their rounding (2^-9 for bf16) does not add to the one rounding of the output.
+//    so that their rounding (2^-9 for bf16) does not add to the one rounding of the output.  fp16 ends at
+//    2^-24, so there p is taken 2^11 times as large (2^15 at most): what many light rows lose beside a heavy one
+//    is 2^-36 of the heavy one's weight each (2^-25 with p as it is: 4096 rows 17 nats lower were lost whole).
 //  - fp32: both operands split into two tf32 terms, three products (hi*hi, hi*lo, lo*hi), short chains.
 //  - 4 bits: a code c in 0..15 is used as the fp16 bit pattern c, the subnormal c * 2^-24: unpacking
 //    is one AND for two codes (another for the codes four bits up, which come out 16 times as large);
@@ -89,6 +91,10 @@ struct PagedCfg {
     static constexpr int SLOT = G * PS;                    // floats of a unit's partial
     static constexpr int KSTEPS = FMT == MOA_KV_F32 ? D / 8 : D / 16;
     static constexpr int QREGS = FMT == MOA_KV_F32 ? 4 : 2;    // B registers per k-step (fp32: two terms)
+    // How far (log2) a score may pass the reference maximum before that moves, and what the probabilities are taken
+    // larger by: weights held in fp16 reach 2^15.  (4 bits have the factor in PagedState::inv.)
+    static constexpr float AHEAD = FMT == MOA_KV_F16 || FMT == MOA_KV_INT4 ? 4.0f : 8.0f;
+    static constexpr float SHIFT = FMT == MOA_KV_F16 ? 11.0f : 0.0f;
     static constexpr size_t OFF_FIRST = (size_t)W * S * STAGE;
     static constexpr size_t OFF_PREF = OFF_FIRST + sizeof(float) * (size_t)W * SLOT;
     static constexpr size_t SMEM_BYTES = OFF_PREF + sizeof(long long) * THREADS;
@@ -279,9 +285,10 @@ __device__ __forceinline__ bool copy_ragged_tile(const PagedArgs &a, uint32_t ds
 template <class C>
 struct PagedState {
     float acc[C::NT][C::MT][4];
-    float m[C::NT][2], msub[C::NT][2], l[C::NT][2];        // heads 8n + 2t and 8n + 2t + 1; msub: m, or 0 while m is -inf
+    // Heads 8n + 2t and 8n + 2t + 1.  msub: m - SHIFT, what probabilities and sums are relative to, or 0 while m is -inf
+    float m[C::NT][2], msub[C::NT][2], l[C::NT][2];
     float om[C::NT][2];                                    // 4 bits: sum of p * (least + 8 scale)
-    float ref, inv;                                        // 4 bits: power of two, at least every row's scale so far; 128 / ref
+    float ref, inv;                                        // 4 bits: power of two, at least every row's scale so far; 2048 / ref
 };
 
 // n * i / of, in 32 bits where that suffices.
@@ -642,7 +649,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                 for (int e = 0; e < 2; ++e) { s.m[n][e] = -INFINITY; s.msub[n][e] = 0.f; s.l[n][e] = 0.f; s.om[n][e] = 0.f; }
             }
             s.ref = 5.9604644775390625e-8f;                // 2^-24, fp16's least positive value
-            s.inv = 2147483648.0f;
+            s.inv = 34359738368.0f;
         };
 
         // ---- one tile: scores, probabilities, weighted sum ----------------------------------
@@ -744,8 +751,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                             if (16 * tt + g + 8 >= nr) x[tt][n][2 + e] = -INFINITY;
                         }
             }
-            // The reference maximum moves only when a score exceeds it by more than 8 (a factor of
-            // 256, far inside the range of every format used here): rarely after the first tiles.
+            // The reference maximum moves only when a score exceeds it by more than 8 (a factor of 256; 4, a factor
+            // of 16, where weights are fp16): rarely after the first tiles.
             float top[NT][2], vtop = 0.f;
             bool up = false;
 #pragma unroll
@@ -755,7 +762,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     top[n][e] = fmaxf(x[0][n][e], x[0][n][2 + e]);
 #pragma unroll
                     for (int tt = 1; tt < TT; ++tt) top[n][e] = fmaxf(top[n][e], fmaxf(x[tt][n][e], x[tt][n][2 + e]));
-                    up |= top[n][e] > s.m[n][e] + 8.0f;
+                    up |= top[n][e] > s.m[n][e] + C::AHEAD;
                 }
             if constexpr (Q4) {
 #pragma unroll
@@ -771,9 +778,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
                         for (int off = 4; off < 32; off <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
                         const float m_new = fmaxf(s.m[n][e], most);
-                        const float alpha = exp2_diff(s.m[n][e], m_new);
+                        const float sub_new = m_new == -INFINITY ? 0.f : m_new - C::SHIFT;
+                        const float alpha = s.m[n][e] == -INFINITY ? 0.f : fast_exp2(s.msub[n][e] - sub_new);
                         s.m[n][e] = m_new;
-                        s.msub[n][e] = m_new == -INFINITY ? 0.f : m_new;
+                        s.msub[n][e] = sub_new;
                         s.l[n][e] *= alpha;
                         if (Q4) s.om[n][e] *= alpha;
 #pragma unroll
@@ -792,7 +800,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) s.acc[n][i][e] *= f;
                         s.ref = r;
-                        s.inv = 128.0f / r;                // exact: weights reach 2^15 at most
+                        s.inv = 2048.0f / r;               // exact: weights reach 2^15 at most
                     }
                 }
             }
@@ -958,10 +966,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     }
                     const int head = 8 * n + 2 * t + e;
                     float f0 = 1.f, f1 = 1.f, add = 0.f;   // of even and of odd features
-                    if (Q4) { f0 = s.ref * 131072.0f; f1 = s.ref * 8192.0f; add = om; }      // 2^24 / 128, and a 16th
+                    if (Q4) { f0 = s.ref * 8192.0f; f1 = s.ref * 512.0f; add = om; }         // 2^24 / 2048, and a 16th
                     long long at = -1;
                     if (dst != nullptr) {
-                        if (g == 0) { dst[head * PS + D] = s.m[n][e]; dst[head * PS + D + 1] = l; }
+                        if (g == 0) { dst[head * PS + D] = s.m[n][e] == -INFINITY ? -INFINITY : s.msub[n][e]; dst[head * PS + D + 1] = l; }
                     } else {
                         const int qh = paged_query_head(a, cc.b, cc.h, head);
                         if (qh >= 0) at = ((long long)cc.b * a.h_q + qh) * D;
