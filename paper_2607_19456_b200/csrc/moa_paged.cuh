@@ -809,18 +809,24 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                 for (int n = 0; n < NT; ++n) s.l[n][0] = s.l[n][1] = __int_as_float(0x7fffffff);
             }
             uint32_t wt[TT][NT][2];                        // 4 bits: weights p * s as B operand
+            uint32_t hi[TT][NT][2], lo[TT][NT][2];         // 16 bits: weights p in two terms as B operand
+            float ls[NT][2];                               // 16 and 32 bits: the lane's probabilities of the stage, added up before they join
+                                                           // the unit's (4 bits: one by one, 78 us instead of 79 on 64 x 1024..8192 rows)
 #pragma unroll
             for (int tt = 0; tt < TT; ++tt) {
                 const uint32_t sv = st + tt * C::TILE + C::KB;
                 const unsigned char *svp = smem + (sv - smem_u);
                 float p[NT][4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < NT; ++n) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[n][e] = fast_exp2(x[tt][n][e] - s.msub[n][e & 1]);
-                        s.l[n][e & 1] += p[n][e];
+                    for (int e = 0; e < 4; ++e) p[n][e] = fast_exp2(x[tt][n][e] - s.msub[n][e & 1]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (Q4) s.l[n][e] = (s.l[n][e] + p[n][e]) + p[n][2 + e];
+                        else ls[n][e] = tt == 0 ? p[n][e] + p[n][2 + e] : ls[n][e] + (p[n][e] + p[n][2 + e]);
                     }
+                }
                 if constexpr (F32) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -858,27 +864,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                         }
                     }
                 } else if constexpr (!Q4) {
-                    uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const uint32_t r = pack16<BF>(p[n][2 * h], p[n][2 * h + 1]);
                             const float2 f = unpack16<BF>(r);
-                            hi[n][h] = movmatrix_trans(r);
-                            lo[n][h] = movmatrix_trans(pack16<BF>(p[n][2 * h] - f.x, p[n][2 * h + 1] - f.y));
+                            hi[tt][n][h] = movmatrix_trans(r);
+                            lo[tt][n][h] = movmatrix_trans(pack16<BF>(p[n][2 * h] - f.x, p[n][2 * h + 1] - f.y));
                         }
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        uint32_t r[4];
-                        const int row = (lane & 7) + ((lane >> 4) << 3);
-                        ldsm4t(r, sv + row * C::ROWB + (((2 * i + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            mma_16x8x16<BF>(s.acc[n][i], r[0], r[1], r[2], r[3], lo[n][0], lo[n][1]);
-                            mma_16x8x16<BF>(s.acc[n][i], r[0], r[1], r[2], r[3], hi[n][0], hi[n][1]);
-                        }
-                    }
                 } else {
                     const float s0 = vpar[tt][0].x * s.inv, s1 = vpar[tt][1].x * s.inv;
                     const float mid0 = fmaf(8.f, vpar[tt][0].x, vpar[tt][0].y), mid1 = fmaf(8.f, vpar[tt][1].x, vpar[tt][1].y);
@@ -889,6 +883,45 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
                         for (int e = 0; e < 2; ++e) s.om[n][e] = fmaf(p[n][e], mid0, fmaf(p[n][2 + e], mid1, s.om[n][e]));
                     }
+                }
+            }
+            if constexpr (!Q4) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) s.l[n][e] += ls[n][e];
+            }
+            // A stage's sum joins the unit's, in fp32.
+            auto add_sum = [&](float (&to)[4], const float (&sum)[4]) {
+#pragma unroll
+                for (int z = 0; z < 4; z += 2) {
+                    const uint64_t y = add2(pack2(__float_as_uint(to[z]), __float_as_uint(to[z + 1])),
+                                            pack2(__float_as_uint(sum[z]), __float_as_uint(sum[z + 1])));
+                    uint32_t y0, y1;
+                    unpack2(y, y0, y1);
+                    to[z] = __uint_as_float(y0);
+                    to[z + 1] = __uint_as_float(y1);
+                }
+            };
+            if constexpr (!F32 && !Q4) {
+                // Weighted sum of the stage's rows, from zero, then added to the unit's in fp32: the MMA's accumulation
+                // cuts off instead of rounding, and in one chain over 131072 rows of one sign that took 7e-4 off the sum.
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    float sum[NT][4] = {};
+#pragma unroll
+                    for (int tt = 0; tt < TT; ++tt) {
+                        uint32_t r[4];
+                        const int row = (lane & 7) + ((lane >> 4) << 3);
+                        ldsm4t(r, st + tt * C::TILE + C::KB + row * C::ROWB + (((2 * i + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma_16x8x16<BF>(sum[n], r[0], r[1], r[2], r[3], lo[tt][n][0], lo[tt][n][1]);
+                            mma_16x8x16<BF>(sum[n], r[0], r[1], r[2], r[3], hi[tt][n][0], hi[tt][n][1]);
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) add_sum(s.acc[n][i], sum[n]);
                 }
             }
             if constexpr (Q4) {
@@ -936,16 +969,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                             }
                             const int to = 4 * j + 2 * i + e;
 #pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int z = 0; z < 4; z += 2) {
-                                    const uint64_t x = add2(pack2(__float_as_uint(s.acc[n][to][z]), __float_as_uint(s.acc[n][to][z + 1])),
-                                                            pack2(__float_as_uint(sum[n][z]), __float_as_uint(sum[n][z + 1])));
-                                    uint32_t x0, x1;
-                                    unpack2(x, x0, x1);
-                                    s.acc[n][to][z] = __uint_as_float(x0);
-                                    s.acc[n][to][z + 1] = __uint_as_float(x1);
-                                }
+                            for (int n = 0; n < NT; ++n) add_sum(s.acc[n][to], sum[n]);
                         }
                 }
             }

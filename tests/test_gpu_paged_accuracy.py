@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 import paper_2607_19456_b200 as moa
-from paged_util import NAMES, TYPES, Paged, attend, attend64, dtype_of
+from paged_util import NAMES, TYPES, Paged, attend, attend64, dtype_of, workspace
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -57,3 +57,39 @@ def test_many_light_rows_beside_a_heavy_one(fmt, dtype, d, nats):
     tol = want * (rel + torch.finfo(out.dtype).eps / 2) + n * 2.0 ** -35 + 2.0 ** -25
     off = np.abs(out.double().cpu().numpy() - want)
     assert np.all(off <= tol), (float(off.max()), float((off / tol).max()))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("fmt", [moa.KV_F32, moa.KV_BF16, moa.KV_F16, moa.KV_INT4], ids=lambda f: NAMES[f])
+def test_long_sums_of_one_sign(fmt, d):
+    """131072 rows of positive values and nearly even weights in one warp's sums: no bias but that of fp32 additions.
+    All sequences name the same few pages again and again."""
+    rng = np.random.default_rng(5)
+    n, page, pages, batch = 131072, 64, 3, 12
+    dtype = dtype_of(fmt, moa.F16)
+    k = rng.uniform(-1, 1, (1, page * pages, d)).astype(np.float32)
+    v = rng.uniform(1, 2, (1, page * pages, d)).astype(np.float32)
+    p = Paged(rng, fmt, [page * pages], 1, d, page, k=[k], v=[v])
+    own = p.table_host[0, :pages]
+    order = own[rng.integers(0, pages, (batch, n // page))].astype(np.int32)
+    lens = torch.full((batch,), n, dtype=torch.int32, device="cuda")
+    q = one_feature(batch, 2, d, dtype)
+    out = torch.empty((batch, 2, d), dtype=TYPES[dtype], device="cuda")
+    ws, size = workspace(batch, 2, 1, d)
+    with one_cta():
+        moa.moa_paged_decode_attn(p.cache, q, out, dtype, 0, batch, 2, lens, torch.from_numpy(order).cuda(), n // page, 0.5, ws, size)
+    assert moa.moa_device_status() == 0
+    got = out.double().cpu().numpy()
+    for b in range(batch):
+        w = np.exp(0.5 * p.values["k"][order[b], 0, :, 0].reshape(-1))
+        want = (w / w.sum()) @ p.values["v"][order[b], 0].reshape(-1, d)
+        # The rows repeat, so the roundings of a sum's additions may repeat too and all have one sign: N additions of equal parts, each
+        # off by half a unit in the last place of the sum so far, are off by N * 2^-25 of the whole sum.  N is the stages of 16 rows
+        # (32 for rows of 64 in 16 bits and for 4 bits): 2^13 in the weighted sum and as many in the sum of probabilities, 2^-11
+        # in all, 2^-12 for stages of 32; in 4 bits the sum of probabilities goes row by row (2^14 additions in a lane, 2^-11) and
+        # the weights have one rounding (2^-12 of either sign, 192 different rows of a span of less than 1: 2^-14).  Products and sums within a stage 2^-16.
+        stage = 32 if fmt == moa.KV_INT4 or (d == 64 and fmt in (moa.KV_BF16, moa.KV_F16)) else 16
+        rel = (2 if fmt != moa.KV_INT4 else 5) * (n // stage) * 2.0 ** -25 + 2.0 ** -16 + (2.0 ** -14 if fmt == moa.KV_INT4 else 0)
+        tol = np.abs(want) * (torch.finfo(out.dtype).eps / 2 + rel)
+        off = np.abs(got[b] - want)
+        assert np.all(off <= tol), (b, float((off / want).max()), float((off / tol).max()))
