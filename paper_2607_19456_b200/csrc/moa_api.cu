@@ -952,10 +952,11 @@ static cudaError_t launch_paged_cfg(const PagedArgs &a, int grid, cudaStream_t s
 //   fp32,    d = 128: 6 warps 69; 5 warps 76 (7 do not fit)
 //   4 bits:           12 warps of 168 registers 77; 16 of 128 82; 10 of 204 89; 12 with a third stage 81
 // 16 heads: 8 warps, whose 255 registers hold two column tiles (4 bits, 8 x 60001..131072 rows: 60; 10 warps 78).
+// 4 bits with fp16 outputs: weights in two terms (64 x 1024..8192 rows 92, in one 78; 8 x 60001..131072 66, in one 57).
 template <int D>
 static cudaError_t launch_paged(int format, int heads, const PagedArgs &a, int grid, cudaStream_t st)
 {
-    constexpr bool wide = D == 128;        //                                                      NT  W   S  TT
+    constexpr bool wide = D == 128;        //                                                      NT  W   S  TT  terms
     switch (format) {
     case MOA_KV_F32: return launch_paged_cfg<PagedCfg<MOA_KV_F32, D, 1, wide ? 6 : 8, 2, 1>>(a, grid, st);
     case MOA_KV_BF16:
@@ -965,6 +966,10 @@ static cudaError_t launch_paged(int format, int heads, const PagedArgs &a, int g
         if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 1, wide ? 8 : 12, 2, wide ? 1 : 2>>(a, grid, st);
         return launch_paged_cfg<PagedCfg<MOA_KV_F16, D, 2, 8, wide ? 2 : 4, 1>>(a, grid, st);
     default:
+        if (a.dtype == MOA_F16) {
+            if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 12, 2, 2, 2>>(a, grid, st);
+            return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 8, wide ? 3 : 4, 2, 2>>(a, grid, st);
+        }
         if (heads == 8) return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 1, 12, 2, 2>>(a, grid, st);
         return launch_paged_cfg<PagedCfg<MOA_KV_INT4, D, 2, 8, wide ? 3 : 4, 2>>(a, grid, st);
     }

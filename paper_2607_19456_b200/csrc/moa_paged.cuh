@@ -30,7 +30,9 @@
 //    The score of a row is scale * (s * <q, c> + m * sum(q)) with the row's (s, m); in the weighted
 //    sum the weight of a row is p * s, and sum(p * (m + 8 s)) is kept beside it.  q is brought to fp16 by a
 //    power of two per head (exact but for terms 2^-38 of the largest); the weights are brought into
-//    fp16's range by a power of two that follows the largest s seen.
+//    fp16's range by a power of two that follows the largest s seen.  For fp16 outputs they are split into two terms, as
+//    above (one rounding of 2^-12 each made the outputs 1.45 times as far off as their own rounding does); for bf16
+//    outputs one term is an eighth of the output's rounding and does not show (1.67e-3 against 1.66e-3 in the 2-norm).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -73,9 +75,10 @@ struct PagedArgs {
 
 // W warps, S ring stages of TT tiles of 16 rows (K and V) each.  The ring and the slots of the first cut unit
 // share the 227 KB of an SM; the slot of the last cut unit is the ring itself, empty by then.
-template <int FMT_, int D_, int NT_, int W_, int S_, int TT_>
+// TERMS: fp16 terms that a weight of a 4-bit row is held in: two for fp16 outputs, one for bf16.
+template <int FMT_, int D_, int NT_, int W_, int S_, int TT_, int TERMS_ = 1>
 struct PagedCfg {
-    static constexpr int FMT = FMT_, D = D_, NT = NT_, W = W_, S = S_, TT = TT_;
+    static constexpr int FMT = FMT_, D = D_, NT = NT_, W = W_, S = S_, TT = TT_, TERMS = TERMS_;
     static constexpr int THREADS = W * 32, R = 16 * TT;    // rows of a stage
     static constexpr int ROWB = FMT == MOA_KV_F32 ? 4 * D : FMT == MOA_KV_INT4 ? D / 2 : 2 * D;   // bytes of a row
     static constexpr int CPR = ROWB / 16;                  // 16-byte chunks of a row
@@ -808,7 +811,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
                 for (int n = 0; n < NT; ++n) s.l[n][0] = s.l[n][1] = __int_as_float(0x7fffffff);
             }
-            uint32_t wt[TT][NT][2];                        // 4 bits: weights p * s as B operand
+            uint32_t wt[TT][NT][2], wl[TT][NT][2];         // 4 bits: weights p * s as B operand, and their second terms
             uint32_t hi[TT][NT][2], lo[TT][NT][2];         // 16 bits: weights p in two terms as B operand
             float ls[NT][2];                               // 16 and 32 bits: the lane's probabilities of the stage, added up before they join
                                                            // the unit's (4 bits: one by one, 78 us instead of 79 on 64 x 1024..8192 rows)
@@ -878,8 +881,16 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     const float mid0 = fmaf(8.f, vpar[tt][0].x, vpar[tt][0].y), mid1 = fmaf(8.f, vpar[tt][1].x, vpar[tt][1].y);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        wt[tt][n][0] = movmatrix_trans(pack16<false>(p[n][0] * s0, p[n][1] * s0));
-                        wt[tt][n][1] = movmatrix_trans(pack16<false>(p[n][2] * s1, p[n][3] * s1));
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float w0 = p[n][2 * h] * (h ? s1 : s0), w1 = p[n][2 * h + 1] * (h ? s1 : s0);
+                            const uint32_t r = pack16<false>(w0, w1);
+                            wt[tt][n][h] = movmatrix_trans(r);
+                            if constexpr (C::TERMS == 2) {
+                                const float2 f = unpack16<false>(r);
+                                wl[tt][n][h] = movmatrix_trans(pack16<false>(w0 - f.x, w1 - f.y));
+                            }
+                        }
 #pragma unroll
                         for (int e = 0; e < 2; ++e) s.om[n][e] = fmaf(p[n][e], mid0, fmaf(p[n][2 + e], mid1, s.om[n][e]));
                     }
@@ -927,8 +938,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
             if constexpr (Q4) {
                 // Weighted sum of the stage's codes, from zero, then added to the unit's in fp32.  The sums are of c - 8:
                 // with codes from 0 they would carry 7.5 steps of every row, which over 1e5 rows are 500 times
-                // the result, and the rounding of the accumulation and of the weights would act on them (7.4e-4 off the
-                // definition at 131072 rows with fp16 outputs, whose own rounding is 2.0e-4; this way 3.0e-4).
+                // the result, and the rounding of the accumulation and of the weights would act on them (fp16 outputs at
+                // 131072 rows, whose own rounding is 2.1e-4, are 2.4e-4 off the definition; with weights of one term 3.0e-4,
+                // and with codes from 0 as well 7.4e-4).
                 // What is to be taken off, 8 * sum of the rounded weights, comes as a product of its own with a
                 // constant operand, which the sums start from.  Low features of a byte: its low code; the rows of
                 // the high ones hold c0 + 16 c1 (so 136 comes off), taken apart at the end of the unit.
@@ -938,8 +950,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
 #pragma unroll
                     for (int e = 0; e < 4; ++e) off[n][e] = 0.f;
 #pragma unroll
-                    for (int tt = 0; tt < TT; ++tt)
+                    for (int tt = 0; tt < TT; ++tt) {
+                        if (C::TERMS == 2) mma_16x8x16<false>(off[n], 0x80088008u, 0x80888088u, 0x80088008u, 0x80888088u, wl[tt][n][0], wl[tt][n][1]);
                         mma_16x8x16<false>(off[n], 0x80088008u, 0x80888088u, 0x80088008u, 0x80888088u, wt[tt][n][0], wt[tt][n][1]);
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {
@@ -964,8 +978,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                                 const uint32_t a1 = e ? __byte_perm(r[tt][2 * i], 0u, 0x4341) : r[tt][2 * i] & 0x00ff00ffu;
                                 const uint32_t a3 = e ? __byte_perm(r[tt][2 * i + 1], 0u, 0x4341) : r[tt][2 * i + 1] & 0x00ff00ffu;
 #pragma unroll
-                                for (int n = 0; n < NT; ++n)
+                                for (int n = 0; n < NT; ++n) {
+                                    if (C::TERMS == 2) mma_16x8x16<false>(sum[n], a1 & 0x000f000fu, a1, a3 & 0x000f000fu, a3, wl[tt][n][0], wl[tt][n][1]);
                                     mma_16x8x16<false>(sum[n], a1 & 0x000f000fu, a1, a3 & 0x000f000fu, a3, wt[tt][n][0], wt[tt][n][1]);
+                                }
                             }
                             const int to = 4 * j + 2 * i + e;
 #pragma unroll

@@ -93,3 +93,36 @@ def test_long_sums_of_one_sign(fmt, d):
         tol = np.abs(want) * (torch.finfo(out.dtype).eps / 2 + rel)
         off = np.abs(got[b] - want)
         assert np.all(off <= tol), (b, float((off / want).max()), float((off / tol).max()))
+
+
+def rowwise64(p, b, q0, scale, terms):
+    """Definition and bound of sequence b (one kv head, one-feature queries of size q0) on a 4-bit cache: weights in fp16 in `terms` terms,
+    relative to each row's own span, and what fp16's least positive value takes off each of them."""
+    k, v = p.rows("k", b)[0], p.rows("v", b)[0]
+    s = scale * q0 * k[:, 0]
+    w = np.exp(s - s.max())
+    w /= w.sum()
+    span, top = v.max(-1) - v.min(-1), np.abs(v).max(-1)
+    # scores: four roundings of parts below 2^5 in log2, twice 2^-17; probabilities and their sums 2^-16; a stage's codes in the
+    # MMA's accumulation 2^-18 of eight steps each
+    bound = (w * (top * 2.0 ** -15 + span * (2.0 ** -12 if terms == 1 else 2.0 ** -18))).sum() + len(w) * 2.0 ** -32 * span.max() / 15
+    return w @ v, bound
+
+
+@pytest.mark.parametrize("n", [2, 3, 7, 40])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("h_q", [4, 16])
+def test_few_rows_in_4_bits(n, d, h_q):
+    """fp16 outputs of a 4-bit cache are rounded once: the weights of a few heavy rows do not add a rounding of their own."""
+    rng = np.random.default_rng(n + d)
+    batch = 24
+    v = [rng.standard_normal((1, n, d)) for _ in range(batch)]
+    k = [np.clip(rng.standard_normal((1, n, d)), -2, 2) for _ in range(batch)]
+    p = Paged(rng, moa.KV_INT4, [n] * batch, 1, d, 16, k=k, v=v)
+    q = one_feature(batch, h_q, d, moa.F16)
+    out = attend(p, q, moa.F16, 0.7).double().cpu().numpy()
+    for b in range(batch):
+        want, bound = rowwise64(p, b, 1.0, 0.7, 2)
+        tol = bound + np.abs(want) * 2.0 ** -11 + 2.0 ** -25
+        off = np.abs(out[b] - want)
+        assert np.all(off <= tol), (b, float(off.max()), float((off / tol).max()))
