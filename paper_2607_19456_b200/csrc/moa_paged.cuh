@@ -29,7 +29,8 @@
 //    V's bytes are used whole, c0 + 16 c1, beside c0 alone: four instructions for eight codes.
 //    The score of a row is scale * (s * <q, c> + m * sum(q)) with the row's (s, m); in the weighted
 //    sum the weight of a row is p * s, and sum(p * (m + 8 s)) is kept beside it.  q is brought to fp16 by a
-//    power of two per head (exact but for terms 2^-38 of the largest); the weights are brought into
+//    power of two per head that puts its largest value at 2^13, whatever bf16 value that is (what is rounded off is 2^-38
+//    of the largest value, 2^-34 in the features of the high codes, which take q / 16); the weights are brought into
 //    fp16's range by a power of two that follows the largest s seen.  For fp16 outputs they are split into two terms, as
 //    above (one rounding of 2^-12 each made the outputs 1.45 times as far off as their own rounding does); for bf16
 //    outputs one term is an eighth of the output's rounding and does not show (1.67e-3 against 1.66e-3 in the 2-norm).
@@ -609,7 +610,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     for (int i = 0; i < D / 32; ++i)
                         raw[i] = qh >= 0 ? *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + base + t * (D / 4) + 8 * i)
                                          : make_uint4(0u, 0u, 0u, 0u);
-                    float most = 0.f, sum = 0.f;
+                    float most = 0.f;
                     auto pair = [&](uint32_t r) { return dtype == MOA_BF16 ? unpack16<true>(r) : unpack16<false>(r); };
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i)
@@ -617,17 +618,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                         for (int e = 0; e < 4; ++e) {
                             const float2 f = pair(reinterpret_cast<const uint32_t *>(&raw[i])[e]);
                             most = fmaxf(most, fmaxf(fabsf(f.x), fabsf(f.y)));
-                            sum += f.x + f.y;
                         }
 #pragma unroll
-                    for (int off = 1; off < 4; off <<= 1) {
-                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
-                        sum += __shfl_xor_sync(0xffffffffu, sum, off);
-                    }
-                    // largest magnitude into [2^13, 2^14)
+                    for (int off = 1; off < 4; off <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+                    // largest magnitude into [2^13, 2^14), from 2^127 down to 2^-113; below, times 2^126
                     int e = 13 - ((int)((__float_as_uint(most) >> 23) & 255u) - 127);
-                    e = e > 100 ? 100 : e < -100 ? -100 : e;
+                    e = e > 126 ? 126 : e < -114 ? -114 : e;
                     const float up = __uint_as_float((uint32_t)(127 + e) << 23), up16 = up * 0.0625f;
+                    float sum = 0.f;                       // of q times that power, which overflows where the score does, not before
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) {     // word i: features 8i.. of the lane's; pairs (0,4) (1,5), then (2,6) (3,7)
                         const float2 f01 = pair(raw[i].x), f23 = pair(raw[i].y), f45 = pair(raw[i].z), f67 = pair(raw[i].w);
@@ -635,9 +633,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                         qf[n][2 * i][1] = pack16<false>(f01.y * up16, f45.y * up16);
                         qf[n][2 * i + 1][0] = pack16<false>(f23.x * up, f67.x * up);
                         qf[n][2 * i + 1][1] = pack16<false>(f23.y * up16, f67.y * up16);
+                        sum += fmaf(f01.x, up, f01.y * up) + fmaf(f23.x, up, f23.y * up) + (fmaf(f45.x, up, f45.y * up) + fmaf(f67.x, up, f67.y * up));
                     }
-                    const float down = __uint_as_float((uint32_t)(127 - e) << 23) * 16777216.0f * a.qscale;
-                    sum *= a.qscale;
+#pragma unroll
+                    for (int off = 1; off < 4; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                    const float down = __uint_as_float((uint32_t)(127 - e) << 23) * a.qscale;
+                    sum *= down;
 #pragma unroll
                     for (int e2 = 0; e2 < 2; ++e2) {       // of heads 8n + 2t + e2: held by lanes with g = 2t + e2
                         fa[n][e2] = __shfl_sync(0xffffffffu, down, (2 * t + e2) * 4);
@@ -722,6 +723,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     }
                     const __half2 *par = reinterpret_cast<const __half2 *>(skp + 2 * C::KB);
                     const float2 k0 = __half22float2(par[g]), k1 = __half22float2(par[g + 8]);
+                    const float ks0 = k0.x * 16777216.0f, ks1 = k1.x * 16777216.0f;        // codes are c * 2^-24
                     vpar[tt][0] = __half22float2(par[16 + g]);
                     vpar[tt][1] = __half22float2(par[24 + g]);
                     float c[NT][4] = {};
@@ -738,8 +740,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            x[tt][n][e] = fmaf(k0.x, c[n][e] * fa[n][e], k0.y * fm[n][e]);
-                            x[tt][n][2 + e] = fmaf(k1.x, c[n][2 + e] * fa[n][e], k1.y * fm[n][e]);
+                            x[tt][n][e] = fmaf(ks0, c[n][e] * fa[n][e], k0.y * fm[n][e]);
+                            x[tt][n][2 + e] = fmaf(ks1, c[n][2 + e] * fa[n][e], k1.y * fm[n][e]);
                         }
                 }
             }

@@ -126,3 +126,23 @@ def test_few_rows_in_4_bits(n, d, h_q):
         tol = bound + np.abs(want) * 2.0 ** -11 + 2.0 ** -25
         off = np.abs(out[b] - want)
         assert np.all(off <= tol), (b, float(off.max()), float((off / tol).max()))
+
+
+@pytest.mark.parametrize("size", [1e-38, 2.0 ** 115, 2.0 ** 116, 1e36, 3.3e38])
+def test_queries_at_the_ends_of_bf16(size):
+    """4 bits: a query's largest value is brought to 2^13 whatever it is; the product of queries and scale is an ordinary one."""
+    rng = np.random.default_rng(31)
+    d = 128
+    p = Paged(rng, moa.KV_INT4, [90, 5, 300], 1, d, 16)
+    q = rng.uniform(-1, 1, (3, 3, d))
+    q[:, :, 7] = [1, -1, 0.9]
+    qd = (torch.from_numpy(q) * size).cuda().bfloat16()
+    scale = float(np.float32(0.25 / size))
+    out = attend(p, qd, moa.BF16, scale)
+    want, bound = attend64(qd.double().cpu().numpy(), p, scale)
+    # scale * log2(e) among fp32's subnormals (below 2^-126) has a rounding of 2^-150 of its own: twice that, relative to the scale, of scores of
+    # 300 at most, acting on weights
+    extra = 300 * 2.0 ** -149 / scale * np.abs(p.values["v"][np.isfinite(p.values["v"])]).max()
+    off = np.abs(out.double().cpu().numpy() - want)
+    tol = bound + extra + np.abs(want) * 2.0 ** -8 + 2.0 ** -25
+    assert np.all(off <= tol), (float(off.max()), float((off / tol).max()))
