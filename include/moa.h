@@ -298,7 +298,7 @@ int moa_paged_append(const moa_paged_cache *cache, const void *q, const void *k,
  * [0, seq_lens[b]), with the head grouping of section 6.
  *   q [batch, h_q, d], `q_stride` elements between sequences (a multiple of 16 bytes; 0: h_q * d);
  *   out [batch, h_q, d], dense.  Both of type `dtype`: the cache's own for 16 and 32 bits, MOA_BF16
- *   or MOA_F16 for MOA_KV_INT4.  16-byte aligned.
+ *   or MOA_F16 for MOA_KV_INT4.  16-byte aligned.  `scale` is below 2^127 in size.
  * Scores, softmax and sums are fp32; out is rounded once.  (MOA_KV_INT4 with MOA_BF16: the weight of each row is
  * rounded to fp16 on the way, 2^-12 of it, an eighth of bf16's own rounding.)  seq_lens and page_table are read on the
  * device at execution time.  A sequence of length 0 (a padded batch) gets zeros.  A length below 0

@@ -980,7 +980,7 @@ static int paged_decode_impl(const moa_paged_cache *c, const void *q, void *out,
                              float scale, void *ws, size_t ws_bytes, cudaStream_t st)
 {
     if (!c || !q || !out || !seq_lens || !page_table) return MOA_ERR_INVALID;
-    if (batch < 1 || h_q < 1 || max_pages < 1 || !isfinite(scale) || q_stride < 0) return MOA_ERR_INVALID;
+    if (batch < 1 || h_q < 1 || max_pages < 1 || !isfinite(scale * kLog2e) || q_stride < 0) return MOA_ERR_INVALID;
     PagedArgs a = {};
     long long ks[3], vs[3];
     int rc = check_paged(c, ks, vs, false);
