@@ -72,7 +72,9 @@ __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity)
 // while this one is still running (its CTAs take the SMs that this kernel's CTAs leave).
 // launch_dependents allows that; grid_dependency_wait blocks until the previous kernel in
 // the stream has completed and its writes are visible, and is placed before the first read
-// of anything that kernel may have written.  Both are no-ops for an ordinary launch.
+// of anything that kernel may have written.  Such reads are plain loads: one through the
+// read-only path promises data that stays as it is while the kernel lives, and is bound to no
+// order.  Both are no-ops for an ordinary launch.
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -511,12 +511,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
         auto fetch_pages = [&]() {
             if (row0 < fast_end) {
 #pragma unroll
-                for (int tt = 0; tt < TT; ++tt) page[tt] = __ldg(trow + page_index(a, row0 + 16 * tt));
+                for (int tt = 0; tt < TT; ++tt) page[tt] = trow[page_index(a, row0 + 16 * tt)];
             } else {
 #pragma unroll
                 for (int tt = 0; tt < TT; ++tt) {
                     const int row = row0 + 16 * tt + (lane & 15);
-                    page[tt] = row < lc.len ? __ldg(trow + page_index(a, row)) : -1;
+                    page[tt] = row < lc.len ? trow[page_index(a, row)] : -1;
                 }
             }
         };

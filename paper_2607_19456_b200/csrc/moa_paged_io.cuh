@@ -192,14 +192,14 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
         int lo = 0, hi = a.batch;                          // last b with token_start[b] <= tok
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (__ldg(a.token_start + mid) <= tok) lo = mid; else hi = mid;
+            if (a.token_start[mid] <= tok) lo = mid; else hi = mid;
         }
         b = lo;
-        const int first = __ldg(a.token_start + b), next = __ldg(a.token_start + b + 1);
+        const int first = a.token_start[b], next = a.token_start[b + 1];
         if (first > tok || tok >= next) return;            // behind the last sequence: left as it is
-        pos = (long long)__ldg(a.seq_lens + b) - ((long long)next - tok);
+        pos = (long long)a.seq_lens[b] - ((long long)next - tok);
     } else {
-        pos = (long long)__ldg(a.seq_lens + b) - 1;
+        pos = (long long)a.seq_lens[b] - 1;
         if (pos == -1) return;                             // a padded batch: no token
     }
     const int pi = pos < 0 ? 0 : a.page_shift >= 0 ? (int)pos >> a.page_shift : (int)pos / a.page_size;
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
     long long page = 0;
     if (pos < 0 || pi >= a.max_pages || (TURN != kTurnNone && pos >= a.rope_rows)) status = MOA_STATUS_APPEND_RANGE;
     else {
-        page = __ldg(a.table + (long long)b * a.max_pages + pi);
+        page = a.table[(long long)b * a.max_pages + pi];
         off = (int)pos - pi * a.page_size;
         if (page < 0 || page >= a.num_pages) status = MOA_STATUS_PAGE_RANGE;
     }
@@ -224,8 +224,8 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const bool in = turns && (TURN == kTurnChunks || 8 * part + i < half);
-            cs[i] = in ? __ldg(row + 8 * part + i) : 1.f;
-            sn[i] = in ? __ldg(row + half + 8 * part + i) : 0.f;
+            cs[i] = in ? row[8 * part + i] : 1.f;
+            sn[i] = in ? row[half + 8 * part + i] : 0.f;
         }
     }
     unsigned char *dst = kind == 0 ? static_cast<unsigned char *>(a.q_out) + tok * a.o_st * ES
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
                     const int d = 16 * part + i, pair = d < half ? d : d - half;
                     if (d < rot) {
                         float x = load_as_float(src, pair, DT), y = load_as_float(src, pair + half, DT);
-                        turn(x, y, __ldg(row + pair), __ldg(row + half + pair));
+                        turn(x, y, row[pair], row[half + pair]);
                         (i < 8 ? lo[i] : hi[i - 8]) = d < half ? x : y;
                     }
                 }
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(256) paged_gather_kernel(const __grid_constant
     const unsigned slab = blockIdx.x / chunks;
     const int i0 = (int)(blockIdx.x - slab * chunks) * kGatherRows;
     const int b = (int)(slab / a.h_kv), h = (int)(slab - (unsigned)b * a.h_kv);
-    const int len = __ldg(a.seq_lens + b), from = a.row_start != nullptr ? __ldg(a.row_start + b) : 0;
+    const int len = a.seq_lens[b], from = a.row_start != nullptr ? a.row_start[b] : 0;
     if (from < 0 || len < from || (long long)len - from > a.n_out || len > (long long)a.max_pages * a.page_size) {
         if (i0 == 0 && h == 0 && threadIdx.x == 0) raise_status(MOA_STATUS_SEQLEN_RANGE);
         return;
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(256) paged_gather_kernel(const __grid_constant
         if (i >= len - from) return;                       // (and so are the rows of later passes)
         const int pi = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size;
         const int off = row - pi * a.page_size;
-        const long long page = __ldg(a.table + (long long)b * a.max_pages + pi);
+        const long long page = a.table[(long long)b * a.max_pages + pi];
         if (page < 0 || page >= a.num_pages) {
             if (d == 0) raise_status(MOA_STATUS_PAGE_RANGE);
             continue;
