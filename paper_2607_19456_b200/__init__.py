@@ -122,8 +122,12 @@ def _stream(stream):
         global _current_stream
         if _current_stream is None:
             import torch
-            device, raw = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
-            _current_stream = lambda: raw(device())
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # quick, but not public: it may be gone
+            if raw is not None:
+                device = torch.cuda.current_device
+                _current_stream = lambda: raw(device())
+            else:
+                _current_stream = lambda: torch.cuda.current_stream().cuda_stream
         return _current_stream()
     if isinstance(stream, int):
         return stream
