@@ -305,6 +305,12 @@ int moa_paged_append(const moa_paged_cache *cache, const void *q, const void *k,
  * or above max_pages*page_size sets MOA_STATUS_SEQLEN_RANGE and leaves that item's out untouched; a page number outside
  * [0, num_pages) among a sequence's rows sets MOA_STATUS_PAGE_RANGE, nothing outside the pools
  * is read, and the rows of `out` that depend on it become NaN.
+ * Numbers at the ends.  MOA_KV_F16 and MOA_KV_INT4 hold a row's weight in fp16's range: what is below 2^-36 of the
+ * sequence's heaviest row (4 bits: weight times scale, against that row's weight times the sequence's largest scale) adds nothing
+ * to the weighted sum.  Rows and queries are meant to be finite (fp32: below 2^127 in size).  A value that is not makes NaN
+ * or infinite: in V, its feature (4 bits: every feature) in the heads of its K/V head, NaN also where the definition has an infinity; in
+ * K or q, the heads that the definition makes NaN, and in fp32 and 4 bits also those where it makes the row's weight 0.  Other
+ * features, heads and sequences are what they are without it.
  * `workspace`: as for moa_decode_attn_varlen, at least moa_paged_workspace_bytes(...) bytes.
  * One launch; allocates nothing; can be captured into a CUDA graph after one uncaptured call.
  */

@@ -146,3 +146,92 @@ def test_queries_at_the_ends_of_bf16(size):
     off = np.abs(out.double().cpu().numpy() - want)
     tol = bound + extra + np.abs(want) * 2.0 ** -8 + 2.0 ** -25
     assert np.all(off <= tol), (float(off.max()), float((off / tol).max()))
+
+
+@pytest.mark.parametrize("dtype", [moa.BF16, moa.F16])
+@pytest.mark.parametrize("ratio", [2.0 ** 8, 2.0 ** 14])
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+def test_a_light_row_of_large_scale_in_4_bits(where, ratio, dtype):
+    """A row `ratio` times as large as the others, with a weight of e^-60: before, among and after them, it takes nothing from the others'."""
+    rng = np.random.default_rng(11)
+    d, n, batch = 128, 700, 6
+    at = {"first": 0, "middle": 333, "last": n - 1}[where]
+    k, v = [], []
+    for b in range(batch):
+        kb = np.clip(rng.standard_normal((1, n, d)), -2, 2)
+        vb = rng.standard_normal((1, n, d)) * 2.0 ** -6
+        kb[0, at, 0] = -60
+        vb[0, at] *= ratio
+        k.append(kb)
+        v.append(vb)
+    p = Paged(rng, moa.KV_INT4, [n] * batch, 1, d, 16, k=k, v=v)
+    q = one_feature(batch, 5, d, dtype)
+    with one_cta():
+        out = attend(p, q, dtype, 1.0)
+    got = out.double().cpu().numpy()
+    for b in range(batch):
+        want, bound = rowwise64(p, b, 1.0, 1.0, 1)
+        tol = bound + np.abs(want) * torch.finfo(out.dtype).eps / 2 + 2.0 ** -25
+        off = np.abs(got[b] - want)
+        assert np.all(off <= tol), (b, float(off.max()), float((off / tol).max()))
+
+
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("fmt", range(4), ids=lambda f: NAMES[f])
+def test_values_that_are_not_finite_stay_where_they_are(fmt, value):
+    """In V: the feature they stand in (the row, in 4 bits) of the heads of that K/V head is not finite; everything else of the sequence, and
+    the other sequences, are what the definition gives."""
+    rng = np.random.default_rng(43 + fmt)
+    v = [rng.standard_normal((2, 50, 64)) for _ in range(3)]
+    v[1][1, 20, 3] = value
+    p = Paged(rng, fmt, [50] * 3, 2, 64, 16, v=v)
+    dtype = dtype_of(fmt)
+    q = torch.from_numpy(rng.standard_normal((3, 4, 64)).astype(np.float32)).cuda().to(TYPES[dtype])
+    out = attend(p, q, dtype, 0.1).double().cpu().numpy()
+    hit = np.zeros(out.shape, bool)
+    hit[1, 2:, 3] = True
+    if fmt == moa.KV_INT4:
+        hit[1, 2:] = True
+    assert not np.isfinite(out[hit]).any() and np.isfinite(out[~hit]).all()
+    for name in "kv":                                       # (the definition elsewhere: that value counts as 0)
+        p.values[name] = np.where(np.isfinite(p.values[name]), p.values[name], 0)
+    want, bound = attend64(q.double().cpu().numpy(), p, 0.1)
+    if fmt == moa.KV_F32:
+        bound = np.maximum(bound, 5e-6)
+    off = np.abs(out - want)
+    tol = bound + np.abs(want) * torch.finfo(TYPES[dtype]).eps / 2 + 2.0 ** -25
+    assert np.all((off <= tol)[~hit])
+
+
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("fmt", range(4), ids=lambda f: NAMES[f])
+def test_keys_that_are_not_finite_stay_where_they_are(fmt, value):
+    """In K: NaN in the heads of that K/V head that the definition makes NaN; a score of -inf is a weight of 0 in 16 bits and may be NaN
+    elsewhere.  The other head and the other sequences are what the definition gives."""
+    rng = np.random.default_rng(47 + fmt)
+    k = [rng.standard_normal((2, 50, 64)) for _ in range(3)]
+    k[1][1, 20, 3] = value
+    p = Paged(rng, fmt, [50] * 3, 2, 64, 16, k=k)
+    dtype = dtype_of(fmt)
+    q = torch.from_numpy(rng.standard_normal((3, 4, 64)).astype(np.float32)).cuda().to(TYPES[dtype])
+    q[1, 2, 3], q[1, 3, 3] = 0.5, -0.5
+    out = attend(p, q, dtype, 0.1).double().cpu().numpy()
+    nan = [fmt == moa.KV_INT4 or np.isnan(value) or s * value > 0 for s in (0.5, -0.5)]       # of heads 2 and 3
+    check = np.ones(out.shape, bool)
+    for i in (0, 1):
+        if nan[i]:
+            assert np.isnan(out[1, 2 + i]).all()
+        if nan[i] or fmt == moa.KV_F32:
+            check[1, 2 + i] = False
+    if not check[1, 2:].any():                              # (the definition elsewhere: that value counts as 0)
+        p.values["k"] = np.where(np.isfinite(p.values["k"]), p.values["k"], 0)
+    with np.errstate(invalid="ignore"):
+        want, bound = attend64(q.double().cpu().numpy(), p, 0.1)
+    if check[1, 2:].any():                                  # a weight of 0 for row 20: the bound is that of the other rows
+        b = p.table_host[1, 1]
+        p.values["k"][b, 1, 4] = 0
+        bound[1, 2:] = attend64(q.double().cpu().numpy(), p, 0.1)[1][1, 2:]
+    if fmt == moa.KV_F32:
+        bound = np.maximum(bound, 5e-6)
+    tol = bound + np.abs(want) * torch.finfo(TYPES[dtype]).eps / 2 + 2.0 ** -25
+    assert np.all((np.abs(out - want) <= tol)[check])
