@@ -910,8 +910,10 @@ static int page_shift_of(int page_size)
 
 // Query heads of one pass over a unit's rows: 8, or 16 for the larger groups of the 16- and 4-bit
 // formats (fp32 keeps its query in 64 registers per 8 heads, so it takes 8 at a time and reads the
-// rows of a larger group again, from L2).  4 bits, 16 heads: 135 us in one pass of 32 x 60001..131072 rows, 158 in
-// two passes (at a quarter of that, where the joining of 16 heads counts, 60 and 54).
+// rows of a larger group again).  us, 16 heads at a time against 8, the same for groups of 9, 12 and 16:
+//   24 x 60001..131072 rows, one K/V head: bf16 191 and 355, 4 bits 108 and 127 (fp16 outputs 134 and 152); 64 heads 709 and 1317, 374 and 475
+//   8 x 60001..131072 rows:                bf16  81 and 125, 4 bits  57 and  55 (65 and 64)
+//   32 x 512..2048 rows, two K/V heads:    bf16  33 and  29, 4 bits  24 and  20, where the joining of 16 heads by 8 warps counts
 static int paged_heads(int format, int g) { return format != MOA_KV_F32 && g > 8 ? 16 : 8; }
 
 static int paged_grid(const DeviceState &s)

@@ -9,13 +9,15 @@
 //    only the (at most two) units that a range cuts go through shared memory, once, at the end of
 //    the CTA.  Small caches (16 and 4 bits) have units that take a CTA a microsecond or two; a block
 //    barrier for every unit, as the fp32 streaming kernels have, would cost as much again.
-//  - Tiles come through per-lane 16-byte asynchronous copies into a ring of the warp's own: rows of
-//    one page are a few hundred bytes to a few KB, less than a bulk copy needs to be worth its issue
-//    (one per 70 cycles and SM), and a page may end inside a tile.  The page numbers of a tile are
-//    read while the tile before it is issued.
+//  - Tiles come through per-lane 16-byte asynchronous copies into a ring of the warp's own: a page may
+//    end inside a tile, and a bulk copy per tile and operand (an SM retires one per 70 cycles) would bring
+//    4 bits no more than 15 bytes a cycle of the 24 that HBM has.  16 and 32 bits would have enough of them (58
+//    and 117 at rows of 128); there the copies below reach the copy rate too (bf16, 4 x 131072 rows: 286 us
+//    of 287).  The page numbers of a tile are read while the tile before it is issued.
 //  - Both products run on the warp-level MMA with the cached operand as A (16 rows or 16 features),
 //    heads as the 8 columns: S[16 rows x 8 heads] = K Q^T, O^T[16 features x 8 heads] += V^T P^T.
-//    A query group of one head to eight costs the same; what bounds the kernel is the copy.
+//    A query group of one head to eight costs the same.  What bounds the kernel is the copy in 16 and 32 bits,
+//    instruction issue and the ALU in 4 (52 % and 45 % on 64 x 1024..8192 rows).
 //
 // Number formats of the products:
 //  - bf16, fp16: the stored values are the A operand; q is the B operand as it is (the scale is
@@ -1159,7 +1161,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) paged_decode_kernel(const __gri
     };
     // Units cut between CTAs first (the first group, the last, or both): their partials leave and are
     // counted while the whole units are joined.  One release and one count per CTA and cut unit: fences of
-    // several warps of an SM wait for one another (a count per head and warp took 30 us on 16 heads).
+    // several warps of an SM wait for one another.
     int lead_of[2] = {__ffs(leaders) - 1, 31 - __clz(leaders)}, first[2], last[2];
     bool cut[2];
 #pragma unroll
