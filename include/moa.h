@@ -332,6 +332,50 @@ int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int
                      const int32_t *row_start, const int32_t *seq_lens, const int32_t *page_table,
                      int max_pages, void *stream);
 
+/* ==== many new tokens at once =======================================================
+ *
+ * Attention of every token of whole prompts, packed one behind the other (steps I-III of Algorithm 1 for each
+ * query, with the head grouping of section 6):
+ *     s[l] = scale * <q[t,h], k[l,h / (h_q/h_kv)]>,  a = softmax(s),  out[t,h] = sum_l a[l] v[l,h / (h_q/h_kv)]
+ * over the tokens l of t's own sequence: those up to t (`causal` = 1), or all of them (0).
+ *   q [tokens, h_q, d], k, v [tokens, h_kv, d], out [tokens, h_q, d]: all of type `dtype`; d is 64 or 128.
+ *   token_strides: HOST array of four element counts {q, k, v, out} between consecutive tokens (the heads of
+ *       a token are dense: slices of one projection's output are taken as they are), or NULL: dense.
+ *   token_start: device int32[batch + 1], ascending: tokens [token_start[b], token_start[b+1]) are sequence b;
+ *       tokens behind the last sequence are left alone (a padded batch), sequences without tokens are allowed.  NULL:
+ *       batch is 1 and all tokens are its.  A sequence whose tokens are not inside [0, tokens) in ascending order sets
+ *       MOA_STATUS_SEQLEN_RANGE and is left out.
+ * q, k, v, out are 16-byte aligned, token strides multiples of 16 bytes; `scale` is below 2^127 in size.
+ * Scores, softmax statistics and sums are fp32 and out is rounded once; for 16-bit types the weight of each row is
+ * rounded to that type on its way into the weighted sum (fp16: below 2^-36 of the heaviest row's weight it adds nothing).
+ * A value that is not finite makes NaN or infinite: in q, the row; in k, the rows that see it; in v, its feature
+ * in the rows that see it (NaN also where the definition has an infinity).  What a row does not see does not touch it.
+ * `workspace`: device memory, 256-byte aligned, at least moa_prompt_workspace_bytes(...) bytes, contents
+ * undefined on entry and exit; not to be shared by calls that can overlap on the GPU.
+ * One launch; allocates nothing; can be captured into a CUDA graph after one uncaptured call.
+ */
+int moa_prompt_attn(const void *q, const void *k, const void *v, void *out, int dtype, const long long *token_strides,
+                    int tokens, int h_q, int h_kv, int d, int batch, const int32_t *token_start, int causal, float scale,
+                    void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * Attention of chunks of new tokens over a paged cache: the next piece of a prompt, draft tokens to be checked, single
+ * tokens among them.  The new tokens' rows are in the cache already (moa_paged_append, given the same token_start and
+ * seq_lens): token i of sequence b's n attends over rows [0, seq_lens[b] - n + i].
+ *   q [tokens, h_q, d], `q_stride` elements between tokens (a multiple of 16 bytes; 0: h_q * d); out [tokens, h_q, d], dense.
+ *       Both of type `dtype`: the cache's own for 16 and 32 bits, MOA_BF16 or MOA_F16 for MOA_KV_INT4.
+ *   token_start: as above; NULL: token t is the one new token of sequence t (tokens == batch), and a length of 0
+ *       (a padded batch) gives zeros.
+ * A length below the number of new tokens or beyond max_pages*page_size sets MOA_STATUS_SEQLEN_RANGE and leaves
+ * the sequence's out untouched; a page number outside [0, num_pages) among the rows that a sequence's tokens see sets
+ * MOA_STATUS_PAGE_RANGE, nothing outside the pools is read, and the rows of out that depend on it become NaN.
+ * All else (scale, numbers, workspace, launch) as for moa_prompt_attn.
+ */
+int moa_paged_chunk_attn(const moa_paged_cache *cache, const void *q, void *out, int dtype, long long q_stride, int tokens, int h_q,
+                         int batch, const int32_t *token_start, const int32_t *seq_lens, const int32_t *page_table, int max_pages,
+                         float scale, void *workspace, size_t workspace_bytes, void *stream);
+/* Workspace of both calls (0 on invalid dimensions). */
+size_t moa_prompt_workspace_bytes(int tokens, int h_q, int h_kv, int d, int batch);
+
 /*
  * Host-buffer convenience call: q, K, V, out are HOST pointers (pinned memory gives
  * full copy bandwidth).  Copies the inputs to library-owned device staging buffers,
@@ -437,6 +481,7 @@ const char *moa_strerror(int code);
                                   fused step: 17..32) */
 #define MOA_PATH_MMA       4   /* streaming kernel with warp-level MMA, 8 or 16 heads per fetched row (larger groups in
                                   several passes), d_k, d_v in {64,128} */
+#define MOA_PATH_PROMPT    6   /* reported only: moa_prompt_attn, moa_paged_chunk_attn */
 #define MOA_PATH_PAGED     5   /* reported only: the paged calls have one kernel family, never forced */
 int moa_set_option(int option, int value);
 int moa_last_path(void);

@@ -21,7 +21,7 @@ STATUS_APPEND_RANGE, STATUS_SEQLEN_RANGE, STATUS_WAIT_TIMEOUT, STATUS_PAGE_RANGE
 OPT_FORCE_PATH, OPT_NUM_CTAS, OPT_GROUPED_HEADS, OPT_DEPENDENT_LAUNCH, OPT_GROUPED_OPERANDS = 1, 2, 3, 4, 5
 OPT_WAIT_LIMIT, OPT_TEST_SKIP_COPY = 7, 8
 NOALLOC_SCRATCH_BYTES = 4 << 20
-PATH_AUTO, PATH_GENERIC, PATH_STREAM, PATH_GROUPED, PATH_MMA, PATH_PAGED = 0, 1, 2, 3, 4, 5
+PATH_AUTO, PATH_GENERIC, PATH_STREAM, PATH_GROUPED, PATH_MMA, PATH_PAGED, PATH_PROMPT = 0, 1, 2, 3, 4, 5, 6
 F32, BF16, F16 = 0, 1, 2                               # element types of tensors
 KV_F32, KV_BF16, KV_F16, KV_INT4 = 0, 1, 2, 3          # formats of a paged cache
 ROPE_HALVES, ROPE_PAIRS = 0, 1
@@ -88,6 +88,10 @@ def lib():
         L.moa_paged_workspace_bytes.argtypes = [i, i, i, i]
         L.moa_paged_workspace_bytes.restype = sz
         L.moa_paged_gather.argtypes = [pc, p, p, i, i, i, p, p, p, i, p]
+        L.moa_prompt_attn.argtypes = [p, p, p, p, i, p, i, i, i, i, i, p, i, f, p, sz, p]
+        L.moa_paged_chunk_attn.argtypes = [pc, p, p, i, C.c_longlong, i, i, i, p, p, p, i, f, p, sz, p]
+        L.moa_prompt_workspace_bytes.argtypes = [i, i, i, i, i]
+        L.moa_prompt_workspace_bytes.restype = sz
         L.moa_device_status.argtypes = [p, C.POINTER(C.c_int)]
         L.moa_min_bytes.argtypes = [i, i, i, C.c_longlong, i, i]
         L.moa_min_bytes.restype = C.c_longlong
@@ -279,6 +283,39 @@ def moa_paged_gather(cache, k_out, v_out, dtype, batch, n_out, row_start, seq_le
                                             _ptr(seq_lens), _ptr(page_table), max_pages, _stream(stream))
     if code != OK:
         raise MoaError(code, "moa_paged_gather")
+
+
+def _token_strides(st, what):
+    if st is None:
+        return None
+    if len(st) != 4:
+        raise ValueError("token strides are (%s) element counts" % what)
+    return _strides4(*st)
+
+
+def moa_prompt_attn(q, k, v, out, dtype, token_strides, tokens, h_q, h_kv, d, batch, token_start, causal, scale,
+                    workspace, workspace_bytes, stream=None):
+    """Attention over whole prompts packed one behind the other.
+    token_strides: None (dense) or element counts between tokens of (q, k, v, out)."""
+    code = (_lib or lib()).moa_prompt_attn(_ptr(q), _ptr(k), _ptr(v), _ptr(out), dtype,
+                                           _token_strides(token_strides, "q, k, v, out"), tokens, h_q, h_kv, d, batch,
+                                           _ptr(token_start), causal, scale, _ptr(workspace), workspace_bytes, _stream(stream))
+    if code != OK:
+        raise MoaError(code, "moa_prompt_attn")
+
+
+def moa_paged_chunk_attn(cache, q, out, dtype, q_stride, tokens, h_q, batch, token_start, seq_lens, page_table, max_pages,
+                         scale, workspace, workspace_bytes, stream=None):
+    """Attention of each sequence's new tokens, whose rows are in the cache already, over the rows up to their own."""
+    code = (_lib or lib()).moa_paged_chunk_attn(cache, _ptr(q), _ptr(out), dtype, q_stride, tokens, h_q, batch,
+                                                _ptr(token_start), _ptr(seq_lens), _ptr(page_table), max_pages, scale,
+                                                _ptr(workspace), workspace_bytes, _stream(stream))
+    if code != OK:
+        raise MoaError(code, "moa_paged_chunk_attn")
+
+
+def moa_prompt_workspace_bytes(tokens, h_q, h_kv, d, batch) -> int:
+    return int(lib().moa_prompt_workspace_bytes(tokens, h_q, h_kv, d, batch))
 
 
 def moa_decode_attn_host(q, K, V, out, batch, h_q, h_kv, n, d_k, d_v, scale):

@@ -17,6 +17,7 @@
 #include "moa_grouped64.cuh"
 #include "moa_paged.cuh"
 #include "moa_paged_io.cuh"
+#include "moa_prompt.cuh"
 
 namespace moa {
 
@@ -1168,6 +1169,155 @@ static int paged_gather_impl(const moa_paged_cache *c, void *k_out, void *v_out,
     return e == cudaSuccess ? MOA_OK : MOA_ERR_CUDA;
 }
 
+// ---- many new tokens at once ----------------------------------------------------------------
+static int prompt_grid(const DeviceState &s) { return paged_grid(s); }
+// Pieces that a call may cut its units into at most, and the rows that one of them holds.
+static int prompt_slots(int grid) { return 2 * grid; }
+static int prompt_slot_rows(long long rows) { return rows >= 256 ? 256 : (int)((rows + 31) / 32 * 32); }
+static size_t prompt_slot_bytes(int grid, long long rows, int d)
+{
+    return ((size_t)prompt_slots(grid) * prompt_slot_rows(rows) * (d + 2) * sizeof(float) + 255) / 256 * 256;
+}
+static size_t prompt_ticket_bytes(int grid) { return ((size_t)(prompt_slots(grid) + 1) * sizeof(unsigned long long) + 255) / 256 * 256; }
+
+// x / n = x * mul >> sh for 0 <= x < 2^31: mul * n exceeds 2^sh by less than 2^(sh - 31)
+static void quick_division(int n, uint32_t *mul, int *sh)
+{
+    int log2_up = 0;
+    while ((1LL << log2_up) < n) ++log2_up;
+    *sh = 31 + log2_up;
+    *mul = (uint32_t)(((1ULL << *sh) + n - 1) / n);
+}
+
+template <class C>
+static cudaError_t launch_prompt_cfg(const PromptArgs &a, int grid, cudaStream_t st)
+{
+    static bool attr_set[kMaxDevices] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(prompt_attn_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
+    launch_dependent(prompt_attn_kernel<C>, grid, C::THREADS, C::SMEM, st, a);
+    count_launch();
+    return cudaGetLastError();
+}
+
+template <int D>
+static cudaError_t launch_prompt(int format, int dtype, bool paged, const PromptArgs &a, int grid, cudaStream_t st)
+{
+    if (!paged) {
+        if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_BF16, true, D, false>>(a, grid, st);
+        return launch_prompt_cfg<PromptCfg<MOA_KV_F16, false, D, false>>(a, grid, st);
+    }
+    if (format == MOA_KV_INT4) {
+        if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_INT4, true, D, true>>(a, grid, st);
+        return launch_prompt_cfg<PromptCfg<MOA_KV_INT4, false, D, true>>(a, grid, st);
+    }
+    if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_BF16, true, D, true>>(a, grid, st);
+    return launch_prompt_cfg<PromptCfg<MOA_KV_F16, false, D, true>>(a, grid, st);
+}
+
+// What both calls share once their own arguments are in `a`: sizes, scale, workspace, launch.
+static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d, float scale, void *ws, size_t ws_bytes, cudaStream_t st)
+{
+    const long long rows = (long long)a.tokens * a.g;
+    if ((long long)a.tokens * a.h_q > 0x7fffffffLL - 1024 || ((rows + 127) / 128 + a.batch) * a.h_kv >= (1LL << 20)) return MOA_ERR_CAPACITY;
+    if (!ws) return MOA_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return MOA_ERR_ALIGN;
+    DeviceState *dev = nullptr;
+    const int rc = current_device(&dev);
+    if (rc != MOA_OK) return rc;
+    const int grid = prompt_grid(*dev);
+    const size_t slots = prompt_slot_bytes(grid, rows, d);
+    if (ws_bytes < slots + prompt_ticket_bytes(grid)) return MOA_ERR_WORKSPACE;
+    quick_division(a.g, &a.g_mul, &a.g_sh);
+    // A scale of 0 becomes the least positive number: what is masked is -infinity times the scale.
+    a.qscale = fmaxf(fabsf(scale) * kLog2e, 1.4e-45f);
+    a.negate = scale < 0.f;
+    a.slots = static_cast<float *>(ws);
+    a.slot_cap = prompt_slots(grid); a.slot_rows = prompt_slot_rows(rows);
+    a.tickets = reinterpret_cast<unsigned long long *>(static_cast<unsigned char *>(ws) + slots);
+    unsigned long long tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
+    if (tag == 0) tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
+    a.ticket_tag = (tag << 20) | 1ull;
+    const cudaError_t e = d == 128 ? launch_prompt<128>(format, dtype, paged, a, grid, st) : launch_prompt<64>(format, dtype, paged, a, grid, st);
+    if (e != cudaSuccess) return MOA_ERR_CUDA;
+    g_last_path = MOA_PATH_PROMPT;
+    return MOA_OK;
+}
+
+static int prompt_impl(const void *q, const void *k, const void *v, void *out, int dtype, const long long *ts, int tokens, int h_q,
+                       int h_kv, int d, int batch, const int32_t *token_start, int causal, float scale, void *ws, size_t ws_bytes,
+                       cudaStream_t st)
+{
+    if (!q || !k || !v || !out) return MOA_ERR_INVALID;
+    if (tokens < 1 || h_q < 1 || h_kv < 1 || h_q % h_kv != 0 || batch < 1 || d < 1 || !isfinite(scale * kLog2e)) return MOA_ERR_INVALID;
+    if (dtype < MOA_F32 || dtype > MOA_F16 || (causal != 0 && causal != 1) || (!token_start && batch != 1)) return MOA_ERR_INVALID;
+    if (d != 64 && d != 128) return MOA_ERR_UNSUPPORTED;
+    if (dtype == MOA_F32) return MOA_ERR_UNSUPPORTED;
+    const int es = element_bytes(dtype);
+    const long long dense[4] = {(long long)h_q * d, (long long)h_kv * d, (long long)h_kv * d, (long long)h_q * d};
+    long long s[4];
+    bool wide = true;
+    for (int i = 0; i < 4; ++i) {
+        s[i] = ts ? ts[i] : dense[i];
+        if (s[i] < 0 || s[i] > (1LL << 40)) return MOA_ERR_INVALID;
+        if (i == 3 && s[i] < dense[i] && tokens > 1) return MOA_ERR_INVALID;      // rows of out may not overlap
+        if (s[i] * es % 16 != 0) wide = false;
+    }
+    if (!wide || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || (token_start && !aligned(token_start, 4)))
+        return MOA_ERR_ALIGN;
+    PromptArgs a = {};
+    a.q = static_cast<const unsigned char *>(q); a.out = static_cast<unsigned char *>(out);
+    a.k = static_cast<const unsigned char *>(k); a.v = static_cast<const unsigned char *>(v);
+    a.q_st = s[0] * es; a.o_st = s[3] * es;
+    a.k_sr = s[1] * es; a.v_sr = s[2] * es; a.k_sh = a.v_sh = (long long)d * es;
+    a.token_start = token_start;
+    a.tokens = tokens; a.batch = batch; a.h_q = h_q; a.h_kv = h_kv; a.g = h_q / h_kv;
+    a.causal = causal;
+    return prompt_launch(a, dtype, dtype, false, d, scale, ws, ws_bytes, st);
+}
+
+static int paged_chunk_impl(const moa_paged_cache *c, const void *q, void *out, int dtype, long long q_stride, int tokens, int h_q,
+                            int batch, const int32_t *token_start, const int32_t *seq_lens, const int32_t *page_table, int max_pages,
+                            float scale, void *ws, size_t ws_bytes, cudaStream_t st)
+{
+    if (!c || !q || !out || !seq_lens || !page_table) return MOA_ERR_INVALID;
+    if (tokens < 1 || batch < 1 || h_q < 1 || max_pages < 1 || !isfinite(scale * kLog2e) || q_stride < 0) return MOA_ERR_INVALID;
+    if (!token_start && tokens != batch) return MOA_ERR_INVALID;
+    long long ks[3], vs[3];
+    const int rc = check_paged(c, ks, vs, false);
+    if (rc != MOA_OK) return rc;
+    if (h_q % c->h_kv != 0 || dtype < MOA_F32 || dtype > MOA_F16) return MOA_ERR_INVALID;
+    if (!paged_dtype_ok(c->format, dtype)) return MOA_ERR_UNSUPPORTED;
+    if (dtype == MOA_F32) return MOA_ERR_UNSUPPORTED;
+    if (q_stride == 0) q_stride = (long long)h_q * c->d;
+    if (q_stride > (1LL << 40)) return MOA_ERR_INVALID;
+    const int es = element_bytes(dtype);
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(seq_lens, 4) || !aligned(page_table, 4) ||
+        (token_start && !aligned(token_start, 4)) || q_stride * es % 16 != 0)
+        return MOA_ERR_ALIGN;
+    PromptArgs a = {};
+    a.q = static_cast<const unsigned char *>(q); a.out = static_cast<unsigned char *>(out);
+    a.k = static_cast<const unsigned char *>(c->k); a.v = static_cast<const unsigned char *>(c->v);
+    a.kp = static_cast<const uint32_t *>(c->k_params); a.vp = static_cast<const uint32_t *>(c->v_params);
+    a.q_st = q_stride * es; a.o_st = (long long)h_q * c->d * es;
+    a.k_sp = ks[0]; a.k_sh = ks[1]; a.k_sr = ks[2];
+    a.v_sp = vs[0]; a.v_sh = vs[1]; a.v_sr = vs[2];
+    a.num_pages = c->num_pages; a.page_size = c->page_size;
+    quick_division(c->page_size, &a.page_mul, &a.page_sh);
+    a.table = page_table; a.max_pages = max_pages;
+    const long long cap = (long long)max_pages * c->page_size;
+    a.len_max = cap < 0x7fffffffLL - 512 ? (int)cap : 0x7fffffff - 512;      // (row numbers of the last tile stay ints)
+    a.token_start = token_start; a.seq_lens = seq_lens;
+    a.tokens = tokens; a.batch = batch; a.h_q = h_q; a.h_kv = c->h_kv; a.g = h_q / c->h_kv;
+    a.causal = 1;
+    return prompt_launch(a, c->format, dtype, true, c->d, scale, ws, ws_bytes, st);
+}
+
 }  // namespace moa
 
 using namespace moa;
@@ -1488,6 +1638,35 @@ int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int
     Lock lock(g_mu);
     return paged_gather_impl(cache, k_out, v_out, dtype, batch, n_out, row_start, seq_lens, page_table, max_pages,
                              static_cast<cudaStream_t>(stream));
+}
+
+int moa_prompt_attn(const void *q, const void *k, const void *v, void *out, int dtype, const long long *token_strides,
+                    int tokens, int h_q, int h_kv, int d, int batch, const int32_t *token_start, int causal, float scale,
+                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    Lock lock(g_mu);
+    return prompt_impl(q, k, v, out, dtype, token_strides, tokens, h_q, h_kv, d, batch, token_start, causal, scale, workspace,
+                       workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+int moa_paged_chunk_attn(const moa_paged_cache *cache, const void *q, void *out, int dtype, long long q_stride, int tokens, int h_q,
+                         int batch, const int32_t *token_start, const int32_t *seq_lens, const int32_t *page_table, int max_pages,
+                         float scale, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Lock lock(g_mu);
+    return paged_chunk_impl(cache, q, out, dtype, q_stride, tokens, h_q, batch, token_start, seq_lens, page_table, max_pages, scale,
+                            workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+size_t moa_prompt_workspace_bytes(int tokens, int h_q, int h_kv, int d, int batch)
+{
+    Lock lock(g_mu);
+    if (tokens < 1 || h_q < 1 || h_kv < 1 || h_q % h_kv != 0 || (d != 64 && d != 128) || batch < 1) return 0;
+    DeviceState *dev = nullptr;
+    DeviceState plain;
+    plain.sm_count = 256;                  // no device: an upper bound
+    const int grid = prompt_grid(current_device(&dev) == MOA_OK ? *dev : plain);
+    return prompt_slot_bytes(grid, (long long)tokens * (h_q / h_kv), d) + prompt_ticket_bytes(grid);
 }
 
 int moa_decode_attn_host(const float *q, const float *K, const float *V, float *out, int batch,

@@ -1,0 +1,997 @@
+// moa_prompt.cuh -- attention of many new tokens at once: whole prompts packed one behind the other, and chunks of
+// new tokens over a paged cache (16-bit rows, or 4-bit rows with 16-bit queries).
+//
+// For query head h of token i of a sequence of n new tokens behind `past` rows (0 for a prompt), K/V head h / g:
+//     s[l] = scale <q, K[l]>,  out = sum_l 2^(log2e (s[l] - m)) V[l] / sum_l 2^(log2e (s[l] - m)),  l <= past + i
+// (all l of the sequence where a prompt is not causal), in one pass over the rows with a running reference m.
+//
+// Both products run on the tensor core (tcgen05, accumulators in tensor memory).  A UNIT is up to 256 rows of
+// queries -- the g heads of consecutive tokens, which share K and V -- against the rows of one K/V head, 128 keys
+// at a time:
+//   warps 0-3, 4-7   softmax of slot 0 and slot 1, a thread to a query row (a tensor memory lane): scores out, weights in,
+//                    the weighted sum rescaled where the reference moves (it moves when a score passes it by 2^AHEAD, which
+//                    after the first tiles is rare), and the output at the end of the unit
+//   warps 8-11       copies of Q, K and V into swizzled tiles, row by row (a page may end anywhere; 4 bits are unpacked here)
+//   warp 12          issues the products:  P0 V, Q0 K', P1 V, Q1 K'  and so on, so that the softmax of one slot
+//                    runs under the products of the other
+// The two slots hold rows 0..127 and 128..255 of the unit, both against every tile of keys; a unit of at most 128
+// rows has the same rows in both, against the even and the odd tiles, and the slots are joined at its end.
+//
+// A slot's scores and weights share 128 columns of tensor memory (weights of 16 bits in the first 64); products of one
+// thread run in order, so the scores of a slot's next tile overwrite its weights when those are used up, and the
+// arrival of a slot's scores means that its weighted sum is at rest: rescaling needs no barrier of its own.
+//
+// Work is handed out unit by unit (one CTA per SM; the next one's number comes from a counter; what a unit gives does not depend
+// on who takes it).  Where there are few units their keys are cut into pieces; the CTA that delivers a unit's last piece
+// joins them in order.
+#pragma once
+
+#include "moa_grouped64.cuh"
+#include "moa_paged.cuh"
+
+namespace moa {
+
+struct PromptArgs {
+    const unsigned char *q;
+    unsigned char *out;
+    long long q_st, o_st;            // bytes between consecutive tokens
+    const unsigned char *k, *v;      // tensors (heads of a token are dense), or pools
+    const uint32_t *kp, *vp;         // 4-bit rows: (scale, least) pairs
+    long long k_sp, k_sh, k_sr;      // bytes: page (pools), kv head, row
+    long long v_sp, v_sh, v_sr;
+    int num_pages, page_size;
+    uint32_t page_mul;               // row / page_size = row * page_mul >> page_sh, for rows below 2^31
+    int page_sh;
+    const int32_t *table;
+    int max_pages, len_max;
+    const int32_t *token_start;      // [batch + 1]; null: one token each (pools), one sequence (tensors)
+    const int32_t *seq_lens;         // pools: lengths with the new rows
+    int tokens, batch, h_q, h_kv, g;
+    uint32_t g_mul;                  // row / g, as above
+    int g_sh;
+    int causal;
+    float qscale;                    // |scale| * log2(e)
+    int negate;                      // scale < 0
+    float *slots;                    // partial results of pieces, slot_rows * (D + 2) floats each
+    int slot_cap, slot_rows;
+    unsigned long long *tickets;     // slot_cap counters of pieces, then the counter of items handed out
+    unsigned long long ticket_tag;
+};
+
+template <int FMT_, bool BF_, int D_, bool PAGED_>
+struct PromptCfg {
+    static constexpr int FMT = FMT_, D = D_;               // FMT: MOA_KV_INT4, or the 16-bit type
+    static constexpr bool BF = BF_, PAGED = PAGED_, Q4 = FMT == MOA_KV_INT4;
+    static constexpr int THREADS = 512, TILE = 128;
+    static constexpr int HALVES = D / 64;                  // 128-byte column groups of a 16-bit row
+    static constexpr int KV = TILE * D * 2;                // bytes of a tile of K or V in shared memory
+    static constexpr int NST = D == 128 ? 2 : 4;           // stages of K and of V
+    static constexpr int NPAR = 2 * NST;                   // parameters of 4-bit rows: twice as many tiles as stages
+    static constexpr uint32_t OFF_Q = 0;
+    static constexpr uint32_t OFF_K = OFF_Q + 2 * KV;
+    static constexpr uint32_t OFF_V = OFF_K + NST * KV;
+    static constexpr uint32_t OFF_PAR = OFF_V + NST * KV;  // [NPAR][2 (K, V)][128] (scale, least + 8 scale)
+    static constexpr uint32_t OFF_PMAX = OFF_PAR + (Q4 ? NPAR * 2 * 128 * 8 : 0);      // [NPAR][4] largest scales of V
+    static constexpr uint32_t OFF_NF = OFF_PMAX + (Q4 ? NPAR * 16 : 0);                // [2][D] first key with a V that is not finite
+    static constexpr uint32_t OFF_ML = OFF_NF + 2 * D * 4; // [2][128] (m, l) of the slots
+    static constexpr uint32_t OFF_PLAN = OFF_ML + 2 * 128 * 8;
+    static constexpr uint32_t SMEM = OFF_PLAN + 512 * 8 + 1024;      // (1024: alignment of the base)
+    static constexpr float AHEAD = BF && !Q4 ? 8.0f : BF ? 8.0f : 4.0f;
+    static constexpr float SHIFT = BF ? 0.0f : 11.0f;      // weights held in fp16 reach 2^15 (as in the single-query kernel)
+    static constexpr int DEG = BF ? 3 : 4;
+};
+
+struct PromptSeq { int first, n, past, len; };
+
+// Sequence b; n = 0 where it has no new tokens or is refused (bad: its status).
+template <bool PAGED>
+__device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b, int &bad)
+{
+    PromptSeq s;
+    long long first, next;
+    if (a.token_start != nullptr) { first = a.token_start[b]; next = a.token_start[b + 1]; }
+    else if (PAGED) { first = b; next = b + 1; }
+    else { first = 0; next = a.tokens; }
+    bad = 0;
+    if (first < 0 || next < first || next > a.tokens) { bad = MOA_STATUS_SEQLEN_RANGE; first = next = 0; }
+    s.first = (int)first; s.n = (int)(next - first);
+    s.len = PAGED ? a.seq_lens[b] : s.n;
+    s.past = s.len - s.n;
+    if (PAGED && s.n > 0) {
+        const bool none = a.token_start == nullptr && s.len == 0;      // a padded batch: a token that sees nothing
+        if (!none && (s.len < s.n || s.len > a.len_max)) { bad = MOA_STATUS_SEQLEN_RANGE; s.n = 0; }
+    }
+    return s;
+}
+
+__device__ __forceinline__ int div_g(const PromptArgs &a, int r) { return (int)(((unsigned long long)(uint32_t)r * a.g_mul) >> a.g_sh); }
+
+// Keys that row r (token r / g) of a sequence sees.
+__device__ __forceinline__ int prompt_sees(const PromptArgs &a, const PromptSeq &s, int r)
+{
+    if (!a.causal) return s.len;
+    return s.past + div_g(a, r) + 1;
+}
+
+struct PromptItem {
+    int first, past, len;            // the sequence
+    int head;                        // kv head
+    int table_row;                   // sequence number
+    int row0, rows;                  // query rows of the unit: first one, and how many (1..256); 0: there is no further item
+    int t0, e0, e1;                  // tiles of keys: first one, and the ends for slot 0 and slot 1
+    int pair;                        // the slots take the even and the odd tiles of the same rows
+    int least;                       // keys that the unit's first row sees
+    int slot, pieces, slot_step;     // piece 0's slot (-1: one piece), pieces, distance of the pieces' slots
+    int piece;
+};
+
+// ---- how the work is cut ------------------------------------------------------------------
+struct PromptPlan { int rows, step_max, items; };
+
+template <bool PAGED>
+__device__ __forceinline__ void prompt_counts(const PromptArgs &a, const PromptSeq &s, int R, int T, int &tiles, int &pieces)
+{
+    const long long rows = (long long)s.n * a.g;
+    tiles = (int)((rows + R - 1) / R);
+    pieces = 0;
+    if (s.n == 0) return;
+    const int keys = (prompt_sees(a, s, (int)rows - 1) + 127) >> 7;
+    const int steps = rows <= 128 || R == 128 ? (keys + 1) >> 1 : keys;
+    pieces = steps > T ? (steps + T - 1) / T : 1;
+}
+
+__device__ __forceinline__ long long prompt_block_sum(long long v, long long *scratch)
+{
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    long long t = 0;
+    for (int i = 0; i < (int)blockDim.x / 32; ++i) t += scratch[i];
+    return t;
+}
+
+// Every CTA finds the same plan: rows of a unit, the most steps (a tile of keys for 256 rows) that a piece has, and in
+// pref[i] how many (items, slots) the sequences before group i have.
+template <bool PAGED>
+__device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs &a, int2 *pref, long long *scratch, bool report)
+{
+    const int tid = threadIdx.x, nt = blockDim.x;
+    const int gs = (a.batch + nt - 1) / nt;                // sequences of a group: one thread's
+    const int b0 = min(tid * gs, a.batch), b1 = min(b0 + gs, a.batch);
+    long long units = 0, work = 0;
+    int bad;
+    for (int b = b0; b < b1; ++b) {
+        const PromptSeq s = prompt_seq<PAGED>(a, b, bad);
+        if (bad != 0 && report) raise_status(bad);
+        if (s.n == 0) continue;
+        int tiles, pieces;
+        prompt_counts<PAGED>(a, s, 256, 0x7fffffff, tiles, pieces);
+        const long long rows = (long long)s.n * a.g;
+        const int last = (prompt_sees(a, s, (int)rows - 1) + 127) >> 7, front = (prompt_sees(a, s, 0) + 127) >> 7;
+        units += (long long)tiles * a.h_kv;
+        work += rows <= 128 ? (long long)a.h_kv * ((last + 1) >> 1) : (long long)a.h_kv * tiles * (last + front + 1) / 2;
+    }
+    units = prompt_block_sum(units, scratch);
+    work = prompt_block_sum(work, scratch);
+    const int grid = gridDim.x;
+    PromptPlan p;
+    p.rows = units >= 2 * grid || work >= 32LL * grid ? 256 : 128;
+    long long T = (work + grid - 1) / grid;
+    if (T < 6) T = 6;
+    int items, slots;
+    for (;;) {
+        items = slots = 0;
+        long long all = 0;
+        for (int b = b0; b < b1; ++b) {
+            const PromptSeq s = prompt_seq<PAGED>(a, b, bad);
+            int tiles, pieces;
+            prompt_counts<PAGED>(a, s, p.rows, (int)min(T, 0x7fffffffLL), tiles, pieces);
+            const long long c = (long long)tiles * pieces * a.h_kv;
+            if (pieces > 1) { all += c; if (c <= a.slot_cap) slots += (int)c; }
+            items += (int)min(c, 0x7fffffffLL);
+        }
+        if (prompt_block_sum(all, scratch) <= a.slot_cap) break;
+        T += T / 2;
+    }
+    p.step_max = (int)min(T, 0x7fffffffLL);
+    // exclusive prefix over the groups
+    int2 inc = make_int2(items, slots);
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, inc.x, off), y = __shfl_up_sync(0xffffffffu, inc.y, off);
+        if ((tid & 31) >= off) { inc.x += x; inc.y += y; }
+    }
+    int2 *sums = reinterpret_cast<int2 *>(scratch);
+    __syncthreads();
+    if ((tid & 31) == 31) sums[tid >> 5] = inc;
+    __syncthreads();
+    int2 before = make_int2(0, 0), total = make_int2(0, 0);
+    for (int i = 0; i < nt / 32; ++i) {
+        if (i < (tid >> 5)) { before.x += sums[i].x; before.y += sums[i].y; }
+        total.x += sums[i].x;
+    }
+    pref[tid] = make_int2(before.x + inc.x - items, before.y + inc.y - slots);
+    p.items = total.x;
+    __syncthreads();
+    return p;
+}
+
+// Item number `i`.  One thread.
+template <bool PAGED>
+__device__ __forceinline__ void prompt_item(const PromptArgs &a, const PromptPlan &p, const int2 *pref, int nt, int i, PromptItem &it)
+{
+    it.rows = 0;
+    if (i >= p.items) return;
+    int lo = 0, hi = nt;                                   // last group with pref <= i
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (pref[mid].x <= i) lo = mid; else hi = mid;
+    }
+    const int gs = (a.batch + nt - 1) / nt;
+    int at = pref[lo].x, slot = pref[lo].y, bad, tiles = 0, pieces = 0, b = lo * gs;
+    PromptSeq s;
+    for (;; ++b) {
+        if (b >= a.batch) return;                          // (not reached: the plan counted the item)
+        s = prompt_seq<PAGED>(a, b, bad);
+        prompt_counts<PAGED>(a, s, p.rows, p.step_max, tiles, pieces);
+        const int c = tiles * pieces * a.h_kv;
+        if (i < at + c) break;
+        at += c;
+        if (pieces > 1) slot += c;
+    }
+    // inside a sequence: the last tiles of rows, which see most keys, first; heads innermost
+    const int j = i - at, head = j % a.h_kv, k = j / a.h_kv, piece = k % pieces, tile = tiles - 1 - k / pieces;
+    const int all = s.n * a.g;
+    it.first = s.first; it.past = s.past; it.len = s.len; it.head = head; it.table_row = b;
+    it.row0 = tile * p.rows;
+    it.rows = min(p.rows, all - it.row0);
+    it.pair = it.rows <= 128;
+    it.least = prompt_sees(a, s, it.row0);
+    const int end1 = (prompt_sees(a, s, it.row0 + it.rows - 1) + 127) >> 7;
+    const int end0 = it.pair ? end1 : (prompt_sees(a, s, it.row0 + 127) + 127) >> 7;
+    it.t0 = (int)((long long)end1 * piece / pieces);
+    it.e1 = (int)((long long)end1 * (piece + 1) / pieces);
+    it.e0 = min(it.e1, end0);
+    it.piece = piece; it.pieces = pieces;
+    it.slot_step = a.h_kv;
+    it.slot = pieces > 1 ? slot + (k - piece) * a.h_kv + head : -1;
+}
+
+// Steps of slot s of an item.
+__device__ __forceinline__ int prompt_steps(const PromptItem &it, int s)
+{
+    const int n = it.e1 - it.t0;
+    if (it.pair) return s == 0 ? (n + 1) >> 1 : n >> 1;
+    return s == 0 ? max(0, it.e0 - it.t0) : n;
+}
+
+// ---- tensor core --------------------------------------------------------------------------
+namespace tc {
+// Instruction descriptor of kind::f16, fp32 accumulate: A and B bf16 or fp16; bit 13 negates A.
+__host__ __device__ constexpr uint32_t idesc_16(bool bf16, int M, int N, bool b_mn_major)
+{
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) |
+           ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void mma_16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+}  // namespace tc
+
+// Wait of a whole warp: all lanes leave it with the same answer.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+{
+    for (uint32_t it = 0; it < kWaitLimit; ++it) {
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+        if ((it & 15u) == 15u && __any_sync(0xffffffffu, *abort_flag)) return false;
+    }
+    *abort_flag = 1;
+    raise_status(MOA_STATUS_WAIT_TIMEOUT);
+    return false;
+}
+
+__device__ __forceinline__ float max_nan(float x, float y)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pack2f(float lo, float hi) { return pack2(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ float2 unpack2f(uint64_t v)
+{
+    uint32_t lo, hi;
+    unpack2(v, lo, hi);
+    return make_float2(__uint_as_float(lo), __uint_as_float(hi));
+}
+
+// 2^x for two x at once on the FMA units: x = n + f with |f| <= 1/2, a polynomial in f (least relative error over
+// the interval, fitted for this file: 7.5e-5 of degree 3, 2.6e-6 of degree 4), times 2^n as a bit pattern.  x at or
+// below -127 gives 0.  The special function unit makes 16 results a cycle and SM; a tile of 128 x 128 scores would keep it busy
+// exactly as long as the tensor core takes for the tile's two products, so a share of the weights goes this way.
+template <int DEG>
+__device__ __forceinline__ float2 exp2_pair(uint64_t x)
+{
+    const float2 v = unpack2f(x);
+    x = pack2f(fmaxf(v.x, -127.0f), fmaxf(v.y, -127.0f));
+    const uint64_t magic = pack2f(12582912.0f + 127.0f, 12582912.0f + 127.0f);      // low bits: n + 127
+    const uint64_t t = add2(x, magic);
+    const uint64_t f = sub2(x, sub2(t, magic));
+    uint64_t r;
+    if (DEG == 3) {
+        r = fma2(f, pack2f(0.0551716685f, 0.0551716685f), pack2f(0.2426111251f, 0.2426111251f));
+        r = fma2(f, r, pack2f(0.6932609677f, 0.6932609677f));
+        r = fma2(f, r, pack2f(0.9999280572f, 0.9999280572f));
+    } else {
+        r = fma2(f, pack2f(0.0095701022f, 0.0095701022f), pack2f(0.0559178591f, 0.0559178591f));
+        r = fma2(f, r, pack2f(0.2402474433f, 0.2402474433f));
+        r = fma2(f, r, pack2f(0.6931217909f, 0.6931217909f));
+        r = fma2(f, r, pack2f(0.9999992847f, 0.9999992847f));
+    }
+    uint32_t a, b;
+    unpack2(t, a, b);
+    return unpack2f(mul2(r, pack2(a << 23, b << 23)));
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid_constant__ PromptArgs a)
+{
+    constexpr int D = C::D, NST = C::NST, HALVES = C::HALVES;
+    constexpr bool BF = C::BF, Q4 = C::Q4, PAGED = C::PAGED;
+    extern __shared__ unsigned char smem_prompt[];
+    __shared__ __align__(8) uint64_t bars[4 * NST + 8 + 2 + 4 + 4 + C::NPAR];
+    __shared__ PromptItem s_item[2];
+    __shared__ long long s_scratch[16];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort, s_last, s_nf[2];
+    __shared__ float2 s_more[Q4 ? 2 : 1][Q4 ? 128 : 1];      // 4 bits: what joins the slots beside (m, l)
+    const uint32_t base = (smem_u32(smem_prompt) + 1023u) & ~1023u;
+    unsigned char *const smem = smem_prompt + (base - smem_u32(smem_prompt));
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int *abort_flag = &s_abort;
+
+    const uint32_t bar0 = smem_u32(bars);
+    auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+    auto k_full = [&](int i) { return bar(i); };
+    auto k_empty = [&](int i) { return bar(NST + i); };
+    auto v_full = [&](int i) { return bar(2 * NST + i); };
+    auto v_empty = [&](int i) { return bar(3 * NST + i); };
+    auto s_full = [&](int s) { return bar(4 * NST + s); };
+    auto p_full = [&](int s) { return bar(4 * NST + 2 + s); };
+    auto o_full = [&](int s) { return bar(4 * NST + 4 + s); };
+    const uint32_t q_full = bar(4 * NST + 6), q_empty = bar(4 * NST + 7);
+    auto item_full = [&](int i) { return bar(4 * NST + 8 + i); };
+    auto item_empty = [&](int i) { return bar(4 * NST + 10 + i); };
+    const uint32_t joined = bar(4 * NST + 12), parted = bar(4 * NST + 13), delivered = bar(4 * NST + 14), counted = bar(4 * NST + 15);
+    const uint32_t drained = bar(4 * NST + 16);
+    auto par_full = [&](int i) { return bar(4 * NST + 18 + i); };
+
+    if (tid == 0) {
+        for (int i = 0; i < NST; ++i) { mbar_init(k_full(i), 4); mbar_init(k_empty(i), 1); mbar_init(v_full(i), 4); mbar_init(v_empty(i), 1); }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(s_full(s), 1); mbar_init(p_full(s), 4); mbar_init(o_full(s), 1);
+            mbar_init(item_full(s), 1); mbar_init(item_empty(s), 12);
+        }
+        mbar_init(q_full, 4); mbar_init(q_empty, 1);
+        mbar_init(joined, 8); mbar_init(parted, 8); mbar_init(delivered, 8); mbar_init(counted, 1); mbar_init(drained, 1);
+        for (int i = 0; i < C::NPAR; ++i) mbar_init(par_full(i), 4);
+        mbar_fence_init();
+        s_abort = 0;
+    }
+    if (warp == 12) tc::tmem_alloc(smem_u32(&s_tmem), 512);
+    launch_dependents();
+    grid_dependency_wait();
+    int2 *const pref = reinterpret_cast<int2 *>(smem + C::OFF_PLAN);
+    const PromptPlan plan = prompt_plan<PAGED>(a, pref, s_scratch, blockIdx.x == 0);
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = s_tmem;
+    auto t_s = [tmem](int s) -> uint32_t { return tmem + 128u * (uint32_t)s; };
+    auto t_o = [tmem](int s) -> uint32_t { return tmem + 256u + (uint32_t)(s * D); };
+
+    if (warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (warp == 12 && lane == 0) {
+            // ================= products =================
+            const uint32_t sQ = base + C::OFF_Q, sK = base + C::OFF_K, sV = base + C::OFF_V;
+            const uint32_t id_qk = tc::idesc_16(BF, 128, 128, false) | (a.negate ? 1u << 13 : 0u);
+            constexpr uint32_t id_pv = tc::idesc_16(BF, 128, D, true);
+            constexpr uint32_t hiword = 64u | (1u << 14) | (2u << 29);       // 1024 bytes between groups of 8 rows, 128-byte swizzle
+            uint32_t nk = 0, nv = 0, nq = 0, np[2] = {0, 0};
+            bool ok = true;
+            for (uint32_t n = 0; ok; ++n) {
+                if (!wait_suspended(item_full(n & 1), (n >> 1) & 1, abort_flag)) { ok = false; break; }
+                const PromptItem it = s_item[n & 1];
+                if (it.rows == 0) break;
+                const int cnt[2] = {prompt_steps(it, 0), prompt_steps(it, 1)};
+                int left = cnt[0] + cnt[1];
+                if (left > 0) {
+                    auto scores = [&](int s, int i) {
+                        const uint32_t kt = nk + (uint32_t)(it.pair ? 2 * i + s : i), st = kt % NST;
+                        if (!wait_suspended(k_full(st), (kt / NST) & 1, abort_flag)) return false;
+                        tc::fence_after_sync();
+                        const uint32_t qa = sQ + (it.pair ? 0u : (uint32_t)(s * C::KV)), kb = sK + st * C::KV;
+#pragma unroll
+                        for (uint32_t ks = 0; ks < D / 16; ++ks) {
+                            const uint32_t off = (ks / 4) * 16384u + (ks % 4) * 32u;
+                            tc::mma_16_ss(t_s(s), tc::pack64(((qa + off) >> 4) | (1u << 16), hiword), tc::pack64(((kb + off) >> 4) | (1u << 16), hiword), id_qk, ks != 0);
+                        }
+                        tc::mma_commit(s_full(s));
+                        if (it.pair || s == 1) tc::mma_commit(k_empty(st));
+                        if (--left == 0) tc::mma_commit(q_empty);
+                        return true;
+                    };
+                    ok = wait_suspended(q_full, nq & 1, abort_flag);
+                    for (int s = 0; ok && s < 2; ++s) if (cnt[s] > 0) ok = scores(s, 0);
+                    const int steps = max(cnt[0], cnt[1]);
+                    for (int i = 0; ok && i < steps; ++i) {
+                        for (int s = 0; ok && s < 2; ++s) {
+                            if (i >= cnt[s]) continue;
+                            const uint32_t vt = nv + (uint32_t)(it.pair ? 2 * i + s : i), st = vt % NST;
+                            ok = wait_suspended(v_full(st), (vt / NST) & 1, abort_flag) && wait_suspended(p_full(s), np[s] & 1, abort_flag);
+                            if (!ok) break;
+                            ++np[s];
+                            tc::fence_after_sync();
+                            const uint32_t vb = sV + st * C::KV;
+#pragma unroll
+                            for (uint32_t ks = 0; ks < 8; ++ks)
+                                tc::mma_16_ts(t_o(s), t_s(s) + 8u * ks, tc::pack64(((vb + ks * 2048u) >> 4) | (1024u << 16), hiword), id_pv, (i != 0 || ks != 0));
+                            if (it.pair || s == 1) tc::mma_commit(v_empty(st));
+                            if (i + 1 < cnt[s]) ok = scores(s, i + 1);
+                            else tc::mma_commit(o_full(s));
+                        }
+                    }
+                    nk += (uint32_t)(it.e1 - it.t0);
+                    nv += (uint32_t)(it.e1 - it.t0);
+                    ++nq;
+                }
+                tc::mbar_arrive(item_empty(n & 1));
+            }
+            if (!ok) {                                     // leave nothing in flight
+                tc::mma_commit(drained);
+                mbar_wait_bounded(drained, 0);
+            }
+        }
+    } else if (warp >= 8) {
+        // ================= copies =================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        const int w = warp - 8;
+        constexpr int CPR = D / 8, RPI = 32 / CPR;         // 16-byte chunks of a 16-bit row; rows of a warp's copy
+        const int chunk = lane % CPR, rsub = lane / CPR;
+        const uint32_t col = (uint32_t)(chunk >> 3) * 16384u;
+        uint32_t nk = 0, nv = 0, nq = 0;
+        bool ok = true;
+        // Copies under way, oldest first: the barrier that their arrival is told to, and for V whether to look for values that are not finite.
+        uint32_t pend_bar[2];
+        int pend_chk[2], pending = 0;                      // pend_chk: -1, or 2 * tile of keys + set of the item
+        uint32_t pend_at[2];
+        auto dst_of = [&](int r) -> uint32_t { return col + (uint32_t)r * 128u + (uint32_t)(((chunk & 7) ^ (r & 7)) << 4); };
+        auto look = [&](uint32_t at, int tile, int nf_set) {      // own chunks of a tile of V: zero what is not finite, and note where
+            for (int i = 0; i < 32 / RPI; ++i) {
+                const int r = 32 * w + RPI * i + rsub;
+                const uint32_t p = at + dst_of(r);
+                uint32_t u[4];
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(p) : "memory");
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t x = u[e >> 1] >> (16 * (e & 1)), ex = BF ? 0x7f80u : 0x7c00u;
+                    if ((x & ex) == ex) {
+                        any = true;
+                        u[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+                        atomicMin(reinterpret_cast<int *>(smem + C::OFF_NF) + nf_set * D + chunk * 8 + e, tile * 128 + r);
+                        s_nf[nf_set] = 1;
+                    }
+                }
+                if (any) asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+            }
+        };
+        auto retire = [&]() {                              // the oldest has arrived
+            if (pending == 2) cp_wait<1>(); else cp_wait<0>();
+            if (pend_chk[0] >= 0) look(pend_at[0], pend_chk[0] >> 1, pend_chk[0] & 1);
+            tc::fence_async_smem();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(pend_bar[0]);
+            pend_bar[0] = pend_bar[1]; pend_chk[0] = pend_chk[1]; pend_at[0] = pend_at[1];
+            --pending;
+        };
+        auto push = [&](uint32_t b, uint32_t at, int chk) {
+            cp_commit();
+            pend_bar[pending] = b; pend_at[pending] = at; pend_chk[pending] = chk;
+            if (++pending == 2) retire();
+        };
+        auto wait_free = [&](uint32_t b, uint32_t parity) {
+            if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
+            while (pending > 0) retire();                  // what this waits for may need them
+            return wait_warp(b, parity, abort_flag);
+        };
+
+        for (uint32_t n = 0; ok; ++n) {
+            const int set = n & 1;
+            if (w == 0) {
+                if (n >= 2) {
+                    ok = wait_free(item_empty(set), ((n >> 1) - 1) & 1);
+                    if (!ok) break;
+                }
+                if (lane == 0) {
+                    int i = blockIdx.x;
+                    if (n > 0) {
+                        i = 0x7fffffff;
+                        if (plan.items > (int)gridDim.x) {
+                            unsigned long long *word = a.tickets + a.slot_cap;
+                            const unsigned j = ticket_arrive(word, a.ticket_tag);
+                            if (j + 1 == (unsigned)plan.items) *word = 0;          // every CTA has drawn its last number
+                            i = (int)min((unsigned)gridDim.x + j, 0x7fffffffu);
+                        }
+                    }
+                    prompt_item<PAGED>(a, plan, pref, C::THREADS, i, s_item[set]);
+                    s_nf[set] = 0;
+                }
+                for (int f = lane; f < D; f += 32) reinterpret_cast<int *>(smem + C::OFF_NF)[set * D + f] = 0x7fffffff;
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(item_full(set));
+            }
+            ok = wait_free(item_full(set), (n >> 1) & 1);
+            if (!ok) break;
+            const PromptItem it = s_item[set];
+            if (it.rows == 0) break;
+            const int tiles = it.e1 - it.t0;
+            if (prompt_steps(it, 0) + prompt_steps(it, 1) > 0) {
+                PromptSeq sq;
+                sq.first = it.first; sq.past = it.past; sq.len = it.len; sq.n = 0;
+                const int sees = prompt_sees(a, sq, it.row0 + it.rows - 1);     // rows behind are not read
+                // the addresses of this lane's row of a tile: row 32 w + lane
+                const unsigned char *ka = nullptr, *va = nullptr;
+                uint32_t k_pair = 0, v_pair = 0;
+                bool row_ok = false, row_bad = false;
+                auto locate = [&](int t) {
+                    const long long row = (long long)t * 128 + 32 * w + lane;
+                    row_ok = row < sees;
+                    row_bad = false;
+                    ka = a.k; va = a.v;
+                    if (!row_ok) return;
+                    if (PAGED) {
+                        const int pi = (int)(((unsigned long long)(uint32_t)row * a.page_mul) >> a.page_sh), off = (int)row - pi * a.page_size;
+                        const int page = a.table[(long long)it.table_row * a.max_pages + pi];
+                        if (page < 0 || page >= a.num_pages) { row_bad = true; row_ok = false; raise_status(MOA_STATUS_PAGE_RANGE); return; }
+                        ka += page * a.k_sp + it.head * a.k_sh + off * a.k_sr;
+                        va += page * a.v_sp + it.head * a.v_sh + off * a.v_sr;
+                        if (Q4) {
+                            const long long at = ((long long)page * a.h_kv + it.head) * a.page_size + off;
+                            k_pair = a.kp[at]; v_pair = a.vp[at];
+                        }
+                    } else {
+                        ka += it.head * a.k_sh + (it.first + row) * a.k_sr;
+                        va += it.head * a.v_sh + (it.first + row) * a.v_sr;
+                    }
+                };
+                auto copy_rows = [&](uint32_t at, const unsigned char *mine, bool is_k) {
+#pragma unroll 4
+                    for (int i = 0; i < 32 / RPI; ++i) {
+                        const int from = RPI * i + rsub;
+                        const unsigned char *p = reinterpret_cast<const unsigned char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
+                        const int good = __shfl_sync(0xffffffffu, (int)row_ok, from);
+                        cp16(at + dst_of(32 * w + from), p + 16 * chunk, good != 0);
+                    }
+                    if (PAGED && is_k && __any_sync(0xffffffffu, row_bad)) {      // a page that does not exist: its scores are NaN
+                        cp_commit(); cp_wait<0>(); __syncwarp();
+                        for (int i = 0; i < 32 / RPI; ++i) {
+                            const int from = RPI * i + rsub;
+                            if (__shfl_sync(0xffffffffu, (int)row_bad, from))
+                                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at + dst_of(32 * w + from)), "r"(0x7fff7fffu) : "memory");
+                        }
+                    }
+                };
+                // 4-bit rows: a code c becomes c - 8 (exact), two to a register; the row's scale and least value go to the softmax.
+                auto unpack_rows = [&](uint32_t at, const unsigned char *mine) {
+                    constexpr int CP4 = D / 32;            // 16-byte chunks of a row of codes: 32 codes
+                    constexpr int NIT = CP4;               // 32 rows * CP4 chunks / 32 lanes
+                    uint4 x[NIT];
+#pragma unroll
+                    for (int i = 0; i < NIT; ++i) {
+                        const int from = i * (32 / CP4) + lane / CP4;
+                        const unsigned char *p = reinterpret_cast<const unsigned char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
+                        const int good = __shfl_sync(0xffffffffu, (int)row_ok, from);
+                        x[i] = good ? *reinterpret_cast<const uint4 *>(p + 16 * (lane % CP4)) : make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < NIT; ++i) {
+                        const int r = 32 * w + i * (32 / CP4) + lane / CP4;
+                        const uint32_t c4[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t two = (((c4[e] >> (8 * k)) & 0xffu) * 0x1001u) & 0x000f000fu;
+                                if (BF) {                  // 128 + c, less 136
+                                    const uint32_t y = two | 0x43004300u;
+                                    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&y), __floats2bfloat162_rn(136.f, 136.f));
+                                    o[k] = *reinterpret_cast<const uint32_t *>(&d);
+                                } else {                   // 1024 + c, less 1032
+                                    const uint32_t y = two | 0x64006400u;
+                                    const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&y), __floats2half2_rn(1032.f, 1032.f));
+                                    o[k] = *reinterpret_cast<const uint32_t *>(&d);
+                                }
+                            }
+                            const int ch = 4 * (lane % CP4) + e;              // 8 features of the row
+                            const uint32_t p = at + (uint32_t)(ch >> 3) * 16384u + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                        }
+                    }
+                };
+                auto copy_q = [&]() {
+                    ok = nq == 0 || wait_free(q_empty, (nq - 1) & 1);
+                    if (!ok) return;
+                    ++nq;
+                    const int parts = it.pair ? 1 : 2;
+                    for (int s = 0; s < parts; ++s) {
+                        const int r = 128 * s + 32 * w + lane;              // this lane finds one row's place
+                        const bool in = r < it.rows;
+                        const int row = it.row0 + (in ? r : 0), tok = div_g(a, row);
+                        const unsigned char *mine = a.q + (long long)(it.first + tok) * a.q_st + ((long long)it.head * a.g + (row - tok * a.g)) * (D * 2);
+#pragma unroll 4
+                        for (int i = 0; i < 32 / RPI; ++i) {
+                            const int from = RPI * i + rsub;
+                            const unsigned char *p = reinterpret_cast<const unsigned char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
+                            const int good = __shfl_sync(0xffffffffu, (int)in, from);
+                            cp16(base + C::OFF_Q + s * C::KV + dst_of(32 * w + from), p + 16 * chunk, good != 0);
+                        }
+                    }
+                    push(q_full, 0, -1);
+                    if (Q4) retire();
+                };
+                for (int t = 0; ok && t < tiles; ++t) {
+                    const uint32_t st = nk % NST;
+                    locate(it.t0 + t);
+                    ok = nk < NST || wait_free(k_empty(st), (nk / NST - 1) & 1);
+                    if (!ok) break;
+                    const uint32_t kd = base + C::OFF_K + st * C::KV, vd = base + C::OFF_V + st * C::KV;
+                    if (Q4) {
+                        // parameters: the softmax of the tile that had this place is done (its V is used up, NPAR / 2 tiles ago at the least)
+                        const uint32_t ps = nk % C::NPAR;
+                        const float2 kf = unpack16<false>(k_pair), vf = unpack16<false>(v_pair);
+                        float2 *par = reinterpret_cast<float2 *>(smem + C::OFF_PAR) + ps * 256 + 32 * w + lane;
+                        const float nan = __uint_as_float(0x7fffffffu);
+                        par[0] = row_bad ? make_float2(nan, nan) : row_ok ? make_float2(kf.x, fmaf(8.f, kf.x, kf.y)) : make_float2(0.f, 0.f);
+                        par[128] = row_ok ? make_float2(vf.x, fmaf(8.f, vf.x, vf.y)) : make_float2(0.f, 0.f);
+                        float top = row_ok ? vf.x : 0.f;
+#pragma unroll
+                        for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                        if (lane == 0) reinterpret_cast<float *>(smem + C::OFF_PMAX)[ps * 4 + w] = top;
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(par_full(ps));
+                        unpack_rows(kd, ka);
+                        tc::fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(k_full(st));
+                    } else {
+                        copy_rows(kd, ka, true);
+                        push(k_full(st), 0, -1);
+                    }
+                    ++nk;
+                    if (t == 0) { copy_q(); if (!ok) break; }
+                    ok = nv < NST || wait_free(v_empty(st), (nv / NST - 1) & 1);
+                    if (!ok) break;
+                    if (Q4) {
+                        unpack_rows(vd, va);
+                        tc::fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(v_full(st));
+                    } else {
+                        copy_rows(vd, va, false);
+                        push(v_full(st), vd, a.causal && (it.t0 + t + 1) * 128LL > it.least ? 2 * (it.t0 + t) + set : -1);
+                    }
+                    ++nv;
+                }
+                while (pending > 0) retire();              // the next item's number takes a while
+            }
+            if (w != 0 && ok) { __syncwarp(); if (lane == 0) tc::mbar_arrive(item_empty(set)); }
+        }
+        while (pending > 0) retire();
+        cp_wait<0>();
+    } else {
+        // ================= softmax =================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        const int s = warp >> 2, wq = warp & 3, row = 32 * wq + lane;       // slot; row of the slot = tensor memory lane
+        const uint32_t lane_at = (uint32_t)(32 * wq) << 16;
+        const uint32_t tS = t_s(s) + lane_at, tO = t_o(s) + lane_at;
+        float2 *const ml = reinterpret_cast<float2 *>(smem + C::OFF_ML);
+        uint32_t ns = 0, no = 0, nj = 0, nc = 0, np = 0;   // uses of s_full, o_full, joins, pieces, tiles of keys before the item
+        bool ok = true, unread = false;                    // unread: the other slot may still read this slot's sums
+        for (uint32_t n = 0; ok; ++n) {
+            ok = wait_warp(item_full(n & 1), (n >> 1) & 1, abort_flag);
+            if (!ok) break;
+            const PromptItem it = s_item[n & 1];
+            if (it.rows == 0) break;
+            const int cnt = prompt_steps(it, s), other = prompt_steps(it, s ^ 1);
+            const int r = row + (it.pair ? 0 : 128 * s);   // row of the unit
+            const bool valid = r < it.rows;
+            PromptSeq sq;
+            sq.first = it.first; sq.past = it.past; sq.len = it.len; sq.n = 0;
+            const int my = it.row0 + (valid ? r : 0), tok = div_g(a, my), qh = it.head * a.g + (my - tok * a.g);
+            const int lim = valid ? prompt_sees(a, sq, my) : 0;
+            float m = -INFINITY, l = 0.f;                  // reference (log2), sum of weights
+            float lm = 0.f, sigma = 0.f, sumq = 0.f;       // 4 bits: sum of weight * (least + 8 scale); power of two of the scales; sum of q
+            if (Q4 && cnt > 0 && valid) {
+                const uint4 *p = reinterpret_cast<const uint4 *>(a.q + (long long)(it.first + tok) * a.q_st + (long long)qh * (D * 2));
+                float s0 = 0.f, s1 = 0.f;
+#pragma unroll 4
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint4 u = p[i];
+                    const float2 x0 = unpack16<BF>(u.x), x1 = unpack16<BF>(u.y), x2 = unpack16<BF>(u.z), x3 = unpack16<BF>(u.w);
+                    s0 += (x0.x + x1.x) + (x2.x + x3.x);
+                    s1 += (x0.y + x1.y) + (x2.y + x3.y);
+                }
+                sumq = a.negate ? -(s0 + s1) : s0 + s1;
+            }
+            const int dead = !__any_sync(0xffffffffu, valid);                // a warp without rows only keeps step
+            for (int i = 0; ok && i < cnt; ++i, ++ns) {
+                const int t = it.t0 + (it.pair ? 2 * i + s : i);
+                ok = wait_warp(s_full(s), ns & 1, abort_flag);
+                if (!ok) break;
+                if (i == 0 && unread) {                    // (the join before: the other slot's reads come before these weights)
+                    ok = wait_warp(parted, (nj - 1) & 1, abort_flag);
+                    unread = false;
+                    if (!ok) break;
+                }
+                const uint32_t ps = (np + (uint32_t)(t - it.t0)) % C::NPAR;
+                if (Q4) {
+                    ok = wait_warp(par_full(ps), ((np + (uint32_t)(t - it.t0)) / C::NPAR) & 1, abort_flag);
+                    if (!ok) break;
+                }
+                if (!dead) {
+                    tc::fence_after_sync();
+                    uint32_t x[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tc::tmem_ld32(tS + 32 * c, x[c]);
+                    tc::tmem_ld_wait();
+                    float2 *const par = reinterpret_cast<float2 *>(smem + C::OFF_PAR) + ps * 256;
+                    if (Q4) {                              // scale * <q, c - 8> + (least + 8 scale) * sum(q)
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) {
+                            const float2 k2 = par[c];
+                            x[c >> 5][c & 31] = __float_as_uint(fmaf(k2.x, __uint_as_float(x[c >> 5][c & 31]), k2.y * sumq));
+                        }
+                    }
+                    const int vis = lim - t * 128;         // keys of this tile that the row sees
+                    const bool masked = !__all_sync(0xffffffffu, vis >= 128);
+                    if (masked) {
+#pragma unroll
+                        for (int c = 0; c < 128; ++c)
+                            if (c >= vis) x[c >> 5][c & 31] = 0xff800000u;
+                    }
+                    float mx[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float u = __uint_as_float(x[c][0]);
+#pragma unroll
+                        for (int e = 1; e < 32; ++e) u = max_nan(u, __uint_as_float(x[c][e]));
+                        mx[c] = u;
+                    }
+                    float top = max_nan(max_nan(mx[0], mx[1]), max_nan(mx[2], mx[3])) * a.qscale;
+                    if (masked && vis <= 0) top = -INFINITY;                 // (a scale of 0 would make it NaN)
+                    // The reference moves for a row where a score passes it by AHEAD; for all rows of the warp then.
+                    float sig_new = sigma;
+                    if (Q4 && !BF) {
+                        const float4 u = *reinterpret_cast<const float4 *>(smem + C::OFF_PMAX + ps * 16);
+                        const float st = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
+                        if (st > sigma) sig_new = __uint_as_float((__float_as_uint(st) + 0x007fffffu) & 0x7f800000u);
+                    }
+                    if (__any_sync(0xffffffffu, !(top <= m + C::AHEAD) && !(top == -INFINITY)) || (Q4 && !BF && sig_new != sigma)) {
+                        float mn = max_nan(m, top);
+                        if (mn == INFINITY) mn = __uint_as_float(0x7fffffffu);      // (infinity less itself: the row is NaN)
+                        float f = mn == m ? 1.f : m == -INFINITY && mn == mn ? 0.f : fast_exp2(m - mn);
+                        l *= f; lm *= f;
+                        if (Q4 && !BF) { if (sigma > 0.f) f *= sigma / sig_new; sigma = sig_new; }
+                        m = mn;
+                        if (i > 0) {
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 32) {
+                                uint32_t o[32];
+                                tc::tmem_ld32(tO + c, o);
+                                tc::tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tc::tmem_st32(tO + c, o);
+                            }
+                        }
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    const uint64_t qs2 = pack2f(a.qscale, a.qscale), nm2 = pack2f(C::SHIFT - ref, C::SHIFT - ref);
+                    uint64_t sum = pack2f(0.f, 0.f), summ = pack2f(0.f, 0.f);
+                    const float isig = Q4 && !BF ? 1.f / fmaxf(sigma, 1e-30f) : 1.f;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const uint64_t y = fma2(pack2(x[c][e], x[c][e + 1]), qs2, nm2);
+                            float2 p;
+                            if ((e & 7) == 6) p = exp2_pair<C::DEG>(y);
+                            else { const float2 v = unpack2f(y); p = make_float2(fast_exp2(v.x), fast_exp2(v.y)); }
+                            const uint64_t pp = pack2f(p.x, p.y);
+                            sum = add2(sum, pp);
+                            if (Q4) {
+                                float4 u = *reinterpret_cast<const float4 *>(par + 128 + 32 * c + e);      // (scale, least + 8 scale) of two rows
+                                if (masked) {              // a row that is not seen may hold anything
+                                    if (32 * c + e >= vis) u.x = u.y = 0.f;
+                                    if (32 * c + e + 1 >= vis) u.z = u.w = 0.f;
+                                }
+                                summ = fma2(pp, pack2f(u.y, u.w), summ);
+                                p.x *= u.x * isig; p.y *= u.z * isig;
+                            }
+                            pk[e >> 1] = pack16<BF>(p.x, p.y);
+                        }
+                        tc::tmem_st16(tS + 16 * c, pk);
+                    }
+                    const float2 u = unpack2f(sum);
+                    l += u.x + u.y;
+                    if (Q4) { const float2 v = unpack2f(summ); lm += v.x + v.y; }
+                    tc::tmem_st_wait();
+                    tc::fence_before_sync();
+                }
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(p_full(s));
+            }
+            if (!ok) break;
+            np += (uint32_t)(it.e1 - it.t0);
+
+            // ---- the unit's end ----
+            if (cnt > 0) { ok = wait_warp(o_full(s), no & 1, abort_flag); ++no; if (!ok) break; }
+            const bool nf = s_nf[n & 1] != 0;
+            const int *const nf_key = reinterpret_cast<const int *>(smem + C::OFF_NF) + (n & 1) * D;
+            int c0 = 0, c1 = D;                            // this thread's columns
+            float fa = 1.f, fb = 0.f;                      // factors of the slots' sums
+            float M = m, L = l, add = lm;
+            if (Q4 && !BF) fa = sigma;
+            if (it.pair) {                                 // each thread joins half the columns of both slots
+                ml[s * 128 + row] = make_float2(m, l);
+                if (Q4) s_more[Q4 ? s : 0][Q4 ? row : 0] = make_float2(lm, sigma);
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(joined);
+                ok = wait_warp(joined, nj & 1, abort_flag);
+                if (!ok) break;
+                tc::fence_after_sync();
+                const float2 o = ml[(s ^ 1) * 128 + row];
+                M = max_nan(m, o.x);
+                const float f0 = m == -INFINITY ? 0.f : fast_exp2(m - M), f1 = o.x == -INFINITY ? 0.f : fast_exp2(o.x - M);
+                L = l * f0 + o.y * f1;
+                fa = f0; fb = f1;
+                if (Q4) {
+                    const float2 e = s_more[Q4 ? s ^ 1 : 0][Q4 ? row : 0];
+                    add = lm * f0 + e.x * f1;
+                    if (!BF) { fa *= sigma; fb *= e.y; }
+                }
+                c0 = s * (D / 2); c1 = c0 + D / 2;
+            }
+            const uint32_t tB = t_o(s ^ 1) + lane_at;
+            float inv = 1.f;
+            float *part = nullptr;
+            if (it.slot < 0) inv = lim <= 0 ? 0.f : 1.f / L;
+            else part = a.slots + (long long)(it.slot + it.piece * it.slot_step) * a.slot_rows * (D + 2);
+            unsigned char *const dst = a.out + (long long)(it.first + tok) * a.o_st + (long long)qh * (D * 2);
+#pragma unroll 1
+            for (int c = c0; c < c1; c += 32) {
+                uint32_t o[32];
+                if (cnt > 0) { tc::tmem_ld32(tO + c, o); tc::tmem_ld_wait(); }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = cnt > 0 && M != -INFINITY ? __float_as_uint(__uint_as_float(o[e]) * fa) : 0u;
+                if (it.pair && other > 0) {
+                    uint32_t o2[32];
+                    tc::tmem_ld32(tB + c, o2);
+                    tc::tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) if (M != -INFINITY) o[e] = __float_as_uint(fmaf(__uint_as_float(o2[e]), fb, __uint_as_float(o[e])));
+                }
+                if (Q4) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) + add);
+                }
+                if (nf) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) if (nf_key[c + e] < lim) o[e] = 0x7fffffffu;
+                }
+                if (valid) {
+                    if (part == nullptr) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                y[k] = pack16<BF>(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
+                            *reinterpret_cast<uint4 *>(dst + (c + e) * 2) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            reinterpret_cast<uint4 *>(part)[(long long)((c + e) >> 2) * a.slot_rows + r] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    }
+                }
+            }
+            if (it.pair) {
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(parted);
+                ++nj;
+                unread = true;
+            }
+            if (part != nullptr) {
+                if (valid && (!it.pair || s == 0)) reinterpret_cast<float2 *>(part + (long long)D * a.slot_rows)[r] = make_float2(M, L);
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(delivered);
+                ok = wait_warp(delivered, nc & 1, abort_flag);
+                if (!ok) break;
+                if (tid == 0) {
+                    unsigned long long *word = a.tickets + it.slot;
+                    const bool last = ticket_arrive(word, a.ticket_tag) + 1 == (unsigned)it.pieces;
+                    if (last) *word = 0;
+                    __threadfence();
+                    s_last = last;
+                    tc::mbar_arrive(counted);
+                }
+                ok = wait_warp(counted, nc & 1, abort_flag);
+                ++nc;
+                if (!ok) break;
+                if (s_last && valid) {                     // join the pieces, in order
+                    const float *const p0 = a.slots + (long long)it.slot * a.slot_rows * (D + 2);
+                    const long long step = (long long)it.slot_step * a.slot_rows * (D + 2);
+                    float top = -INFINITY, total = 0.f;
+                    for (int p = 0; p < it.pieces; ++p) top = max_nan(top, __ldcg(reinterpret_cast<const float2 *>(p0 + p * step + (long long)D * a.slot_rows) + r).x);
+                    for (int p = 0; p < it.pieces; ++p) {
+                        const float2 e = __ldcg(reinterpret_cast<const float2 *>(p0 + p * step + (long long)D * a.slot_rows) + r);
+                        total = fmaf(e.y, exp2_diff(e.x, top), total);
+                    }
+                    const float scale = lim <= 0 ? 0.f : 1.f / total;
+#pragma unroll 1
+                    for (int c = c0; c < c1; c += 16) {
+                        float acc[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+                        for (int p = 0; p < it.pieces; ++p) {
+                            const float *const pp = p0 + p * step;
+                            const float f = exp2_diff(__ldcg(reinterpret_cast<const float2 *>(pp + (long long)D * a.slot_rows) + r).x, top);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) {
+                                const float4 u = __ldcg(reinterpret_cast<const float4 *>(pp) + (long long)((c + e) >> 2) * a.slot_rows + r);
+                                acc[e] = fmaf(u.x, f, acc[e]); acc[e + 1] = fmaf(u.y, f, acc[e + 1]);
+                                acc[e + 2] = fmaf(u.z, f, acc[e + 2]); acc[e + 3] = fmaf(u.w, f, acc[e + 3]);
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; e += 8)
+                            *reinterpret_cast<uint4 *>(dst + (c + e) * 2) =
+                                make_uint4(pack16<BF>(acc[e] * scale, acc[e + 1] * scale), pack16<BF>(acc[e + 2] * scale, acc[e + 3] * scale),
+                                           pack16<BF>(acc[e + 4] * scale, acc[e + 5] * scale), pack16<BF>(acc[e + 6] * scale, acc[e + 7] * scale));
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(item_empty(n & 1));
+        }
+    }
+    __syncwarp();
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    if (warp == 12) tc::tmem_dealloc(tmem, 512);
+}
+
+}  // namespace moa
