@@ -294,6 +294,33 @@ int moa_paged_append(const moa_paged_cache *cache, const void *q, const void *k,
                      void *stream);
 
 /*
+ * Positions with several axes (time, height and width of an image or a video).  Pair i of a token's heads is
+ * turned by the angle of position positions[axis_of_pair[i]][token]: its cosine and sine are entries i and
+ * rot_dim/2 + i of that row of cos_sin.
+ *   positions: device int32 [axes][tokens]; axes from 1 to MOA_MAX_AXES.
+ *   axis_of_pair: HOST, rot_dim/2 bytes below `axes`, read during the call: any order (runs of pairs, axes by turns).
+ *   cos_sin, rope_rows, rot_dim (2 at least), rope_style: as for moa_paged_append, and so is the arithmetic.
+ * A token with a position outside [0, rope_rows) on any axis sets MOA_STATUS_APPEND_RANGE and nothing of it is written.
+ *
+ * moa_paged_append_axes: moa_paged_append with such positions (which say nothing about the row: that is
+ *   still the token's place in its sequence).
+ * moa_rotate_axes: queries and keys without a cache (before moa_prompt_attn): q [tokens, h_q, d], k [tokens, h_kv, d]
+ *   into q_out, k_out of the same shape and type.  h_q and h_kv are independent; one of them may be 0 (its tensors are
+ *   not touched and may be NULL).  q_out may be q and k_out k, with the same stride.  token_strides: HOST, {q, k, q_out, k_out}, or
+ *   NULL: dense.  Tensors are 16-byte aligned, strides multiples of 16 bytes; d is 64 or 128.
+ */
+#define MOA_MAX_AXES 4
+int moa_paged_append_axes(const moa_paged_cache *cache, const void *q, const void *k, const void *v, void *q_out,
+                          int dtype, const long long *token_strides, int tokens, int h_q, int batch,
+                          const int32_t *token_start, const int32_t *seq_lens, const int32_t *page_table,
+                          int max_pages, const int32_t *positions, int axes, const unsigned char *axis_of_pair,
+                          const float *cos_sin, int rope_rows, int rot_dim, int rope_style, void *stream);
+int moa_rotate_axes(const void *q, const void *k, void *q_out, void *k_out, int dtype, const long long *token_strides,
+                    int tokens, int h_q, int h_kv, int d, const int32_t *positions, int axes,
+                    const unsigned char *axis_of_pair, const float *cos_sin, int rope_rows, int rot_dim, int rope_style,
+                    void *stream);
+
+/*
  * Decode attention over a paged cache: Algorithm 1 for one query per sequence and head over rows
  * [0, seq_lens[b]), with the head grouping of section 6.
  *   q [batch, h_q, d], `q_stride` elements between sequences (a multiple of 16 bytes; 0: h_q * d);

@@ -88,6 +88,8 @@ def lib():
         L.moa_paged_workspace_bytes.argtypes = [i, i, i, i]
         L.moa_paged_workspace_bytes.restype = sz
         L.moa_paged_gather.argtypes = [pc, p, p, i, i, i, p, p, p, i, p]
+        L.moa_paged_append_axes.argtypes = [pc, p, p, p, p, i, p, i, i, i, p, p, p, i, p, i, C.c_char_p, p, i, i, i, p]
+        L.moa_rotate_axes.argtypes = [p, p, p, p, i, p, i, i, i, i, p, i, C.c_char_p, p, i, i, i, p]
         L.moa_prompt_attn.argtypes = [p, p, p, p, i, p, i, i, i, i, i, p, i, f, p, sz, p]
         L.moa_paged_chunk_attn.argtypes = [pc, p, p, i, C.c_longlong, i, i, i, p, p, p, i, f, p, sz, p]
         L.moa_prompt_workspace_bytes.argtypes = [i, i, i, i, i]
@@ -291,6 +293,40 @@ def _token_strides(st, what):
     if len(st) != 4:
         raise ValueError("token strides are (%s) element counts" % what)
     return _strides4(*st)
+
+
+def _axis_map(axis_of_pair, rot_dim):
+    if type(axis_of_pair) is not bytes and axis_of_pair is not None:
+        axis_of_pair = bytes(axis_of_pair)
+    if axis_of_pair is not None and len(axis_of_pair) != rot_dim // 2:
+        raise ValueError("axis_of_pair names an axis for each of the rot_dim / 2 pairs")
+    return axis_of_pair
+
+
+def moa_paged_append_axes(cache, q, k, v, q_out, dtype, token_strides, tokens, h_q, batch, token_start, seq_lens,
+                          page_table, max_pages, positions, axes, axis_of_pair, cos_sin, rope_rows, rot_dim, rope_style,
+                          stream=None):
+    """:func:`moa_paged_append` with positions [axes, tokens]; axis_of_pair: bytes (or a sequence of small
+    numbers), the axis that turns each pair."""
+    code = (_lib or lib()).moa_paged_append_axes(cache, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), dtype,
+                                                 _token_strides(token_strides, "q, k, v, q_out"), tokens, h_q, batch,
+                                                 _ptr(token_start), _ptr(seq_lens), _ptr(page_table), max_pages,
+                                                 _ptr(positions), axes, _axis_map(axis_of_pair, rot_dim), _ptr(cos_sin),
+                                                 rope_rows, rot_dim, rope_style, _stream(stream))
+    if code != OK:
+        raise MoaError(code, "moa_paged_append_axes")
+
+
+def moa_rotate_axes(q, k, q_out, k_out, dtype, token_strides, tokens, h_q, h_kv, d, positions, axes, axis_of_pair, cos_sin,
+                    rope_rows, rot_dim, rope_style, stream=None):
+    """Queries and keys turned by positions [axes, tokens].
+    token_strides: None (dense) or element counts between tokens of (q, k, q_out, k_out)."""
+    code = (_lib or lib()).moa_rotate_axes(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), dtype,
+                                           _token_strides(token_strides, "q, k, q_out, k_out"), tokens, h_q, h_kv, d,
+                                           _ptr(positions), axes, _axis_map(axis_of_pair, rot_dim), _ptr(cos_sin), rope_rows,
+                                           rot_dim, rope_style, _stream(stream))
+    if code != OK:
+        raise MoaError(code, "moa_rotate_axes")
 
 
 def moa_prompt_attn(q, k, v, out, dtype, token_strides, tokens, h_q, h_kv, d, batch, token_start, causal, scale,

@@ -1055,28 +1055,65 @@ static PagedIoArgs paged_io_args(const moa_paged_cache *c, const long long *ks, 
     return a;
 }
 
-template <int FMT, int DT, int D>
+template <int FMT, int DT, int D, int MODE>
 static cudaError_t launch_append(const PagedIoArgs &a, cudaStream_t st)
 {
-    const long long rows = (long long)a.tokens * (a.q_runs + 2 * a.kv_runs), per_block = 256 / (D / 16);
+    const long long rows = (long long)a.tokens * (a.q_runs + (MODE == kRotateOnly ? 1 : 2) * a.kv_runs), per_block = 256 / (D / 16);
     const int blocks = (int)((rows + per_block - 1) / per_block);
-    if (a.rot == 0) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnNone>, blocks, 256, 0, st, a);
-    else if (a.pairs) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnPairs>, blocks, 256, 0, st, a);
-    else if (a.rot % 16 == 0) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnChunks>, blocks, 256, 0, st, a);
-    else launch_dependent(paged_append_kernel<FMT, DT, D, kTurnAny>, blocks, 256, 0, st, a);
+    if (a.rot == 0) { if constexpr (MODE == kByRow) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnNone>, blocks, 256, 0, st, a); }
+    else if (a.pairs) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnPairs, MODE>, blocks, 256, 0, st, a);
+    else if (a.rot % 16 == 0) launch_dependent(paged_append_kernel<FMT, DT, D, kTurnChunks, MODE>, blocks, 256, 0, st, a);
+    else launch_dependent(paged_append_kernel<FMT, DT, D, kTurnAny, MODE>, blocks, 256, 0, st, a);
     count_launch();
     return cudaGetLastError();
 }
-template <int FMT, int DT>
+template <int FMT, int DT, int MODE>
 static cudaError_t launch_append(const PagedIoArgs &a, int d, cudaStream_t st)
 {
-    return d == 128 ? launch_append<FMT, DT, 128>(a, st) : launch_append<FMT, DT, 64>(a, st);
+    return d == 128 ? launch_append<FMT, DT, 128, MODE>(a, st) : launch_append<FMT, DT, 64, MODE>(a, st);
+}
+template <int MODE>
+static cudaError_t launch_append(const PagedIoArgs &a, int format, int dtype, int d, cudaStream_t st)
+{
+    switch (format) {
+    case MOA_KV_F32: return launch_append<MOA_KV_F32, MOA_F32, MODE>(a, d, st);
+    case MOA_KV_BF16: return launch_append<MOA_KV_BF16, MOA_BF16, MODE>(a, d, st);
+    case MOA_KV_F16: return launch_append<MOA_KV_F16, MOA_F16, MODE>(a, d, st);
+    default:
+        if constexpr (MODE == kRotateOnly) return cudaErrorInvalidValue;
+        else return dtype == MOA_BF16 ? launch_append<MOA_KV_INT4, MOA_BF16, MODE>(a, d, st) : launch_append<MOA_KV_INT4, MOA_F16, MODE>(a, d, st);
+    }
+}
+
+// Heads of one run: 4 share the search for the token's sequence and page and its cosines and sines
+// where there are rows enough to fill the GPU that way, one where there are not (7.9k tokens of 48 heads in bf16:
+// 38.5 us with runs of 4, 38.8 with 8, 42.7 with 2).
+static void append_runs(PagedIoArgs &a, const DeviceState &dev, long long rows, int d)
+{
+    const long long fill = (long long)dev.sm_count * 1024 / (d / 16);
+    a.run = rows >= 4 * fill ? 4 : rows >= 2 * fill ? 2 : 1;
+    a.q_runs = (a.h_q + a.run - 1) / a.run;
+    a.kv_runs = (a.h_kv + a.run - 1) / a.run;
+}
+
+// Positions of several axes: device [axes][tokens], and HOST, for each pair, the axis that turns it.
+struct RopeAxes { const int32_t *positions; int axes; const unsigned char *axis_of_pair; };
+
+static int check_axes(const RopeAxes &x, int rot_dim, PagedIoArgs &a)
+{
+    if (!x.positions || !x.axis_of_pair || x.axes < 1 || x.axes > MOA_MAX_AXES || rot_dim < 2) return MOA_ERR_INVALID;
+    a.positions = x.positions; a.axes = x.axes;
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        if (x.axis_of_pair[i] >= x.axes) return MOA_ERR_INVALID;
+        a.axis_map[i >> 5] |= (unsigned long long)x.axis_of_pair[i] << (2 * (i & 31));
+    }
+    return aligned(x.positions, 4) ? MOA_OK : MOA_ERR_ALIGN;
 }
 
 static int paged_append_impl(const moa_paged_cache *c, const void *q, const void *k, const void *v, void *q_out, int dtype,
                              const long long *ts, int tokens, int h_q, int batch, const int32_t *token_start,
                              const int32_t *seq_lens, const int32_t *page_table, int max_pages, const float *cos_sin,
-                             int rope_rows, int rot_dim, int rope_style, cudaStream_t st)
+                             int rope_rows, int rot_dim, int rope_style, const RopeAxes *axes, cudaStream_t st)
 {
     if (!c || !k || !v || !seq_lens || !page_table) return MOA_ERR_INVALID;
     if (tokens < 1 || h_q < 0 || batch < 1 || max_pages < 1) return MOA_ERR_INVALID;
@@ -1089,6 +1126,11 @@ static int paged_append_impl(const moa_paged_cache *c, const void *q, const void
     if (rot_dim < 0 || rot_dim > c->d || rot_dim % 2 != 0) return MOA_ERR_INVALID;
     if (rot_dim > 0 && (!cos_sin || rope_rows < 1 || (rope_style != MOA_ROPE_HALVES && rope_style != MOA_ROPE_PAIRS))) return MOA_ERR_INVALID;
     if (!token_start && tokens != batch) return MOA_ERR_INVALID;
+    PagedIoArgs a = paged_io_args(c, ks, vs, batch, seq_lens, page_table, max_pages);
+    if (axes) {
+        rc = check_axes(*axes, rot_dim, a);
+        if (rc != MOA_OK) return rc;
+    }
     const long long dense[4] = {(long long)h_q * c->d, (long long)c->h_kv * c->d, (long long)c->h_kv * c->d, (long long)h_q * c->d};
     long long s[4];
     const int es = element_bytes(dtype);
@@ -1110,27 +1152,52 @@ static int paged_append_impl(const moa_paged_cache *c, const void *q, const void
     DeviceState *dev = nullptr;
     rc = current_device(&dev);
     if (rc != MOA_OK) return rc;
-    PagedIoArgs a = paged_io_args(c, ks, vs, batch, seq_lens, page_table, max_pages);
     a.q = q; a.k = k; a.v = v; a.q_out = q_out;
     a.q_st = s[0]; a.k_st = s[1]; a.v_st = s[2]; a.o_st = s[3];
     a.tokens = tokens; a.h_q = h_q; a.token_start = token_start;
     a.cos_sin = cos_sin; a.rope_rows = rope_rows; a.rot = rot_dim; a.pairs = rope_style == MOA_ROPE_PAIRS;
-    // Heads of one run: 4 share the search for the token's sequence and page and its cosines and sines
-    // where there are rows enough to fill the GPU that way, one where there are not (7.9k tokens of 48 heads in bf16:
-    // 38.5 us with runs of 4, 38.8 with 8, 42.7 with 2).
-    const long long fill = (long long)dev->sm_count * 1024 / (c->d / 16);
-    a.run = rows >= 4 * fill ? 4 : rows >= 2 * fill ? 2 : 1;
-    a.q_runs = (h_q + a.run - 1) / a.run;
-    a.kv_runs = (c->h_kv + a.run - 1) / a.run;
-    cudaError_t e;
-    switch (c->format) {
-    case MOA_KV_F32: e = launch_append<MOA_KV_F32, MOA_F32>(a, c->d, st); break;
-    case MOA_KV_BF16: e = launch_append<MOA_KV_BF16, MOA_BF16>(a, c->d, st); break;
-    case MOA_KV_F16: e = launch_append<MOA_KV_F16, MOA_F16>(a, c->d, st); break;
-    default:
-        e = dtype == MOA_BF16 ? launch_append<MOA_KV_INT4, MOA_BF16>(a, c->d, st) : launch_append<MOA_KV_INT4, MOA_F16>(a, c->d, st);
-    }
+    append_runs(a, *dev, rows, c->d);
+    const cudaError_t e = axes ? launch_append<kByAxes>(a, c->format, dtype, c->d, st) : launch_append<kByRow>(a, c->format, dtype, c->d, st);
     return e == cudaSuccess ? MOA_OK : MOA_ERR_CUDA;
+}
+
+static int rotate_impl(const void *q, const void *k, void *q_out, void *k_out, int dtype, const long long *ts, int tokens, int h_q,
+                       int h_kv, int d, const RopeAxes &axes, const float *cos_sin, int rope_rows, int rot_dim, int rope_style,
+                       cudaStream_t st)
+{
+    if (tokens < 1 || h_q < 0 || h_kv < 0 || h_q + h_kv < 1 || d < 1 || dtype < MOA_F32 || dtype > MOA_F16) return MOA_ERR_INVALID;
+    if ((h_q > 0 && (!q || !q_out)) || (h_kv > 0 && (!k || !k_out))) return MOA_ERR_INVALID;
+    if (d != 64 && d != 128) return MOA_ERR_UNSUPPORTED;
+    if (rot_dim < 2 || rot_dim > d || rot_dim % 2 != 0 || !cos_sin || rope_rows < 1 || (rope_style != MOA_ROPE_HALVES && rope_style != MOA_ROPE_PAIRS))
+        return MOA_ERR_INVALID;
+    const int heads[4] = {h_q, h_kv, h_q, h_kv}, es = element_bytes(dtype);
+    const void *at[4] = {q, k, q_out, k_out};
+    long long s[4];
+    bool wide = true;
+    for (int i = 0; i < 4; ++i) {
+        s[i] = 0;
+        if (heads[i] == 0) continue;
+        s[i] = ts ? ts[i] : (long long)heads[i] * d;
+        if (s[i] < 0 || s[i] > (1LL << 40)) return MOA_ERR_INVALID;
+        if (i >= 2 && s[i] < (long long)heads[i] * d && tokens > 1) return MOA_ERR_INVALID;      // written rows may not overlap
+        if (s[i] * es % 16 != 0 || !aligned(at[i], 16)) wide = false;
+    }
+    if ((h_q > 0 && q == q_out && s[0] != s[2]) || (h_kv > 0 && k == k_out && s[1] != s[3])) return MOA_ERR_INVALID;
+    PagedIoArgs a = {};
+    int rc = check_axes(axes, rot_dim, a);
+    if (rc != MOA_OK) return rc;
+    if (!wide || !aligned(cos_sin, 16)) return MOA_ERR_ALIGN;
+    const long long rows = (long long)tokens * ((long long)h_q + h_kv);
+    if ((long long)h_q + h_kv > 0x7fffffffLL || rows > 0x7fffffffLL * 16) return MOA_ERR_CAPACITY;
+    DeviceState *dev = nullptr;
+    rc = current_device(&dev);
+    if (rc != MOA_OK) return rc;
+    a.q = q; a.k = k; a.q_out = q_out; a.rk_out = k_out;
+    a.q_st = s[0]; a.k_st = s[1]; a.o_st = s[2]; a.rk_st = s[3];
+    a.tokens = tokens; a.h_q = h_q; a.h_kv = h_kv;
+    a.cos_sin = cos_sin; a.rope_rows = rope_rows; a.rot = rot_dim; a.pairs = rope_style == MOA_ROPE_PAIRS;
+    append_runs(a, *dev, rows, d);
+    return launch_append<kRotateOnly>(a, dtype, dtype, d, st) == cudaSuccess ? MOA_OK : MOA_ERR_CUDA;
 }
 
 template <int D>
@@ -1607,7 +1674,29 @@ int moa_paged_append(const moa_paged_cache *cache, const void *q, const void *k,
 {
     Lock lock(g_mu);
     return paged_append_impl(cache, q, k, v, q_out, dtype, token_strides, tokens, h_q, batch, token_start, seq_lens,
-                             page_table, max_pages, cos_sin, rope_rows, rot_dim, rope_style, static_cast<cudaStream_t>(stream));
+                             page_table, max_pages, cos_sin, rope_rows, rot_dim, rope_style, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+int moa_paged_append_axes(const moa_paged_cache *cache, const void *q, const void *k, const void *v, void *q_out, int dtype,
+                          const long long *token_strides, int tokens, int h_q, int batch, const int32_t *token_start,
+                          const int32_t *seq_lens, const int32_t *page_table, int max_pages, const int32_t *positions, int axes,
+                          const unsigned char *axis_of_pair, const float *cos_sin, int rope_rows, int rot_dim, int rope_style,
+                          void *stream)
+{
+    Lock lock(g_mu);
+    const RopeAxes x = {positions, axes, axis_of_pair};
+    return paged_append_impl(cache, q, k, v, q_out, dtype, token_strides, tokens, h_q, batch, token_start, seq_lens,
+                             page_table, max_pages, cos_sin, rope_rows, rot_dim, rope_style, &x, static_cast<cudaStream_t>(stream));
+}
+
+int moa_rotate_axes(const void *q, const void *k, void *q_out, void *k_out, int dtype, const long long *token_strides, int tokens,
+                    int h_q, int h_kv, int d, const int32_t *positions, int axes, const unsigned char *axis_of_pair,
+                    const float *cos_sin, int rope_rows, int rot_dim, int rope_style, void *stream)
+{
+    Lock lock(g_mu);
+    const RopeAxes x = {positions, axes, axis_of_pair};
+    return rotate_impl(q, k, q_out, k_out, dtype, token_strides, tokens, h_q, h_kv, d, x, cos_sin, rope_rows, rot_dim, rope_style,
+                       static_cast<cudaStream_t>(stream));
 }
 
 int moa_paged_decode_attn(const moa_paged_cache *cache, const void *q, void *out, int dtype, long long q_stride, int batch,

@@ -36,6 +36,12 @@ struct PagedIoArgs {
     const float *cos_sin;            // [rope_rows, rot]: rot/2 cosines, rot/2 sines
     int rope_rows, rot;
     int pairs;                       // features (2i, 2i+1) turn together; else (i, rot/2 + i)
+    // positions of several axes
+    const int32_t *positions;        // [axes, tokens]
+    int axes;
+    unsigned long long axis_map[2];  // two bits a pair: the axis that turns it
+    void *rk_out;                    // keys that are turned without a cache, rk_st elements between tokens
+    long long rk_st;
     // read-back
     void *k_out, *v_out;
     const int32_t *row_start;
@@ -143,6 +149,9 @@ __device__ __forceinline__ void pack_row(const float (&lo)[8], const float (&hi)
 // How the pairs that turn together lie: none, in a thread's two chunks (halves, rot a multiple of 16),
 // next to each other, or anywhere (halves of another size: partners are fetched one by one).
 enum PagedTurn { kTurnNone, kTurnChunks, kTurnPairs, kTurnAny };
+// What turns a row and where it goes: by its row number into a cache, by its token's positions on several axes into a
+// cache, or by these from tensor to tensor (queries and keys only).
+enum PagedMode { kByRow, kByAxes, kRotateOnly };
 
 // Two chunks of a row as they are loaded.
 template <int DT> struct RowPart { uint4 u[DT == MOA_F32 ? 4 : 2]; };
@@ -158,7 +167,7 @@ __device__ __forceinline__ void fetch(RowPart<DT> &r, const unsigned char *row, 
 }
 
 // FMT: of the pools; DT: of q, k, v.  The same for 16 and 32 bits.
-template <int FMT, int DT, int D, int TURN>
+template <int FMT, int DT, int D, int TURN, int MODE = kByRow>
 __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || FMT == MOA_KV_INT4 ? 3 : 4) paged_append_kernel(const __grid_constant__ PagedIoArgs a)
 {
     constexpr int TPR = D / 16, SLOTS = 256 / TPR, ES = DT == MOA_F32 ? 4 : 2, N = DT == MOA_F32 ? 2 : 1;
@@ -169,7 +178,7 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
     const long long item = (long long)blockIdx.x * SLOTS + threadIdx.x / TPR;     // run by run, the tokens of a run in order
     const int run = item <= 0xffffffffll ? (int)((unsigned)item / (unsigned)a.tokens) : (int)(item / a.tokens);
     const int tok = (int)(item - (long long)run * a.tokens);
-    if (run >= a.q_runs + 2 * a.kv_runs) return;           // (the threads of a row leave together)
+    if (run >= a.q_runs + (MODE == kRotateOnly ? 1 : 2) * a.kv_runs) return;           // (the threads of a row leave together)
     const int kind = run < a.q_runs ? 0 : run < a.q_runs + a.kv_runs ? 1 : 2;      // q, k, v
     const int h0 = (run - (kind == 0 ? 0 : kind == 1 ? a.q_runs : a.q_runs + a.kv_runs)) * a.run;
     const int h1 = min(h0 + a.run, kind == 0 ? a.h_q : a.h_kv);
@@ -186,51 +195,70 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
     fetch<DT>(next, src, d_lo, d_hi);
 
     // The token's sequence, position and row.
-    int b = tok;
-    long long pos;
-    if (a.token_start != nullptr) {
-        int lo = 0, hi = a.batch;                          // last b with token_start[b] <= tok
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.token_start[mid] <= tok) lo = mid; else hi = mid;
+    long long pos = 0, page = 0;
+    int off = 0, status = 0;
+    if constexpr (MODE != kRotateOnly) {
+        int b = tok;
+        if (a.token_start != nullptr) {
+            int lo = 0, hi = a.batch;                          // last b with token_start[b] <= tok
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.token_start[mid] <= tok) lo = mid; else hi = mid;
+            }
+            b = lo;
+            const int first = a.token_start[b], next = a.token_start[b + 1];
+            if (first > tok || tok >= next) return;            // behind the last sequence: left as it is
+            pos = (long long)a.seq_lens[b] - ((long long)next - tok);
+        } else {
+            pos = (long long)a.seq_lens[b] - 1;
+            if (pos == -1) return;                             // a padded batch: no token
         }
-        b = lo;
-        const int first = a.token_start[b], next = a.token_start[b + 1];
-        if (first > tok || tok >= next) return;            // behind the last sequence: left as it is
-        pos = (long long)a.seq_lens[b] - ((long long)next - tok);
-    } else {
-        pos = (long long)a.seq_lens[b] - 1;
-        if (pos == -1) return;                             // a padded batch: no token
+        const int pi = pos < 0 ? 0 : a.page_shift >= 0 ? (int)pos >> a.page_shift : (int)pos / a.page_size;
+        if (pos < 0 || pi >= a.max_pages || (TURN != kTurnNone && MODE == kByRow && pos >= a.rope_rows)) status = MOA_STATUS_APPEND_RANGE;
+        else {
+            page = a.table[(long long)b * a.max_pages + pi];
+            off = (int)pos - pi * a.page_size;
+            if (page < 0 || page >= a.num_pages) status = MOA_STATUS_PAGE_RANGE;
+        }
     }
-    const int pi = pos < 0 ? 0 : a.page_shift >= 0 ? (int)pos >> a.page_shift : (int)pos / a.page_size;
-    int status = 0, off = 0;
-    long long page = 0;
-    if (pos < 0 || pi >= a.max_pages || (TURN != kTurnNone && pos >= a.rope_rows)) status = MOA_STATUS_APPEND_RANGE;
-    else {
-        page = a.table[(long long)b * a.max_pages + pi];
-        off = (int)pos - pi * a.page_size;
-        if (page < 0 || page >= a.num_pages) status = MOA_STATUS_PAGE_RANGE;
+    // Where its angles stand: a row of the table, or a row for each axis.
+    const int rot = a.rot, half = rot / 2;
+    const float *row = a.cos_sin + pos * rot, *axis_row[4] = {};
+    if constexpr (MODE != kByRow) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            if (x < a.axes) {
+                const int at = a.positions[(long long)x * a.tokens + tok];
+                if (at < 0 || at >= a.rope_rows) status = MOA_STATUS_APPEND_RANGE;
+                axis_row[x] = a.cos_sin + (long long)at * rot;
+            }
+        }
     }
+    auto row_of = [&](int pair) {                          // pair: of the head
+        if constexpr (MODE == kByRow) return row;
+        const int x = (int)(a.axis_map[pair >> 5] >> (2 * (pair & 31))) & 3;
+        return x == 0 ? axis_row[0] : x == 1 ? axis_row[1] : x == 2 ? axis_row[2] : axis_row[3];
+    };
     if (status != 0) {
         if (part == 0 && run == 0) raise_status(status);
         return;
     }
 
     // This thread's share of the token's cosines and sines.
-    const int rot = a.rot, half = rot / 2;
     float cs[8], sn[8];
-    const float *row = a.cos_sin + pos * rot;
     if constexpr (TURN == kTurnChunks || TURN == kTurnPairs) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const bool in = turns && (TURN == kTurnChunks || 8 * part + i < half);
-            cs[i] = in ? row[8 * part + i] : 1.f;
-            sn[i] = in ? row[half + 8 * part + i] : 0.f;
+            const float *at = in ? row_of(8 * part + i) : nullptr;
+            cs[i] = in ? at[8 * part + i] : 1.f;
+            sn[i] = in ? at[half + 8 * part + i] : 0.f;
         }
     }
     unsigned char *dst = kind == 0 ? static_cast<unsigned char *>(a.q_out) + tok * a.o_st * ES
+                       : MODE == kRotateOnly ? static_cast<unsigned char *>(a.rk_out) + tok * a.rk_st * ES
                        : kind == 1 ? a.k_pool + page * a.k_sp + off * a.k_sr : a.v_pool + page * a.v_sp + off * a.v_sr;
-    const long long dst_step = kind == 0 ? D * ES : kind == 1 ? a.k_sh : a.v_sh;
+    const long long dst_step = kind == 0 || MODE == kRotateOnly ? D * ES : kind == 1 ? a.k_sh : a.v_sh;
     dst += h0 * dst_step;
     uint32_t *par = FMT == MOA_KV_INT4 && kind != 0 ? (kind == 1 ? a.kp : a.vp) + (page * a.h_kv + h0) * a.page_size + off : nullptr;
 
@@ -261,7 +289,8 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
                     const int d = 16 * part + i, pair = d < half ? d : d - half;
                     if (d < rot) {
                         float x = load_as_float(src, pair, DT), y = load_as_float(src, pair + half, DT);
-                        turn(x, y, row[pair], row[half + pair]);
+                        const float *at = row_of(pair);
+                        turn(x, y, at[pair], at[half + pair]);
                         (i < 8 ? lo[i] : hi[i - 8]) = d < half ? x : y;
                     }
                 }
