@@ -1256,8 +1256,29 @@ static void quick_division(int n, uint32_t *mul, int *sh)
     *mul = (uint32_t)(((1ULL << *sh) + n - 1) / n);
 }
 
+// Tensor maps over K and V for copies of 64 features x `box` rows: pools as (feature, row, head, page), tensors as (feature,
+// token, head, 1).
+struct PromptMaps { CUtensorMap k, v; };
+static bool make_prompt_map(CUtensorMap *m, const void *base, bool bf16, int d, int box, long long rows, int heads, int pages,
+                            const long long (&strides)[3])
+{
+    TmapEncodeFn enc = tmap_encoder();
+    if (!enc) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)rows, (cuuint64_t)heads, (cuuint64_t)pages};
+    cuuint64_t st[3];
+    for (int i = 0; i < 3; ++i) {
+        st[i] = (cuuint64_t)strides[i];
+        if (dims[i + 1] == 1) st[i] = 16;      // never stepped along: any legal stride
+        if (st[i] == 0 || st[i] >= (1ULL << 40)) return false;
+    }
+    cuuint32_t shape[4] = {64, (cuuint32_t)box, 1, 1}, estr[4] = {1, 1, 1, 1};
+    return enc(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(base), dims, st, shape, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <class C>
-static cudaError_t launch_prompt_cfg(const PromptArgs &a, int grid, cudaStream_t st)
+static cudaError_t launch_prompt_cfg(const PromptArgs &a, const PromptMaps &m, int grid, cudaStream_t st)
 {
     static bool attr_set[kMaxDevices] = {};
     int dev = 0;
@@ -1267,24 +1288,24 @@ static cudaError_t launch_prompt_cfg(const PromptArgs &a, int grid, cudaStream_t
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    launch_dependent(prompt_attn_kernel<C>, grid, C::THREADS, C::SMEM, st, a);
+    launch_dependent(prompt_attn_kernel<C>, grid, C::THREADS, C::SMEM, st, a, m.k, m.v);
     count_launch();
     return cudaGetLastError();
 }
 
 template <int D>
-static cudaError_t launch_prompt(int format, int dtype, bool paged, const PromptArgs &a, int grid, cudaStream_t st)
+static cudaError_t launch_prompt(int format, int dtype, bool paged, const PromptArgs &a, const PromptMaps &m, int grid, cudaStream_t st)
 {
     if (!paged) {
-        if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_BF16, true, D, false>>(a, grid, st);
-        return launch_prompt_cfg<PromptCfg<MOA_KV_F16, false, D, false>>(a, grid, st);
+        if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_BF16, true, D, false>>(a, m, grid, st);
+        return launch_prompt_cfg<PromptCfg<MOA_KV_F16, false, D, false>>(a, m, grid, st);
     }
     if (format == MOA_KV_INT4) {
-        if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_INT4, true, D, true>>(a, grid, st);
-        return launch_prompt_cfg<PromptCfg<MOA_KV_INT4, false, D, true>>(a, grid, st);
+        if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_INT4, true, D, true>>(a, m, grid, st);
+        return launch_prompt_cfg<PromptCfg<MOA_KV_INT4, false, D, true>>(a, m, grid, st);
     }
-    if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_BF16, true, D, true>>(a, grid, st);
-    return launch_prompt_cfg<PromptCfg<MOA_KV_F16, false, D, true>>(a, grid, st);
+    if (dtype == MOA_BF16) return launch_prompt_cfg<PromptCfg<MOA_KV_BF16, true, D, true>>(a, m, grid, st);
+    return launch_prompt_cfg<PromptCfg<MOA_KV_F16, false, D, true>>(a, m, grid, st);
 }
 
 // What both calls share once their own arguments are in `a`: sizes, scale, workspace, launch.
@@ -1310,7 +1331,18 @@ static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d
     unsigned long long tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
     if (tag == 0) tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
     a.ticket_tag = (tag << 20) | 1ull;
-    const cudaError_t e = d == 128 ? launch_prompt<128>(format, dtype, paged, a, grid, st) : launch_prompt<64>(format, dtype, paged, a, grid, st);
+    PromptMaps m = {};
+    if (format != MOA_KV_INT4) {               // (a whole tile of 128 rows there has to be; pages are multiples of a copy's rows)
+        const long long most = paged ? (long long)a.max_pages * a.page_size : a.tokens;
+        const int box = !paged || a.page_size % 32 == 0 ? 32 : a.page_size % 16 == 0 ? 16 : 0;
+        const long long ks[3] = {a.k_sr, a.k_sh, a.k_sp}, vs[3] = {a.v_sr, a.v_sh, a.v_sp};
+        const long long rows = paged ? a.page_size : a.tokens;
+        const int pages = paged ? a.num_pages : 1;
+        if (most >= 128 && box > 0 && make_prompt_map(&m.k, a.k, dtype == MOA_BF16, d, box, rows, a.h_kv, pages, ks) &&
+            make_prompt_map(&m.v, a.v, dtype == MOA_BF16, d, box, rows, a.h_kv, pages, vs))
+            a.box = box;
+    }
+    const cudaError_t e = d == 128 ? launch_prompt<128>(format, dtype, paged, a, m, grid, st) : launch_prompt<64>(format, dtype, paged, a, m, grid, st);
     if (e != cudaSuccess) return MOA_ERR_CUDA;
     g_last_path = MOA_PATH_PROMPT;
     return MOA_OK;

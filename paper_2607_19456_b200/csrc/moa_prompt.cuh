@@ -42,6 +42,7 @@ struct PromptArgs {
     int num_pages, page_size;
     uint32_t page_mul;               // row / page_size = row * page_mul >> page_sh, for rows below 2^31
     int page_sh;
+    int box;                         // rows of a tiled copy (16 or 32; a page is a multiple of them); 0: there are no tensor maps
     const int32_t *table;
     int max_pages, len_max;
     const int32_t *token_start;      // [batch + 1]; null: one token each (pools), one sequence (tensors)
@@ -62,8 +63,7 @@ template <int FMT_, bool BF_, int D_, bool PAGED_>
 struct PromptCfg {
     static constexpr int FMT = FMT_, D = D_;               // FMT: MOA_KV_INT4, or the 16-bit type
     static constexpr bool BF = BF_, PAGED = PAGED_, Q4 = FMT == MOA_KV_INT4;
-    static constexpr int THREADS = 512, TILE = 128;
-    static constexpr int HALVES = D / 64;                  // 128-byte column groups of a 16-bit row
+    static constexpr int THREADS = 384, TILE = 128;
     static constexpr int KV = TILE * D * 2;                // bytes of a tile of K or V in shared memory
     static constexpr int NST = D == 128 ? 2 : 4;           // stages of K and of V
     static constexpr int NPAR = 2 * NST;                   // parameters of 4-bit rows: twice as many tiles as stages
@@ -74,8 +74,9 @@ struct PromptCfg {
     static constexpr uint32_t OFF_PMAX = OFF_PAR + (Q4 ? NPAR * 2 * 128 * 8 : 0);      // [NPAR][4] largest scales of V
     static constexpr uint32_t OFF_NF = OFF_PMAX + (Q4 ? NPAR * 16 : 0);                // [2][D] first key with a V that is not finite
     static constexpr uint32_t OFF_ML = OFF_NF + 2 * D * 4; // [2][128] (m, l) of the slots
-    static constexpr uint32_t OFF_PLAN = OFF_ML + 2 * 128 * 8;
-    static constexpr uint32_t SMEM = OFF_PLAN + 512 * 8 + 1024;      // (1024: alignment of the base)
+    static constexpr uint32_t OFF_ROWS = OFF_ML + 2 * 128 * 8;      // [128] places of a tile's rows, K and V
+    static constexpr uint32_t OFF_PLAN = OFF_ROWS + (PAGED ? 128 * 16 : 0);
+    static constexpr uint32_t SMEM = OFF_PLAN + THREADS * 24 + 1024;      // (1024: alignment of the base)
     static constexpr float AHEAD = BF && !Q4 ? 8.0f : BF ? 8.0f : 4.0f;
     static constexpr float SHIFT = BF ? 0.0f : 11.0f;      // weights held in fp16 reach 2^15 (as in the single-query kernel)
     static constexpr int DEG = BF ? 3 : 4;
@@ -140,59 +141,65 @@ __device__ __forceinline__ void prompt_counts(const PromptArgs &a, const PromptS
     pieces = steps > T ? (steps + T - 1) / T : 1;
 }
 
-__device__ __forceinline__ long long prompt_block_sum(long long v, long long *scratch)
+// Sums of two numbers over the block, the same for every thread.
+__device__ __forceinline__ longlong2 prompt_block_sum(long long x, long long y, longlong2 *scratch)
 {
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    for (int off = 16; off >= 1; off >>= 1) {
+        x += __shfl_xor_sync(0xffffffffu, x, off);
+        y += __shfl_xor_sync(0xffffffffu, y, off);
+    }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = make_longlong2(x, y);
     __syncthreads();
-    long long t = 0;
-    for (int i = 0; i < (int)blockDim.x / 32; ++i) t += scratch[i];
+    longlong2 t = make_longlong2(0, 0);
+    for (int i = 0; i < (int)blockDim.x / 32; ++i) { t.x += scratch[i].x; t.y += scratch[i].y; }
     return t;
 }
 
-// Every CTA finds the same plan: rows of a unit, the most steps (a tile of keys for 256 rows) that a piece has, and in
-// pref[i] how many (items, slots) the sequences before group i have.
+// What a thread keeps of its sequences: how many (items, slots) come before them, and the sequence where it is only one.
+struct PromptGroup { int items, slots; PromptSeq s; };
+
+// Every CTA finds the same plan: rows of a unit and the most steps (a tile of keys for 256 rows) that a piece has.
 template <bool PAGED>
-__device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs &a, int2 *pref, long long *scratch, bool report)
+__device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs &a, PromptGroup *groups, longlong2 *scratch, bool report)
 {
     const int tid = threadIdx.x, nt = blockDim.x;
     const int gs = (a.batch + nt - 1) / nt;                // sequences of a group: one thread's
     const int b0 = min(tid * gs, a.batch), b1 = min(b0 + gs, a.batch);
     long long units = 0, work = 0;
-    int bad;
+    int bad, tiles, pieces;
+    PromptSeq s = {0, 0, 0, 0};
     for (int b = b0; b < b1; ++b) {
-        const PromptSeq s = prompt_seq<PAGED>(a, b, bad);
+        s = prompt_seq<PAGED>(a, b, bad);
         if (bad != 0 && report) raise_status(bad);
         if (s.n == 0) continue;
-        int tiles, pieces;
         prompt_counts<PAGED>(a, s, 256, 0x7fffffff, tiles, pieces);
         const long long rows = (long long)s.n * a.g;
         const int last = (prompt_sees(a, s, (int)rows - 1) + 127) >> 7, front = (prompt_sees(a, s, 0) + 127) >> 7;
         units += (long long)tiles * a.h_kv;
         work += rows <= 128 ? (long long)a.h_kv * ((last + 1) >> 1) : (long long)a.h_kv * tiles * (last + front + 1) / 2;
     }
-    units = prompt_block_sum(units, scratch);
-    work = prompt_block_sum(work, scratch);
+    const longlong2 sums = prompt_block_sum(units, work, scratch);
     const int grid = gridDim.x;
     PromptPlan p;
-    p.rows = units >= 2 * grid || work >= 32LL * grid ? 256 : 128;
-    long long T = (work + grid - 1) / grid;
+    p.rows = sums.x >= 2 * grid || sums.y >= 32LL * grid ? 256 : 128;
+    long long T = (sums.y + grid - 1) / grid;
     if (T < 6) T = 6;
     int items, slots;
-    for (;;) {
-        items = slots = 0;
+    for (;;) {                                             // (ends: with T long enough nothing is cut)
         long long all = 0;
+        items = slots = 0;
         for (int b = b0; b < b1; ++b) {
-            const PromptSeq s = prompt_seq<PAGED>(a, b, bad);
-            int tiles, pieces;
+            if (gs > 1) s = prompt_seq<PAGED>(a, b, bad);
             prompt_counts<PAGED>(a, s, p.rows, (int)min(T, 0x7fffffffLL), tiles, pieces);
             const long long c = (long long)tiles * pieces * a.h_kv;
             if (pieces > 1) { all += c; if (c <= a.slot_cap) slots += (int)c; }
             items += (int)min(c, 0x7fffffffLL);
         }
-        if (prompt_block_sum(all, scratch) <= a.slot_cap) break;
+        const longlong2 t = prompt_block_sum(all, items, scratch);
+        p.items = (int)t.y;
+        if (t.x <= a.slot_cap) break;
         T += T / 2;
     }
     p.step_max = (int)min(T, 0x7fffffffLL);
@@ -203,38 +210,34 @@ __device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs &a, int2 *pre
         const int x = __shfl_up_sync(0xffffffffu, inc.x, off), y = __shfl_up_sync(0xffffffffu, inc.y, off);
         if ((tid & 31) >= off) { inc.x += x; inc.y += y; }
     }
-    int2 *sums = reinterpret_cast<int2 *>(scratch);
+    int2 *const per_warp = reinterpret_cast<int2 *>(scratch + 16);
+    if ((tid & 31) == 31) per_warp[tid >> 5] = inc;
     __syncthreads();
-    if ((tid & 31) == 31) sums[tid >> 5] = inc;
-    __syncthreads();
-    int2 before = make_int2(0, 0), total = make_int2(0, 0);
-    for (int i = 0; i < nt / 32; ++i) {
-        if (i < (tid >> 5)) { before.x += sums[i].x; before.y += sums[i].y; }
-        total.x += sums[i].x;
-    }
-    pref[tid] = make_int2(before.x + inc.x - items, before.y + inc.y - slots);
-    p.items = total.x;
-    __syncthreads();
-    return p;
+    int2 before = make_int2(0, 0);
+    for (int i = 0; i < (tid >> 5); ++i) { before.x += per_warp[i].x; before.y += per_warp[i].y; }
+    groups[tid].items = before.x + inc.x - items;
+    groups[tid].slots = before.y + inc.y - slots;
+    groups[tid].s = s;
+    return p;                                              // (a block barrier follows)
 }
 
 // Item number `i`.  One thread.
 template <bool PAGED>
-__device__ __forceinline__ void prompt_item(const PromptArgs &a, const PromptPlan &p, const int2 *pref, int nt, int i, PromptItem &it)
+__device__ __forceinline__ void prompt_item(const PromptArgs &a, const PromptPlan &p, const PromptGroup *groups, int nt, int i, PromptItem &it)
 {
     it.rows = 0;
     if (i >= p.items) return;
-    int lo = 0, hi = nt;                                   // last group with pref <= i
+    int lo = 0, hi = nt;                                   // last group with items <= i
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (pref[mid].x <= i) lo = mid; else hi = mid;
+        if (groups[mid].items <= i) lo = mid; else hi = mid;
     }
     const int gs = (a.batch + nt - 1) / nt;
-    int at = pref[lo].x, slot = pref[lo].y, bad, tiles = 0, pieces = 0, b = lo * gs;
-    PromptSeq s;
+    int at = groups[lo].items, slot = groups[lo].slots, bad, tiles = 0, pieces = 0, b = lo * gs;
+    PromptSeq s = groups[lo].s;
     for (;; ++b) {
         if (b >= a.batch) return;                          // (not reached: the plan counted the item)
-        s = prompt_seq<PAGED>(a, b, bad);
+        if (gs > 1) s = prompt_seq<PAGED>(a, b, bad);
         prompt_counts<PAGED>(a, s, p.rows, p.step_max, tiles, pieces);
         const int c = tiles * pieces * a.h_kv;
         if (i < at + c) break;
@@ -275,6 +278,20 @@ __host__ __device__ constexpr uint32_t idesc_16(bool bf16, int M, int N, bool b_
     return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) |
            ((uint32_t)(M >> 4) << 24);
 }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int c0, int c1, int c2, int c3, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(tmap), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+        : "memory");
+}
+// One lane of a converged warp: the compiler knows the choice for uniform, and issues products from uniform registers.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 __device__ __forceinline__ void mma_16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -303,6 +320,12 @@ __device__ __forceinline__ float max_nan(float x, float y)
 {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float x, float y, float z)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
     return r;
 }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
@@ -348,14 +371,14 @@ __device__ __forceinline__ float2 exp2_pair(uint64_t x)
 }
 
 template <class C>
-__global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid_constant__ PromptArgs a)
+__global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
-    constexpr int D = C::D, NST = C::NST, HALVES = C::HALVES;
+    constexpr int D = C::D, NST = C::NST;
     constexpr bool BF = C::BF, Q4 = C::Q4, PAGED = C::PAGED;
     extern __shared__ unsigned char smem_prompt[];
-    __shared__ __align__(8) uint64_t bars[4 * NST + 8 + 2 + 4 + 4 + C::NPAR];
+    __shared__ __align__(8) uint64_t bars[4 * NST + 25 + C::NPAR];
     __shared__ PromptItem s_item[2];
-    __shared__ long long s_scratch[16];
+    __shared__ longlong2 s_scratch[16 + 8];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_last, s_nf[2];
     __shared__ float2 s_more[Q4 ? 2 : 1][Q4 ? 128 : 1];      // 4 bits: what joins the slots beside (m, l)
@@ -370,33 +393,37 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
     auto k_empty = [&](int i) { return bar(NST + i); };
     auto v_full = [&](int i) { return bar(2 * NST + i); };
     auto v_empty = [&](int i) { return bar(3 * NST + i); };
-    auto s_full = [&](int s) { return bar(4 * NST + s); };
-    auto p_full = [&](int s) { return bar(4 * NST + 2 + s); };
-    auto o_full = [&](int s) { return bar(4 * NST + 4 + s); };
-    const uint32_t q_full = bar(4 * NST + 6), q_empty = bar(4 * NST + 7);
-    auto item_full = [&](int i) { return bar(4 * NST + 8 + i); };
-    auto item_empty = [&](int i) { return bar(4 * NST + 10 + i); };
-    const uint32_t joined = bar(4 * NST + 12), parted = bar(4 * NST + 13), delivered = bar(4 * NST + 14), counted = bar(4 * NST + 15);
-    const uint32_t drained = bar(4 * NST + 16);
-    auto par_full = [&](int i) { return bar(4 * NST + 18 + i); };
+    constexpr int B0 = 4 * NST;
+    auto s_full = [&](int s) { return bar(B0 + s); };                        // scores of a tile
+    auto p_full = [&](int s, int h) { return bar(B0 + 2 + 2 * s + h); };     // weights of half a tile
+    auto half_done = [&](int s) { return bar(B0 + 6 + s); };                 // the first half is in the weighted sum
+    auto o_full = [&](int s) { return bar(B0 + 8 + s); };                    // the weighted sum of a unit
+    auto turn = [&](int s) { return bar(B0 + 10 + s); };
+    const uint32_t q_full = bar(B0 + 12), q_empty = bar(B0 + 13);
+    auto item_full = [&](int i) { return bar(B0 + 14 + i); };
+    auto item_empty = [&](int i) { return bar(B0 + 16 + i); };
+    const uint32_t joined = bar(B0 + 18), parted = bar(B0 + 19), delivered = bar(B0 + 20), counted = bar(B0 + 21), drained = bar(B0 + 22);
+    auto landed = [&](int w) { return bar(B0 + 23 + w); };                   // tiled copies of V that are looked at first
+    auto par_full = [&](int i) { return bar(B0 + 25 + i); };
 
     if (tid == 0) {
-        for (int i = 0; i < NST; ++i) { mbar_init(k_full(i), 4); mbar_init(k_empty(i), 1); mbar_init(v_full(i), 4); mbar_init(v_empty(i), 1); }
+        for (int i = 0; i < NST; ++i) { mbar_init(k_full(i), 2); mbar_init(k_empty(i), 2); mbar_init(v_full(i), 2); mbar_init(v_empty(i), 2); }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(s_full(s), 1); mbar_init(p_full(s), 4); mbar_init(o_full(s), 1);
-            mbar_init(item_full(s), 1); mbar_init(item_empty(s), 12);
+            mbar_init(s_full(s), 1); mbar_init(p_full(s, 0), 4); mbar_init(p_full(s, 1), 4); mbar_init(half_done(s), 1);
+            mbar_init(o_full(s), 1); mbar_init(turn(s), 1); mbar_init(landed(s), 1);
+            mbar_init(item_full(s), 1); mbar_init(item_empty(s), 11);
         }
-        mbar_init(q_full, 4); mbar_init(q_empty, 1);
-        mbar_init(joined, 8); mbar_init(parted, 8); mbar_init(delivered, 8); mbar_init(counted, 1); mbar_init(drained, 1);
-        for (int i = 0; i < C::NPAR; ++i) mbar_init(par_full(i), 4);
+        mbar_init(q_full, 2); mbar_init(q_empty, 2);
+        mbar_init(joined, 8); mbar_init(parted, 8); mbar_init(delivered, 8); mbar_init(counted, 1); mbar_init(drained, 2);
+        for (int i = 0; i < C::NPAR; ++i) mbar_init(par_full(i), 2);
         mbar_fence_init();
         s_abort = 0;
     }
-    if (warp == 12) tc::tmem_alloc(smem_u32(&s_tmem), 512);
+    if (warp == 10) tc::tmem_alloc(smem_u32(&s_tmem), 512);
     launch_dependents();
     grid_dependency_wait();
-    int2 *const pref = reinterpret_cast<int2 *>(smem + C::OFF_PLAN);
-    const PromptPlan plan = prompt_plan<PAGED>(a, pref, s_scratch, blockIdx.x == 0);
+    PromptGroup *const groups = reinterpret_cast<PromptGroup *>(smem + C::OFF_PLAN);
+    const PromptPlan plan = prompt_plan<PAGED>(a, groups, s_scratch, blockIdx.x == 0);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
@@ -404,120 +431,165 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
     auto t_s = [tmem](int s) -> uint32_t { return tmem + 128u * (uint32_t)s; };
     auto t_o = [tmem](int s) -> uint32_t { return tmem + 256u + (uint32_t)(s * D); };
 
-    if (warp >= 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-        if (warp == 12 && lane == 0) {
-            // ================= products =================
-            const uint32_t sQ = base + C::OFF_Q, sK = base + C::OFF_K, sV = base + C::OFF_V;
+    // 384 threads of 168 registers at launch: 256 x 200 + 128 x 104.
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        if (warp >= 10) {
+            // ================= products: a warp for each slot =================
+            // A thread that issues products is held until the tensor core has all but the last two of them, and whatever it does
+            // between two batches (a look at a barrier: 80 to 220 cycles of 1024) the tensor core waits for.  So each slot has
+            // a warp of its own, which has looked at everything when its turn comes.  Taking turns matters: without them both
+            // slots' products run mixed, end together, and the tensor core idles while both softmaxes run.
+            const int s = warp - 10;
+            const uint32_t sQ = base + C::OFF_Q, sK = base + C::OFF_K, sV = base + C::OFF_V, tS = t_s(s), tO = t_o(s);
             const uint32_t id_qk = tc::idesc_16(BF, 128, 128, false) | (a.negate ? 1u << 13 : 0u);
             constexpr uint32_t id_pv = tc::idesc_16(BF, 128, D, true);
             constexpr uint32_t hiword = 64u | (1u << 14) | (2u << 29);       // 1024 bytes between groups of 8 rows, 128-byte swizzle
-            uint32_t nk = 0, nv = 0, nq = 0, np[2] = {0, 0};
+            uint32_t nk = 0, nq = 0, np = 0, nt = 0;       // tiles of keys, items, own tiles, turns so far
             bool ok = true;
             for (uint32_t n = 0; ok; ++n) {
-                if (!wait_suspended(item_full(n & 1), (n >> 1) & 1, abort_flag)) { ok = false; break; }
-                const PromptItem it = s_item[n & 1];
+                if (!wait_warp(item_full(n & 1), (n >> 1) & 1, abort_flag)) { ok = false; break; }
+                const PromptItem &it = s_item[n & 1];
                 if (it.rows == 0) break;
-                const int cnt[2] = {prompt_steps(it, 0), prompt_steps(it, 1)};
-                int left = cnt[0] + cnt[1];
-                if (left > 0) {
-                    auto scores = [&](int s, int i) {
-                        const uint32_t kt = nk + (uint32_t)(it.pair ? 2 * i + s : i), st = kt % NST;
-                        if (!wait_suspended(k_full(st), (kt / NST) & 1, abort_flag)) return false;
+                const int cnt = prompt_steps(it, s), other = prompt_steps(it, s ^ 1), steps = max(cnt, other);
+                const bool pair = it.pair;
+                if (steps > 0) {
+                    ok = wait_warp(q_full, nq & 1, abort_flag);
+                    const uint32_t qa = sQ + (pair ? 0u : (uint32_t)(s * C::KV));
+                    if (cnt == 0 && lane == 0) tc::mbar_arrive(q_empty);
+                    // step i: the weighted sum of tile i, the scores of tile i + 1
+#pragma unroll 1
+                    for (int i = -1; ok && i < steps; ++i) {
+                        const uint32_t vt = nk + (uint32_t)(pair ? 2 * i + s : i), vst = vt % NST;
+                        const uint32_t kt = nk + (uint32_t)(pair ? 2 * (i + 1) + s : i + 1), kst = kt % NST;
+                        const bool sums = i >= 0 && i < cnt, more = i + 1 < cnt;
+                        const bool k_here = more && __all_sync(0xffffffffu, mbar_try_wait(k_full(kst), (kt / NST) & 1));
+                        if (sums) ok = wait_warp(v_full(vst), (vt / NST) & 1, abort_flag) && wait_warp(p_full(s, 0), np & 1, abort_flag);
+                        if (ok && (nt > 0 || s == 1)) ok = wait_warp(turn(s), (nt + (uint32_t)s - 1) & 1, abort_flag);
+                        ++nt;
+                        if (!ok) break;
                         tc::fence_after_sync();
-                        const uint32_t qa = sQ + (it.pair ? 0u : (uint32_t)(s * C::KV)), kb = sK + st * C::KV;
+                        if (sums) {
+                            const uint32_t vb = sV + vst * C::KV;
+                            if (tc::elect_one()) {
 #pragma unroll
-                        for (uint32_t ks = 0; ks < D / 16; ++ks) {
-                            const uint32_t off = (ks / 4) * 16384u + (ks % 4) * 32u;
-                            tc::mma_16_ss(t_s(s), tc::pack64(((qa + off) >> 4) | (1u << 16), hiword), tc::pack64(((kb + off) >> 4) | (1u << 16), hiword), id_qk, ks != 0);
-                        }
-                        tc::mma_commit(s_full(s));
-                        if (it.pair || s == 1) tc::mma_commit(k_empty(st));
-                        if (--left == 0) tc::mma_commit(q_empty);
-                        return true;
-                    };
-                    ok = wait_suspended(q_full, nq & 1, abort_flag);
-                    for (int s = 0; ok && s < 2; ++s) if (cnt[s] > 0) ok = scores(s, 0);
-                    const int steps = max(cnt[0], cnt[1]);
-                    for (int i = 0; ok && i < steps; ++i) {
-                        for (int s = 0; ok && s < 2; ++s) {
-                            if (i >= cnt[s]) continue;
-                            const uint32_t vt = nv + (uint32_t)(it.pair ? 2 * i + s : i), st = vt % NST;
-                            ok = wait_suspended(v_full(st), (vt / NST) & 1, abort_flag) && wait_suspended(p_full(s), np[s] & 1, abort_flag);
+                                for (uint32_t ks = 0; ks < 4; ++ks)
+                                    tc::mma_16_ts(tO, tS + 8u * ks, tc::pack64(((vb + ks * 2048u) >> 4) | (1024u << 16), hiword), id_pv, (i != 0 || ks != 0));
+                                tc::mma_commit(half_done(s));
+                            }
+                            __syncwarp();
+                            ok = wait_warp(p_full(s, 1), np & 1, abort_flag);
+                            ++np;
                             if (!ok) break;
-                            ++np[s];
                             tc::fence_after_sync();
-                            const uint32_t vb = sV + st * C::KV;
+                            if (tc::elect_one()) {
 #pragma unroll
-                            for (uint32_t ks = 0; ks < 8; ++ks)
-                                tc::mma_16_ts(t_o(s), t_s(s) + 8u * ks, tc::pack64(((vb + ks * 2048u) >> 4) | (1024u << 16), hiword), id_pv, (i != 0 || ks != 0));
-                            if (it.pair || s == 1) tc::mma_commit(v_empty(st));
-                            if (i + 1 < cnt[s]) ok = scores(s, i + 1);
-                            else tc::mma_commit(o_full(s));
+                                for (uint32_t ks = 4; ks < 8; ++ks)
+                                    tc::mma_16_ts(tO, tS + 8u * ks, tc::pack64(((vb + ks * 2048u) >> 4) | (1024u << 16), hiword), id_pv, 1);
+                                tc::mma_commit(v_empty(vst));
+                                if (pair || i >= other) tc::mma_commit(v_empty(vst));      // (for the other slot)
+                                if (!more) tc::mma_commit(o_full(s));
+                            }
+                            __syncwarp();
                         }
+                        if (more) {
+                            if (!k_here) {
+                                ok = wait_warp(k_full(kst), (kt / NST) & 1, abort_flag);
+                                if (!ok) break;
+                                tc::fence_after_sync();
+                            }
+                            const uint32_t kb = sK + kst * C::KV;
+                            if (tc::elect_one()) {
+#pragma unroll
+                                for (uint32_t ks = 0; ks < D / 16; ++ks) {
+                                    const uint32_t off = (ks / 4) * 16384u + (ks % 4) * 32u;
+                                    tc::mma_16_ss(tS, tc::pack64(((qa + off) >> 4) | (1u << 16), hiword), tc::pack64(((kb + off) >> 4) | (1u << 16), hiword), id_qk, ks != 0);
+                                }
+                                tc::mma_commit(s_full(s));
+                                tc::mma_commit(k_empty(kst));
+                                if (pair || i + 1 >= other) tc::mma_commit(k_empty(kst));
+                                if (i + 2 == cnt) tc::mma_commit(q_empty);
+                            }
+                            __syncwarp();
+                        }
+                        if (lane == 0) tc::mbar_arrive(turn(s ^ 1));
                     }
                     nk += (uint32_t)(it.e1 - it.t0);
-                    nv += (uint32_t)(it.e1 - it.t0);
                     ++nq;
                 }
-                tc::mbar_arrive(item_empty(n & 1));
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(item_empty(n & 1));
             }
             if (!ok) {                                     // leave nothing in flight
-                tc::mma_commit(drained);
-                mbar_wait_bounded(drained, 0);
+                if (tc::elect_one()) tc::mma_commit(drained);
+                __syncwarp();
+                mbar_wait_bounded(drained, 0, 1u << 16);
             }
-        }
-    } else if (warp >= 8) {
+        } else {
         // ================= copies =================
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        const int w = warp - 8;
+        const int w = warp - 8;                            // of rows 64 w .. 64 w + 63 of a tile
         constexpr int CPR = D / 8, RPI = 32 / CPR;         // 16-byte chunks of a 16-bit row; rows of a warp's copy
         const int chunk = lane % CPR, rsub = lane / CPR;
         const uint32_t col = (uint32_t)(chunk >> 3) * 16384u;
-        uint32_t nk = 0, nv = 0, nq = 0;
+        uint32_t nk = 0, nq = 0;
         bool ok = true;
-        // Copies under way, oldest first: the barrier that their arrival is told to, and for V whether to look for values that are not finite.
-        uint32_t pend_bar[2];
-        int pend_chk[2], pending = 0;                      // pend_chk: -1, or 2 * tile of keys + set of the item
-        uint32_t pend_at[2];
+        // The copies under way before the ones being made: the barrier that their arrival is told to, and for tiles of V that
+        // not every row of the unit sees whole, what to look for: rows behind `pend_rows` (zeroed), and values that are not
+        // finite (zeroed, and noted: the rows that see them become NaN at the unit's end).
+        uint32_t pend_bar = 0, pend_at = 0, lands = 0;
+        int pend_tile = -1, pend_rows = 0, pend_set = 0;   // pend_tile: of keys, -1: nothing to look for
+        bool pending = false, pend_tma = false;
         auto dst_of = [&](int r) -> uint32_t { return col + (uint32_t)r * 128u + (uint32_t)(((chunk & 7) ^ (r & 7)) << 4); };
-        auto look = [&](uint32_t at, int tile, int nf_set) {      // own chunks of a tile of V: zero what is not finite, and note where
-            for (int i = 0; i < 32 / RPI; ++i) {
-                const int r = 32 * w + RPI * i + rsub;
-                const uint32_t p = at + dst_of(r);
+        auto look = [&]() {
+            // a product with 0 is NaN where a value is not finite: one fused multiply-add for two values
+            uint32_t sum = 0;
+#pragma unroll 8
+            for (int i = 0; i < 64 / RPI; ++i) {
+                const int r = 64 * w + RPI * i + rsub;
+                const uint32_t p = pend_at + dst_of(r);
                 uint32_t u[4];
+                if (r >= pend_rows) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(p), "r"(0u) : "memory");
                 asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(p) : "memory");
-                bool any = false;
 #pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (BF) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(u[e]), "r"(0u));
+                    else asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(u[e]), "r"(0u));
+                }
+            }
+            if ((sum & 0x7fff7fffu) == 0u) return;
+            for (int i = 0; i < 64 / RPI; ++i) {
+                const int r = 64 * w + RPI * i + rsub;
+                const uint32_t p = pend_at + dst_of(r);
                 for (int e = 0; e < 8; ++e) {
-                    const uint32_t x = u[e >> 1] >> (16 * (e & 1)), ex = BF ? 0x7f80u : 0x7c00u;
-                    if ((x & ex) == ex) {
-                        any = true;
-                        u[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
-                        atomicMin(reinterpret_cast<int *>(smem + C::OFF_NF) + nf_set * D + chunk * 8 + e, tile * 128 + r);
-                        s_nf[nf_set] = 1;
+                    uint16_t x;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(p + 2 * e) : "memory");
+                    if ((x & (BF ? 0x7f80 : 0x7c00)) == (BF ? 0x7f80 : 0x7c00)) {
+                        atomicMin(reinterpret_cast<int *>(smem + C::OFF_NF) + pend_set * D + chunk * 8 + e, pend_tile * 128 + r);
+                        s_nf[pend_set] = 1;
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(p + 2 * e), "h"((uint16_t)0) : "memory");
                     }
                 }
-                if (any) asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
             }
         };
-        auto retire = [&]() {                              // the oldest has arrived
-            if (pending == 2) cp_wait<1>(); else cp_wait<0>();
-            if (pend_chk[0] >= 0) look(pend_at[0], pend_chk[0] >> 1, pend_chk[0] & 1);
+        auto retire = [&]() {                              // they have arrived
+            if (pend_tma) { wait_warp(landed(w), lands & 1, abort_flag); ++lands; }
+            if (pend_tile >= 0) look();
             tc::fence_async_smem();
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(pend_bar[0]);
-            pend_bar[0] = pend_bar[1]; pend_chk[0] = pend_chk[1]; pend_at[0] = pend_at[1];
-            --pending;
+            if (lane == 0) tc::mbar_arrive(pend_bar);
+            pending = false;
         };
-        auto push = [&](uint32_t b, uint32_t at, int chk) {
+        auto drain = [&]() { if (pending) { cp_wait<0>(); retire(); } };
+        // What has been issued is what is under way from now on; what was before is waited for.
+        auto push = [&](uint32_t b, uint32_t at, int tile, int rows, int set, bool tma) {
             cp_commit();
-            pend_bar[pending] = b; pend_at[pending] = at; pend_chk[pending] = chk;
-            if (++pending == 2) retire();
+            if (pending) { cp_wait<1>(); retire(); }
+            pend_bar = b; pend_at = at; pend_tile = tile; pend_rows = rows; pend_set = set; pend_tma = tma;
+            pending = true;
         };
         auto wait_free = [&](uint32_t b, uint32_t parity) {
             if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
-            while (pending > 0) retire();                  // what this waits for may need them
+            drain();                  // what this waits for may need them
             return wait_warp(b, parity, abort_flag);
         };
 
@@ -539,7 +611,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             i = (int)min((unsigned)gridDim.x + j, 0x7fffffffu);
                         }
                     }
-                    prompt_item<PAGED>(a, plan, pref, C::THREADS, i, s_item[set]);
+                    prompt_item<PAGED>(a, plan, groups, C::THREADS, i, s_item[set]);
                     s_nf[set] = 0;
                 }
                 for (int f = lane; f < D; f += 32) reinterpret_cast<int *>(smem + C::OFF_NF)[set * D + f] = 0x7fffffff;
@@ -548,70 +620,100 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             }
             ok = wait_free(item_full(set), (n >> 1) & 1);
             if (!ok) break;
-            const PromptItem it = s_item[set];
+            const PromptItem &it = s_item[set];
             if (it.rows == 0) break;
             const int tiles = it.e1 - it.t0;
             if (prompt_steps(it, 0) + prompt_steps(it, 1) > 0) {
                 PromptSeq sq;
                 sq.first = it.first; sq.past = it.past; sq.len = it.len; sq.n = 0;
                 const int sees = prompt_sees(a, sq, it.row0 + it.rows - 1);     // rows behind are not read
-                // the addresses of this lane's row of a tile: row 32 w + lane
-                const unsigned char *ka = nullptr, *va = nullptr;
-                uint32_t k_pair = 0, v_pair = 0;
-                bool row_ok = false, row_bad = false;
-                auto locate = [&](int t) {
-                    const long long row = (long long)t * 128 + 32 * w + lane;
-                    row_ok = row < sees;
-                    row_bad = false;
-                    ka = a.k; va = a.v;
-                    if (!row_ok) return;
-                    if (PAGED) {
-                        const int pi = (int)(((unsigned long long)(uint32_t)row * a.page_mul) >> a.page_sh), off = (int)row - pi * a.page_size;
-                        const int page = a.table[(long long)it.table_row * a.max_pages + pi];
-                        if (page < 0 || page >= a.num_pages) { row_bad = true; row_ok = false; raise_status(MOA_STATUS_PAGE_RANGE); return; }
-                        ka += page * a.k_sp + it.head * a.k_sh + off * a.k_sr;
-                        va += page * a.v_sp + it.head * a.v_sh + off * a.v_sr;
-                        if (Q4) {
-                            const long long at = ((long long)page * a.h_kv + it.head) * a.page_size + off;
-                            k_pair = a.kp[at]; v_pair = a.vp[at];
-                        }
-                    } else {
-                        ka += it.head * a.k_sh + (it.first + row) * a.k_sr;
-                        va += it.head * a.v_sh + (it.first + row) * a.v_sr;
+                // Where the rows of a tile are: a lane finds those of rows 64 w + lane and 32 further, and in pools tells them to the warp
+                // through shared memory (an odd address: there is no such row).  The pages' numbers are read a tile ahead.
+                uint2 *const places = reinterpret_cast<uint2 *>(smem + C::OFF_ROWS) + 128 * w;     // [64 rows][K, V]
+                uint32_t k_pair[2] = {}, v_pair[2] = {};
+                int page_next[2] = {-1, -1};
+                bool row_ok[2] = {}, row_bad[2] = {};
+                auto page_index = [&](long long row) { return (int)(((unsigned long long)(uint32_t)row * a.page_mul) >> a.page_sh); };
+                auto look_up = [&](int t) {
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const long long row = (long long)t * 128 + 64 * w + 32 * g + lane;
+                        if (PAGED && row < sees) page_next[g] = a.table[(long long)it.table_row * a.max_pages + page_index(row)];
                     }
                 };
-                auto copy_rows = [&](uint32_t at, const unsigned char *mine, bool is_k) {
-#pragma unroll 4
-                    for (int i = 0; i < 32 / RPI; ++i) {
-                        const int from = RPI * i + rsub;
-                        const unsigned char *p = reinterpret_cast<const unsigned char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
-                        const int good = __shfl_sync(0xffffffffu, (int)row_ok, from);
-                        cp16(at + dst_of(32 * w + from), p + 16 * chunk, good != 0);
+                auto locate = [&](int t, bool last) {
+                    if (!PAGED) return;
+                    const int pages[2] = {page_next[0], page_next[1]};
+                    if (!last) look_up(t + 1);
+                    __syncwarp();                          // (the tile before is through)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const long long row = (long long)t * 128 + 64 * w + 32 * g + lane;
+                        const int page = pages[g];
+                        row_ok[g] = row < sees;
+                        row_bad[g] = row_ok[g] && (page < 0 || page >= a.num_pages);
+                        if (row_bad[g]) { row_ok[g] = false; raise_status(MOA_STATUS_PAGE_RANGE); }
+                        const unsigned char *ka = a.k + 1, *va = a.v + 1;
+                        if (row_ok[g]) {
+                            const int off = (int)row - page_index(row) * a.page_size;
+                            ka = a.k + (page * a.k_sp + it.head * a.k_sh + off * a.k_sr);
+                            va = a.v + (page * a.v_sp + it.head * a.v_sh + off * a.v_sr);
+                            if (Q4) {
+                                const long long at = ((long long)page * a.h_kv + it.head) * a.page_size + off;
+                                k_pair[g] = a.kp[at]; v_pair[g] = a.vp[at];
+                            }
+                        }
+                        *reinterpret_cast<uint4 *>(places + 2 * (32 * g + lane)) =
+                            make_uint4((uint32_t)(uintptr_t)ka, (uint32_t)((uintptr_t)ka >> 32), (uint32_t)(uintptr_t)va, (uint32_t)((uintptr_t)va >> 32));
                     }
-                    if (PAGED && is_k && __any_sync(0xffffffffu, row_bad)) {      // a page that does not exist: its scores are NaN
-                        cp_commit(); cp_wait<0>(); __syncwarp();
-                        for (int i = 0; i < 32 / RPI; ++i) {
+                    __syncwarp();
+                };
+                auto place = [&](int r, bool is_k) {
+                    const uint2 u = places[2 * r + (is_k ? 0 : 1)];
+                    return ((unsigned long long)u.y << 32) | u.x;
+                };
+                auto copy_rows = [&](uint32_t at, int t, bool is_k) {
+                    if (PAGED) {
+#pragma unroll 8
+                        for (int i = 0; i < 64 / RPI; ++i) {
                             const int from = RPI * i + rsub;
-                            if (__shfl_sync(0xffffffffu, (int)row_bad, from))
-                                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at + dst_of(32 * w + from)), "r"(0x7fff7fffu) : "memory");
+                            const unsigned long long p = place(from, is_k);
+                            cp16(at + dst_of(64 * w + from), reinterpret_cast<const unsigned char *>(p & ~1ull) + 16 * chunk, (p & 1) == 0);
+                        }
+                        if (is_k && __any_sync(0xffffffffu, row_bad[0] || row_bad[1])) {      // a page that does not exist: its scores are NaN
+                            cp_commit(); cp_wait<0>(); __syncwarp();
+                            for (int i = 0; i < 64 / RPI; ++i) {
+                                const int from = RPI * i + rsub;
+                                const int b0 = __shfl_sync(0xffffffffu, (int)row_bad[0], from & 31), b1 = __shfl_sync(0xffffffffu, (int)row_bad[1], from & 31);
+                                if (from < 32 ? b0 : b1)
+                                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at + dst_of(64 * w + from)), "r"(0x7fff7fffu) : "memory");
+                            }
+                        }
+                    } else {
+                        const long long first = (long long)t * 128 + 64 * w + rsub;
+                        const long long sr = is_k ? a.k_sr : a.v_sr;
+                        const unsigned char *p = (is_k ? a.k + it.head * a.k_sh : a.v + it.head * a.v_sh) + (it.first + first) * sr + 16 * chunk;
+                        const int left = sees - (int)first;          // rows from this lane's first on
+#pragma unroll 8
+                        for (int i = 0; i < 64 / RPI; ++i, p += RPI * sr) {
+                            const bool in = RPI * i < left;
+                            cp16(at + dst_of(64 * w + RPI * i + rsub), in ? p : a.k, in);
                         }
                     }
                 };
                 // 4-bit rows: a code c becomes c - 8 (exact), two to a register; the row's scale and least value go to the softmax.
-                auto unpack_rows = [&](uint32_t at, const unsigned char *mine) {
-                    constexpr int CP4 = D / 32;            // 16-byte chunks of a row of codes: 32 codes
-                    constexpr int NIT = CP4;               // 32 rows * CP4 chunks / 32 lanes
-                    uint4 x[NIT];
+                constexpr int CP4 = D / 32;                // 16-byte chunks of a row of codes, 32 codes each
+                auto fetch_rows = [&](uint4 (&x)[CP4], int g, bool is_k) {
 #pragma unroll
-                    for (int i = 0; i < NIT; ++i) {
-                        const int from = i * (32 / CP4) + lane / CP4;
-                        const unsigned char *p = reinterpret_cast<const unsigned char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
-                        const int good = __shfl_sync(0xffffffffu, (int)row_ok, from);
-                        x[i] = good ? *reinterpret_cast<const uint4 *>(p + 16 * (lane % CP4)) : make_uint4(0, 0, 0, 0);
+                    for (int i = 0; i < CP4; ++i) {
+                        const unsigned long long p = place(32 * g + i * (32 / CP4) + lane / CP4, is_k);
+                        x[i] = (p & 1) == 0 ? *reinterpret_cast<const uint4 *>(p + 16 * (lane % CP4)) : make_uint4(0, 0, 0, 0);
                     }
+                };
+                auto unpack_rows = [&](uint32_t at, int g, const uint4 (&x)[CP4]) {
 #pragma unroll
-                    for (int i = 0; i < NIT; ++i) {
-                        const int r = 32 * w + i * (32 / CP4) + lane / CP4;
+                    for (int i = 0; i < CP4; ++i) {
+                        const int r = 64 * w + 32 * g + i * (32 / CP4) + lane / CP4;
                         const uint32_t c4[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -641,73 +743,112 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                     ++nq;
                     const int parts = it.pair ? 1 : 2;
                     for (int s = 0; s < parts; ++s) {
-                        const int r = 128 * s + 32 * w + lane;              // this lane finds one row's place
-                        const bool in = r < it.rows;
-                        const int row = it.row0 + (in ? r : 0), tok = div_g(a, row);
-                        const unsigned char *mine = a.q + (long long)(it.first + tok) * a.q_st + ((long long)it.head * a.g + (row - tok * a.g)) * (D * 2);
-#pragma unroll 4
-                        for (int i = 0; i < 32 / RPI; ++i) {
-                            const int from = RPI * i + rsub;
-                            const unsigned char *p = reinterpret_cast<const unsigned char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
-                            const int good = __shfl_sync(0xffffffffu, (int)in, from);
-                            cp16(base + C::OFF_Q + s * C::KV + dst_of(32 * w + from), p + 16 * chunk, good != 0);
+#pragma unroll 8
+                        for (int i = 0; i < 64 / RPI; ++i) {
+                            const int r = 64 * w + RPI * i + rsub, at = 128 * s + r;
+                            const bool in = at < it.rows;
+                            const int row = it.row0 + at, tok = div_g(a, row);
+                            const unsigned char *p = a.q + (long long)(it.first + tok) * a.q_st + ((long long)it.head * a.g + (row - tok * a.g)) * (D * 2) + 16 * chunk;
+                            cp16(base + C::OFF_Q + s * C::KV + dst_of(r), in ? p : a.q, in);
                         }
                     }
-                    push(q_full, 0, -1);
-                    if (Q4) retire();
+                    push(q_full, 0, -1, 0, 0, false);
+                    drain();
                 };
+                look_up(it.t0);
+                uint4 codes[2][CP4];
                 for (int t = 0; ok && t < tiles; ++t) {
                     const uint32_t st = nk % NST;
-                    locate(it.t0 + t);
+                    // Tiled copies where there are tensor maps: this warp's 64 rows as 64 features x 16 or 32 rows each, as far as
+                    // rows are seen.  (Rows of a tensor behind the sequence come along; their scores are masked, their V is zeroed.)
+                    if (!Q4 && a.box > 0) {
+                        const int pages[2] = {page_next[0], page_next[1]};
+                        const int row = (it.t0 + t) * 128 + 64 * w, r0 = lane / (D / 64) * a.box, half = lane % (D / 64);      // the copy that this lane makes
+                        const bool copies = r0 < 64 && row + r0 < sees;
+                        const int p0 = __shfl_sync(0xffffffffu, pages[0], r0 & 31), p1 = __shfl_sync(0xffffffffu, pages[1], r0 & 31);
+                        const int mine = r0 < 32 ? p0 : p1;
+                        if (!PAGED || !__any_sync(0xffffffffu, copies && (mine < 0 || mine >= a.num_pages))) {
+                            if (PAGED && t + 1 < tiles) look_up(it.t0 + t + 1);
+                            const int c1 = PAGED ? row + r0 - page_index(row + r0) * a.page_size : it.first + row + r0, c3 = PAGED ? mine : 0;
+                            const uint32_t to = (uint32_t)(half * 16384 + (64 * w + r0) * 128);
+                            const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, copies)) * (uint32_t)a.box * 128u;
+                            ok = nk < NST || wait_free(k_empty(st), (nk / NST - 1) & 1);
+                            if (!ok) break;
+                            if (lane == 0) mbar_expect_tx(k_full(st), bytes);
+                            __syncwarp();
+                            if (copies) tc::tma_load_4d(base + C::OFF_K + st * C::KV + to, &map_k, 64 * half, c1, it.head, c3, k_full(st));
+                            if (t == 0) { copy_q(); if (!ok) break; }
+                            ok = nk < NST || wait_free(v_empty(st), (nk / NST - 1) & 1);
+                            if (!ok) break;
+                            const bool looks = (it.t0 + t + 1) * 128LL > it.least;
+                            const uint32_t vd = base + C::OFF_V + st * C::KV, to_bar = looks ? landed(w) : v_full(st);
+                            if (looks) drain();
+                            if (lane == 0) mbar_expect_tx(to_bar, bytes);
+                            __syncwarp();
+                            if (copies) tc::tma_load_4d(vd + to, &map_v, 64 * half, c1, it.head, c3, to_bar);
+                            if (looks) push(v_full(st), vd, it.t0 + t, sees - (it.t0 + t) * 128, set, true);
+                            ++nk;
+                            continue;
+                        }
+                    }                                      // (a page that does not exist: row by row)
+                    locate(it.t0 + t, t + 1 == tiles);
+                    if constexpr (Q4) { fetch_rows(codes[0], 0, true); fetch_rows(codes[1], 1, true); }
                     ok = nk < NST || wait_free(k_empty(st), (nk / NST - 1) & 1);
                     if (!ok) break;
                     const uint32_t kd = base + C::OFF_K + st * C::KV, vd = base + C::OFF_V + st * C::KV;
-                    if (Q4) {
+                    if constexpr (Q4) {
                         // parameters: the softmax of the tile that had this place is done (its V is used up, NPAR / 2 tiles ago at the least)
                         const uint32_t ps = nk % C::NPAR;
-                        const float2 kf = unpack16<false>(k_pair), vf = unpack16<false>(v_pair);
-                        float2 *par = reinterpret_cast<float2 *>(smem + C::OFF_PAR) + ps * 256 + 32 * w + lane;
-                        const float nan = __uint_as_float(0x7fffffffu);
-                        par[0] = row_bad ? make_float2(nan, nan) : row_ok ? make_float2(kf.x, fmaf(8.f, kf.x, kf.y)) : make_float2(0.f, 0.f);
-                        par[128] = row_ok ? make_float2(vf.x, fmaf(8.f, vf.x, vf.y)) : make_float2(0.f, 0.f);
-                        float top = row_ok ? vf.x : 0.f;
 #pragma unroll
-                        for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                        if (lane == 0) reinterpret_cast<float *>(smem + C::OFF_PMAX)[ps * 4 + w] = top;
+                        for (int g = 0; g < 2; ++g) {
+                            const float2 kf = unpack16<false>(k_pair[g]), vf = unpack16<false>(v_pair[g]);
+                            float2 *par = reinterpret_cast<float2 *>(smem + C::OFF_PAR) + ps * 256 + 64 * w + 32 * g + lane;
+                            const float nan = __uint_as_float(0x7fffffffu);
+                            par[0] = row_bad[g] ? make_float2(nan, nan) : row_ok[g] ? make_float2(kf.x, fmaf(8.f, kf.x, kf.y)) : make_float2(0.f, 0.f);
+                            par[128] = row_ok[g] ? make_float2(vf.x, fmaf(8.f, vf.x, vf.y)) : make_float2(0.f, 0.f);
+                            float top = row_ok[g] ? vf.x : 0.f;
+#pragma unroll
+                            for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                            if (lane == 0) reinterpret_cast<float *>(smem + C::OFF_PMAX)[ps * 4 + 2 * w + g] = top;
+                        }
                         __syncwarp();
                         if (lane == 0) tc::mbar_arrive(par_full(ps));
-                        unpack_rows(kd, ka);
+                        unpack_rows(kd, 0, codes[0]);
+                        fetch_rows(codes[0], 0, false);
+                        unpack_rows(kd, 1, codes[1]);
+                        fetch_rows(codes[1], 1, false);
                         tc::fence_async_smem();
                         __syncwarp();
                         if (lane == 0) tc::mbar_arrive(k_full(st));
                     } else {
-                        copy_rows(kd, ka, true);
-                        push(k_full(st), 0, -1);
+                        copy_rows(kd, it.t0 + t, true);
+                        push(k_full(st), 0, -1, 0, 0, false);
                     }
-                    ++nk;
                     if (t == 0) { copy_q(); if (!ok) break; }
-                    ok = nv < NST || wait_free(v_empty(st), (nv / NST - 1) & 1);
+                    ok = nk < NST || wait_free(v_empty(st), (nk / NST - 1) & 1);
                     if (!ok) break;
-                    if (Q4) {
-                        unpack_rows(vd, va);
+                    if constexpr (Q4) {
+                        unpack_rows(vd, 0, codes[0]);
+                        unpack_rows(vd, 1, codes[1]);
                         tc::fence_async_smem();
                         __syncwarp();
                         if (lane == 0) tc::mbar_arrive(v_full(st));
                     } else {
-                        copy_rows(vd, va, false);
-                        push(v_full(st), vd, a.causal && (it.t0 + t + 1) * 128LL > it.least ? 2 * (it.t0 + t) + set : -1);
+                        copy_rows(vd, it.t0 + t, false);
+                        push(v_full(st), vd, (it.t0 + t + 1) * 128LL > it.least ? it.t0 + t : -1, 128, set, false);
                     }
-                    ++nv;
+                    ++nk;
                 }
-                while (pending > 0) retire();              // the next item's number takes a while
+                drain();              // the next item's number takes a while
             }
             if (w != 0 && ok) { __syncwarp(); if (lane == 0) tc::mbar_arrive(item_empty(set)); }
         }
-        while (pending > 0) retire();
+        drain();
         cp_wait<0>();
+        }
     } else {
         // ================= softmax =================
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const int s = warp >> 2, wq = warp & 3, row = 32 * wq + lane;       // slot; row of the slot = tensor memory lane
         const uint32_t lane_at = (uint32_t)(32 * wq) << 16;
         const uint32_t tS = t_s(s) + lane_at, tO = t_o(s) + lane_at;
@@ -717,7 +858,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
         for (uint32_t n = 0; ok; ++n) {
             ok = wait_warp(item_full(n & 1), (n >> 1) & 1, abort_flag);
             if (!ok) break;
-            const PromptItem it = s_item[n & 1];
+            const PromptItem &it = s_item[n & 1];
             if (it.rows == 0) break;
             const int cnt = prompt_steps(it, s), other = prompt_steps(it, s ^ 1);
             const int r = row + (it.pair ? 0 : 128 * s);   // row of the unit
@@ -757,97 +898,117 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                 }
                 if (!dead) {
                     tc::fence_after_sync();
-                    uint32_t x[4][32];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tc::tmem_ld32(tS + 32 * c, x[c]);
-                    tc::tmem_ld_wait();
                     float2 *const par = reinterpret_cast<float2 *>(smem + C::OFF_PAR) + ps * 256;
-                    if (Q4) {                              // scale * <q, c - 8> + (least + 8 scale) * sum(q)
-#pragma unroll
-                        for (int c = 0; c < 128; ++c) {
-                            const float2 k2 = par[c];
-                            x[c >> 5][c & 31] = __float_as_uint(fmaf(k2.x, __uint_as_float(x[c >> 5][c & 31]), k2.y * sumq));
-                        }
-                    }
                     const int vis = lim - t * 128;         // keys of this tile that the row sees
                     const bool masked = !__all_sync(0xffffffffu, vis >= 128);
-                    if (masked) {
+                    const uint64_t qs2 = pack2f(a.qscale, a.qscale);
+                    const bool scales = Q4 && !BF;
 #pragma unroll
-                        for (int c = 0; c < 128; ++c)
-                            if (c >= vis) x[c >> 5][c & 31] = 0xff800000u;
-                    }
-                    float mx[4];
+                    for (int h = 0; h < 2; ++h) {          // 64 keys at a time: the first half's product runs under the second's weights
+                        uint32_t x[64];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float u = __uint_as_float(x[c][0]);
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t z[32];
+                            tc::tmem_ld32(tS + 64 * h + 32 * c, z);
 #pragma unroll
-                        for (int e = 1; e < 32; ++e) u = max_nan(u, __uint_as_float(x[c][e]));
-                        mx[c] = u;
-                    }
-                    float top = max_nan(max_nan(mx[0], mx[1]), max_nan(mx[2], mx[3])) * a.qscale;
-                    if (masked && vis <= 0) top = -INFINITY;                 // (a scale of 0 would make it NaN)
-                    // The reference moves for a row where a score passes it by AHEAD; for all rows of the warp then.
-                    float sig_new = sigma;
-                    if (Q4 && !BF) {
-                        const float4 u = *reinterpret_cast<const float4 *>(smem + C::OFF_PMAX + ps * 16);
-                        const float st = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
-                        if (st > sigma) sig_new = __uint_as_float((__float_as_uint(st) + 0x007fffffu) & 0x7f800000u);
-                    }
-                    if (__any_sync(0xffffffffu, !(top <= m + C::AHEAD) && !(top == -INFINITY)) || (Q4 && !BF && sig_new != sigma)) {
-                        float mn = max_nan(m, top);
-                        if (mn == INFINITY) mn = __uint_as_float(0x7fffffffu);      // (infinity less itself: the row is NaN)
-                        float f = mn == m ? 1.f : m == -INFINITY && mn == mn ? 0.f : fast_exp2(m - mn);
-                        l *= f; lm *= f;
-                        if (Q4 && !BF) { if (sigma > 0.f) f *= sigma / sig_new; sigma = sig_new; }
-                        m = mn;
-                        if (i > 0) {
-#pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                uint32_t o[32];
-                                tc::tmem_ld32(tO + c, o);
-                                tc::tmem_ld_wait();
+                            for (int e = 0; e < 32; ++e) x[32 * c + e] = z[e];
+                        }
+                        tc::tmem_ld_wait();
+                        if (Q4) {                          // scale * <q, c - 8> + (least + 8 scale) * sum(q)
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                tc::tmem_st32(tO + c, o);
+                            for (int e = 0; e < 64; ++e) {
+                                const float2 k2 = par[64 * h + e];
+                                x[e] = __float_as_uint(fmaf(k2.x, __uint_as_float(x[e]), k2.y * sumq));
                             }
                         }
-                    }
-                    const float ref = m == -INFINITY ? 0.f : m;
-                    const uint64_t qs2 = pack2f(a.qscale, a.qscale), nm2 = pack2f(C::SHIFT - ref, C::SHIFT - ref);
-                    uint64_t sum = pack2f(0.f, 0.f), summ = pack2f(0.f, 0.f);
-                    const float isig = Q4 && !BF ? 1.f / fmaxf(sigma, 1e-30f) : 1.f;
+                        if (masked) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t pk[16];
+                            for (int e = 0; e < 64; ++e)
+                                if (64 * h + e >= vis) x[e] = 0xff800000u;
+                        }
+                        float sig_new = sigma;
+                        if (scales && h == 0) {
+                            const float4 u = *reinterpret_cast<const float4 *>(smem + C::OFF_PMAX + ps * 16);
+                            const float st = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
+                            if (st > sigma) sig_new = __uint_as_float((__float_as_uint(st) + 0x007fffffu) & 0x7f800000u);
+                        }
+                        // The weights by the reference as it is, and the maximum beside them.  Where a score passes the
+                        // reference by AHEAD, it moves (for every row of the warp), and the weights are made again.
+                        uint64_t sum[2], summ;
+                        for (bool again = false;; again = true) {
+                            const float ref = m == -INFINITY ? 0.f : m;
+                            const uint64_t nm2 = pack2f(C::SHIFT - ref, C::SHIFT - ref);
+                            const float isig = scales ? 1.f / fmaxf(sigma, 1e-30f) : 1.f;
+                            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                            sum[0] = sum[1] = summ = 0;
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const uint64_t y = fma2(pack2(x[c][e], x[c][e + 1]), qs2, nm2);
-                            float2 p;
-                            if ((e & 7) == 6) p = exp2_pair<C::DEG>(y);
-                            else { const float2 v = unpack2f(y); p = make_float2(fast_exp2(v.x), fast_exp2(v.y)); }
-                            const uint64_t pp = pack2f(p.x, p.y);
-                            sum = add2(sum, pp);
-                            if (Q4) {
-                                float4 u = *reinterpret_cast<const float4 *>(par + 128 + 32 * c + e);      // (scale, least + 8 scale) of two rows
-                                if (masked) {              // a row that is not seen may hold anything
-                                    if (32 * c + e >= vis) u.x = u.y = 0.f;
-                                    if (32 * c + e + 1 >= vis) u.z = u.w = 0.f;
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t pk[8];
+#pragma unroll
+                                for (int e = 0; e < 16; e += 2) {
+                                    const uint32_t x0 = x[16 * c + e], x1 = x[16 * c + e + 1];
+                                    mx[(e >> 1) & 3] = max_nan(mx[(e >> 1) & 3], __uint_as_float(x0), __uint_as_float(x1));
+                                    const uint64_t y = fma2(pack2(x0, x1), qs2, nm2);
+                                    float2 p;
+                                    if (e == 2 || e == 8 || e == 14) p = exp2_pair<C::DEG>(y);
+                                    else { const float2 v = unpack2f(y); p = make_float2(fast_exp2(v.x), fast_exp2(v.y)); }
+                                    const uint64_t pp = pack2f(p.x, p.y);
+                                    sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pp);
+                                    if (Q4) {
+                                        const int at = 64 * h + 16 * c + e;
+                                        float4 u = *reinterpret_cast<const float4 *>(par + 128 + at);  // (scale, least + 8 scale) of two rows
+                                        if (masked) {      // a row that is not seen may hold anything
+                                            if (at >= vis) u.x = u.y = 0.f;
+                                            if (at + 1 >= vis) u.z = u.w = 0.f;
+                                        }
+                                        summ = fma2(pp, pack2f(u.y, u.w), summ);
+                                        p.x *= u.x * isig; p.y *= u.z * isig;
+                                    }
+                                    pk[e >> 1] = pack16<BF>(p.x, p.y);
                                 }
-                                summ = fma2(pp, pack2f(u.y, u.w), summ);
-                                p.x *= u.x * isig; p.y *= u.z * isig;
+                                tc::tmem_st8(tS + 32 * h + 8 * c, pk);
                             }
-                            pk[e >> 1] = pack16<BF>(p.x, p.y);
+                            float top = max_nan(max_nan(mx[0], mx[1], mx[2]), mx[3]) * a.qscale;
+                            if (masked && vis <= 64 * h) top = -INFINITY;    // (nothing seen, whatever the scale)
+                            const bool far = !(top <= m + C::AHEAD) && !(top == -INFINITY);
+                            if (again || (!__any_sync(0xffffffffu, far) && sig_new == sigma)) break;
+                            float mn = max_nan(m, top);
+                            if (mn == INFINITY) mn = __uint_as_float(0x7fffffffu);         // (infinity less itself: the row is NaN)
+                            float f = mn == m ? 1.f : m == -INFINITY && mn == mn ? 0.f : fast_exp2(m - mn);
+                            l *= f; lm *= f;
+                            if (scales) { if (sigma > 0.f) f *= sigma / sig_new; sigma = sig_new; }
+                            m = mn;
+                            if (h == 1) {                  // the first half is on its way into the sum
+                                ok = wait_warp(half_done(s), ns & 1, abort_flag);
+                                if (!ok) break;
+                                tc::fence_after_sync();
+                            }
+                            if (i > 0 || h == 1) {
+#pragma unroll 1
+                                for (int c = 0; c < D; c += 16) {
+                                    uint32_t o[16];
+                                    tc::tmem_ld16(tO + c, o);
+                                    tc::tmem_ld_wait();
+#pragma unroll
+                                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                    tc::tmem_st16(tO + c, o);
+                                }
+                            }
                         }
-                        tc::tmem_st16(tS + 16 * c, pk);
+                        if (!ok) break;
+                        const float2 u = unpack2f(add2(sum[0], sum[1]));
+                        l += u.x + u.y;
+                        if (Q4) { const float2 v = unpack2f(summ); lm += v.x + v.y; }
+                        tc::tmem_st_wait();
+                        tc::fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(p_full(s, h));
                     }
-                    const float2 u = unpack2f(sum);
-                    l += u.x + u.y;
-                    if (Q4) { const float2 v = unpack2f(summ); lm += v.x + v.y; }
-                    tc::tmem_st_wait();
-                    tc::fence_before_sync();
+                    if (!ok) break;
+                } else if (lane == 0) {
+                    tc::mbar_arrive(p_full(s, 0));
+                    tc::mbar_arrive(p_full(s, 1));
                 }
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(p_full(s));
             }
             if (!ok) break;
             np += (uint32_t)(it.e1 - it.t0);
@@ -991,7 +1152,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    if (warp == 12) tc::tmem_dealloc(tmem, 512);
+    if (warp == 10) tc::tmem_dealloc(tmem, 512);
 }
 
 }  // namespace moa
