@@ -9,17 +9,17 @@
 // queries -- the g heads of consecutive tokens, which share K and V -- against the rows of one K/V head, 128 keys
 // at a time:
 //   warps 0-3, 4-7   softmax of slot 0 and slot 1, a thread to a query row (a tensor memory lane): scores out, weights in,
-//                    the weighted sum rescaled where the reference moves (it moves when a score passes it by 2^AHEAD, which
+//                    the weighted sum rescaled where the reference moves (it moves when a score passes it by AHEAD, which
 //                    after the first tiles is rare), and the output at the end of the unit
-//   warps 8-11       copies of Q, K and V into swizzled tiles, row by row (a page may end anywhere; 4 bits are unpacked here)
-//   warp 12          issues the products:  P0 V, Q0 K', P1 V, Q1 K'  and so on, so that the softmax of one slot
-//                    runs under the products of the other
+//   warps 8, 9       copies of Q, K and V into swizzled tiles: tiled ones where the layout allows them, else row by row
+//                    (a page may end anywhere); 4 bits are unpacked here
+//   warps 10, 11     issue the products of slot 0 and slot 1
 // The two slots hold rows 0..127 and 128..255 of the unit, both against every tile of keys; a unit of at most 128
 // rows has the same rows in both, against the even and the odd tiles, and the slots are joined at its end.
 //
-// A slot's scores and weights share 128 columns of tensor memory (weights of 16 bits in the first 64); products of one
-// thread run in order, so the scores of a slot's next tile overwrite its weights when those are used up, and the
-// arrival of a slot's scores means that its weighted sum is at rest: rescaling needs no barrier of its own.
+// A slot's scores and weights share 128 columns of tensor memory, 64 for each half of a tile of keys; the weights of a half (32
+// columns) overwrite its scores.  Products of one thread run in order, so the scores of a half of the next tile are issued
+// behind the product that uses up the weights in their place, while the softmax is at the other half.
 //
 // Work is handed out unit by unit (one CTA per SM; the next one's number comes from a counter; what a unit gives does not depend
 // on who takes it).  Where there are few units their keys are cut into pieces; the CTA that delivers a unit's last piece
@@ -77,9 +77,12 @@ struct PromptCfg {
     static constexpr uint32_t OFF_ROWS = OFF_ML + 2 * 128 * 8;      // [128] places of a tile's rows, K and V
     static constexpr uint32_t OFF_PLAN = OFF_ROWS + (PAGED ? 128 * 16 : 0);
     static constexpr uint32_t SMEM = OFF_PLAN + THREADS * 24 + 1024;      // (1024: alignment of the base)
-    static constexpr float AHEAD = BF && !Q4 ? 8.0f : BF ? 8.0f : 4.0f;
-    static constexpr float SHIFT = BF ? 0.0f : 11.0f;      // weights held in fp16 reach 2^15 (as in the single-query kernel)
+    // How far (log2) a score may pass the reference before it moves, and what the weights are taken larger by: those held
+    // in fp16 reach 2^15, and 64 weights of 1 are no reason to move.
+    static constexpr float AHEAD = BF ? 8.0f : 7.0f;
+    static constexpr float SHIFT = BF ? 0.0f : 8.0f;
     static constexpr int DEG = BF ? 3 : 4;
+    static constexpr unsigned POLY = 0x88;                 // of eight pairs of weights, those that go through the polynomial
 };
 
 struct PromptSeq { int first, n, past, len; };
@@ -304,9 +307,19 @@ __device__ __forceinline__ void mma_16_ts(uint32_t d, uint32_t a, uint64_t b, ui
 }
 }  // namespace tc
 
-// Wait of a whole warp: all lanes leave it with the same answer.
+// Wait of a whole warp: all lanes leave it with the same answer.  One lane polls, in a loop of three instructions: these
+// waits lie between the products, 32 lanes that poll one barrier keep the others' arrivals waiting, and code that is fetched from far
+// away costs as much as the wait.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag)
 {
+    uint32_t ok;
+    asm volatile(
+            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
+            "WAIT_%=:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t@p bra DONE_%=;\n\t"
+            "add.u32 n, n, 1;\n\tsetp.lt.u32 q, n, 64;\n\t@q bra WAIT_%=;\n"
+            "DONE_%=:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
+    if (__all_sync(0xffffffffu, ok)) return true;
     for (uint32_t it = 0; it < kWaitLimit; ++it) {
         if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
         if ((it & 15u) == 15u && __any_sync(0xffffffffu, *abort_flag)) return false;
@@ -314,6 +327,13 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
     *abort_flag = 1;
     raise_status(MOA_STATUS_WAIT_TIMEOUT);
     return false;
+}
+// Whether a phase is over, asked by one lane.
+__device__ __forceinline__ bool test_warp(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok = 1;
+    if ((threadIdx.x & 31) == 0) ok = mbar_test_wait(bar, parity);
+    return __all_sync(0xffffffffu, ok);
 }
 
 __device__ __forceinline__ float max_nan(float x, float y)
@@ -394,11 +414,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
     auto v_full = [&](int i) { return bar(2 * NST + i); };
     auto v_empty = [&](int i) { return bar(3 * NST + i); };
     constexpr int B0 = 4 * NST;
-    auto s_full = [&](int s) { return bar(B0 + s); };                        // scores of a tile
-    auto p_full = [&](int s, int h) { return bar(B0 + 2 + 2 * s + h); };     // weights of half a tile
-    auto half_done = [&](int s) { return bar(B0 + 6 + s); };                 // the first half is in the weighted sum
-    auto o_full = [&](int s) { return bar(B0 + 8 + s); };                    // the weighted sum of a unit
-    auto turn = [&](int s) { return bar(B0 + 10 + s); };
+    auto s_full = [&](int s, int h) { return bar(B0 + 2 * s + h); };         // scores of half a tile
+    auto p_full = [&](int s, int h) { return bar(B0 + 4 + 2 * s + h); };     // its weights
+    auto summed = [&](int s) { return bar(B0 + 8 + s); };                    // its part of the weighted sum
+    auto o_full = [&](int s) { return bar(B0 + 10 + s); };                   // the weighted sum of a unit
     const uint32_t q_full = bar(B0 + 12), q_empty = bar(B0 + 13);
     auto item_full = [&](int i) { return bar(B0 + 14 + i); };
     auto item_empty = [&](int i) { return bar(B0 + 16 + i); };
@@ -409,8 +428,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
     if (tid == 0) {
         for (int i = 0; i < NST; ++i) { mbar_init(k_full(i), 2); mbar_init(k_empty(i), 2); mbar_init(v_full(i), 2); mbar_init(v_empty(i), 2); }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(s_full(s), 1); mbar_init(p_full(s, 0), 4); mbar_init(p_full(s, 1), 4); mbar_init(half_done(s), 1);
-            mbar_init(o_full(s), 1); mbar_init(turn(s), 1); mbar_init(landed(s), 1);
+            mbar_init(s_full(s, 0), 1); mbar_init(s_full(s, 1), 1); mbar_init(p_full(s, 0), 4); mbar_init(p_full(s, 1), 4);
+            mbar_init(summed(s), 1); mbar_init(o_full(s), 1); mbar_init(landed(s), 1);
             mbar_init(item_full(s), 1); mbar_init(item_empty(s), 11);
         }
         mbar_init(q_full, 2); mbar_init(q_empty, 2);
@@ -437,82 +456,80 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
         if (warp >= 10) {
             // ================= products: a warp for each slot =================
             // A thread that issues products is held until the tensor core has all but the last two of them, and whatever it does
-            // between two batches (a look at a barrier: 80 to 220 cycles of 1024) the tensor core waits for.  So each slot has
-            // a warp of its own, which has looked at everything when its turn comes.  Taking turns matters: without them both
-            // slots' products run mixed, end together, and the tensor core idles while both softmaxes run.
+            // between two batches (a look at a barrier: 80 to 220 cycles) the tensor core waits for, unless another warp has
+            // products for it.
             const int s = warp - 10;
             const uint32_t sQ = base + C::OFF_Q, sK = base + C::OFF_K, sV = base + C::OFF_V, tS = t_s(s), tO = t_o(s);
-            const uint32_t id_qk = tc::idesc_16(BF, 128, 128, false) | (a.negate ? 1u << 13 : 0u);
+            const uint32_t negate = a.negate ? 1u << 13 : 0u;
             constexpr uint32_t id_pv = tc::idesc_16(BF, 128, D, true);
             constexpr uint32_t hiword = 64u | (1u << 14) | (2u << 29);       // 1024 bytes between groups of 8 rows, 128-byte swizzle
-            uint32_t nk = 0, nq = 0, np = 0, nt = 0;       // tiles of keys, items, own tiles, turns so far
+            uint32_t nk = 0, nq = 0, np = 0;               // tiles of keys, items, own tiles so far
             bool ok = true;
             for (uint32_t n = 0; ok; ++n) {
                 if (!wait_warp(item_full(n & 1), (n >> 1) & 1, abort_flag)) { ok = false; break; }
                 const PromptItem &it = s_item[n & 1];
                 if (it.rows == 0) break;
-                const int cnt = prompt_steps(it, s), other = prompt_steps(it, s ^ 1), steps = max(cnt, other);
+                const int cnt = prompt_steps(it, s), other = prompt_steps(it, s ^ 1);
                 const bool pair = it.pair;
-                if (steps > 0) {
+                if (max(cnt, other) > 0) {
                     ok = wait_warp(q_full, nq & 1, abort_flag);
                     const uint32_t qa = sQ + (pair ? 0u : (uint32_t)(s * C::KV));
                     if (cnt == 0 && lane == 0) tc::mbar_arrive(q_empty);
-                    // step i: the weighted sum of tile i, the scores of tile i + 1
+                    // step (i, h): half h of tile i into the weighted sum, then the scores of half h of tile i + 1 in their place
 #pragma unroll 1
-                    for (int i = -1; ok && i < steps; ++i) {
+                    for (int u = -2; ok && u < 2 * cnt; ++u) {
+                        const int i = u >> 1, h = u & 1;
                         const uint32_t vt = nk + (uint32_t)(pair ? 2 * i + s : i), vst = vt % NST;
                         const uint32_t kt = nk + (uint32_t)(pair ? 2 * (i + 1) + s : i + 1), kst = kt % NST;
-                        const bool sums = i >= 0 && i < cnt, more = i + 1 < cnt;
-                        const bool k_here = more && __all_sync(0xffffffffu, mbar_try_wait(k_full(kst), (kt / NST) & 1));
-                        if (sums) ok = wait_warp(v_full(vst), (vt / NST) & 1, abort_flag) && wait_warp(p_full(s, 0), np & 1, abort_flag);
-                        if (ok && (nt > 0 || s == 1)) ok = wait_warp(turn(s), (nt + (uint32_t)s - 1) & 1, abort_flag);
-                        ++nt;
-                        if (!ok) break;
-                        tc::fence_after_sync();
-                        if (sums) {
-                            const uint32_t vb = sV + vst * C::KV;
+                        const bool more = i + 1 < cnt;
+                        if (i >= 0) {
+                            if (h == 0) ok = wait_warp(v_full(vst), (vt / NST) & 1, abort_flag);
+                            ok = ok && wait_warp(p_full(s, h), np & 1, abort_flag);
+                            if (!ok) break;
+                            np += h;
+                            tc::fence_after_sync();
+                            const uint32_t vb = sV + vst * C::KV + (uint32_t)h * 8192u, tP = tS + 64u * (uint32_t)h;
                             if (tc::elect_one()) {
 #pragma unroll
                                 for (uint32_t ks = 0; ks < 4; ++ks)
-                                    tc::mma_16_ts(tO, tS + 8u * ks, tc::pack64(((vb + ks * 2048u) >> 4) | (1024u << 16), hiword), id_pv, (i != 0 || ks != 0));
-                                tc::mma_commit(half_done(s));
-                            }
-                            __syncwarp();
-                            ok = wait_warp(p_full(s, 1), np & 1, abort_flag);
-                            ++np;
-                            if (!ok) break;
-                            tc::fence_after_sync();
-                            if (tc::elect_one()) {
-#pragma unroll
-                                for (uint32_t ks = 4; ks < 8; ++ks)
-                                    tc::mma_16_ts(tO, tS + 8u * ks, tc::pack64(((vb + ks * 2048u) >> 4) | (1024u << 16), hiword), id_pv, 1);
-                                tc::mma_commit(v_empty(vst));
-                                if (pair || i >= other) tc::mma_commit(v_empty(vst));      // (for the other slot)
-                                if (!more) tc::mma_commit(o_full(s));
+                                    tc::mma_16_ts(tO, tP + 8u * ks, tc::pack64(((vb + ks * 2048u) >> 4) | (1024u << 16), hiword), id_pv, (u != 0 || ks != 0));
+                                tc::mma_commit(summed(s));
+                                if (h == 1) {
+                                    tc::mma_commit(v_empty(vst));
+                                    if (pair || i >= other) tc::mma_commit(v_empty(vst));  // (for the other slot)
+                                    if (!more) tc::mma_commit(o_full(s));
+                                }
                             }
                             __syncwarp();
                         }
-                        if (more) {
-                            if (!k_here) {
+                        // The scores by halves, so that one is there while the softmax is at the other: 64 keys take the tensor core
+                        // as long as 128 (the queries are read again), which is still the better (2 x 8192 tokens 0.90 ms;
+                        // whole tiles 1.15, or 0.92..1.2 with the two warps in turns).  A unit of few rows waits for memory
+                        // and takes whole tiles (64 x 4 draft tokens 296 us; by halves 450).
+                        if (more && (h == 1 || !pair)) {
+                            if (h == 0 || pair) {
                                 ok = wait_warp(k_full(kst), (kt / NST) & 1, abort_flag);
                                 if (!ok) break;
                                 tc::fence_after_sync();
                             }
-                            const uint32_t kb = sK + kst * C::KV;
+                            const uint32_t half = pair ? 0u : (uint32_t)h, kb = sK + kst * C::KV + half * 8192u, tH = tS + 64u * half;
+                            const uint32_t id_qk = tc::idesc_16(BF, 128, pair ? 128 : 64, false) | negate;
                             if (tc::elect_one()) {
 #pragma unroll
                                 for (uint32_t ks = 0; ks < D / 16; ++ks) {
                                     const uint32_t off = (ks / 4) * 16384u + (ks % 4) * 32u;
-                                    tc::mma_16_ss(tS, tc::pack64(((qa + off) >> 4) | (1u << 16), hiword), tc::pack64(((kb + off) >> 4) | (1u << 16), hiword), id_qk, ks != 0);
+                                    tc::mma_16_ss(tH, tc::pack64(((qa + off) >> 4) | (1u << 16), hiword), tc::pack64(((kb + off) >> 4) | (1u << 16), hiword), id_qk, ks != 0);
                                 }
-                                tc::mma_commit(s_full(s));
-                                tc::mma_commit(k_empty(kst));
-                                if (pair || i + 1 >= other) tc::mma_commit(k_empty(kst));
-                                if (i + 2 == cnt) tc::mma_commit(q_empty);
+                                if (pair) tc::mma_commit(s_full(s, 0));
+                                tc::mma_commit(s_full(s, h));
+                                if (h == 1) {
+                                    tc::mma_commit(k_empty(kst));
+                                    if (pair || i + 1 >= other) tc::mma_commit(k_empty(kst));
+                                    if (i + 2 == cnt) tc::mma_commit(q_empty);
+                                }
                             }
                             __syncwarp();
                         }
-                        if (lane == 0) tc::mbar_arrive(turn(s ^ 1));
                     }
                     nk += (uint32_t)(it.e1 - it.t0);
                     ++nq;
@@ -588,7 +605,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             pending = true;
         };
         auto wait_free = [&](uint32_t b, uint32_t parity) {
-            if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
+            if (test_warp(b, parity)) return true;
             drain();                  // what this waits for may need them
             return wait_warp(b, parity, abort_flag);
         };
@@ -884,8 +901,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             const int dead = !__any_sync(0xffffffffu, valid);                // a warp without rows only keeps step
             for (int i = 0; ok && i < cnt; ++i, ++ns) {
                 const int t = it.t0 + (it.pair ? 2 * i + s : i);
-                ok = wait_warp(s_full(s), ns & 1, abort_flag);
-                if (!ok) break;
                 if (i == 0 && unread) {                    // (the join before: the other slot's reads come before these weights)
                     ok = wait_warp(parted, (nj - 1) & 1, abort_flag);
                     unread = false;
@@ -897,14 +912,16 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                     if (!ok) break;
                 }
                 if (!dead) {
-                    tc::fence_after_sync();
                     float2 *const par = reinterpret_cast<float2 *>(smem + C::OFF_PAR) + ps * 256;
                     const int vis = lim - t * 128;         // keys of this tile that the row sees
                     const bool masked = !__all_sync(0xffffffffu, vis >= 128);
                     const uint64_t qs2 = pack2f(a.qscale, a.qscale);
                     const bool scales = Q4 && !BF;
-#pragma unroll
+#pragma unroll 1
                     for (int h = 0; h < 2; ++h) {          // 64 keys at a time: the first half's product runs under the second's weights
+                        ok = wait_warp(s_full(s, h), ns & 1, abort_flag);
+                        if (!ok) break;
+                        tc::fence_after_sync();
                         uint32_t x[64];
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
@@ -914,17 +931,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             for (int e = 0; e < 32; ++e) x[32 * c + e] = z[e];
                         }
                         tc::tmem_ld_wait();
+                        const float2 *const kpar = par + 64 * h, *const vpar = kpar + 128;
+                        const int left = vis - 64 * h;     // keys of this half that the row sees
                         if (Q4) {                          // scale * <q, c - 8> + (least + 8 scale) * sum(q)
 #pragma unroll
                             for (int e = 0; e < 64; ++e) {
-                                const float2 k2 = par[64 * h + e];
+                                const float2 k2 = kpar[e];
                                 x[e] = __float_as_uint(fmaf(k2.x, __uint_as_float(x[e]), k2.y * sumq));
                             }
                         }
                         if (masked) {
+                            const uint32_t see0 = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
+                            const uint32_t see1 = left >= 64 ? 0xffffffffu : left <= 32 ? 0u : (1u << (left - 32)) - 1u;
 #pragma unroll
                             for (int e = 0; e < 64; ++e)
-                                if (64 * h + e >= vis) x[e] = 0xff800000u;
+                                if (!((e < 32 ? see0 : see1) & (1u << (e & 31)))) x[e] = 0xff800000u;
                         }
                         float sig_new = sigma;
                         if (scales && h == 0) {
@@ -932,14 +953,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             const float st = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
                             if (st > sigma) sig_new = __uint_as_float((__float_as_uint(st) + 0x007fffffu) & 0x7f800000u);
                         }
-                        // The weights by the reference as it is, and the maximum beside them.  Where a score passes the
-                        // reference by AHEAD, it moves (for every row of the warp), and the weights are made again.
+                        // The weights by the reference as it is.  Where one may be above 2^AHEAD -- their sum is, or a score that goes
+                        // through the polynomial, which takes no larger ones -- the reference moves to the largest
+                        // score (for every row of the warp), and the weights are made again.
                         uint64_t sum[2], summ;
                         for (bool again = false;; again = true) {
                             const float ref = m == -INFINITY ? 0.f : m;
                             const uint64_t nm2 = pack2f(C::SHIFT - ref, C::SHIFT - ref);
                             const float isig = scales ? 1.f / fmaxf(sigma, 1e-30f) : 1.f;
-                            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                            float mx = -INFINITY;
                             sum[0] = sum[1] = summ = 0;
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
@@ -947,43 +969,48 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
 #pragma unroll
                                 for (int e = 0; e < 16; e += 2) {
                                     const uint32_t x0 = x[16 * c + e], x1 = x[16 * c + e + 1];
-                                    mx[(e >> 1) & 3] = max_nan(mx[(e >> 1) & 3], __uint_as_float(x0), __uint_as_float(x1));
                                     const uint64_t y = fma2(pack2(x0, x1), qs2, nm2);
                                     float2 p;
-                                    if (e == 2 || e == 8 || e == 14) p = exp2_pair<C::DEG>(y);
-                                    else { const float2 v = unpack2f(y); p = make_float2(fast_exp2(v.x), fast_exp2(v.y)); }
+                                    if (C::POLY >> (e >> 1) & 1) {
+                                        mx = max_nan(mx, __uint_as_float(x0), __uint_as_float(x1));
+                                        p = exp2_pair<C::DEG>(y);
+                                    } else { const float2 v = unpack2f(y); p = make_float2(fast_exp2(v.x), fast_exp2(v.y)); }
                                     const uint64_t pp = pack2f(p.x, p.y);
                                     sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pp);
                                     if (Q4) {
-                                        const int at = 64 * h + 16 * c + e;
-                                        float4 u = *reinterpret_cast<const float4 *>(par + 128 + at);  // (scale, least + 8 scale) of two rows
+                                        const int at = 16 * c + e;
+                                        float4 u = *reinterpret_cast<const float4 *>(vpar + at);       // (scale, least + 8 scale) of two rows
                                         if (masked) {      // a row that is not seen may hold anything
-                                            if (at >= vis) u.x = u.y = 0.f;
-                                            if (at + 1 >= vis) u.z = u.w = 0.f;
+                                            if (at >= left) u.x = u.y = 0.f;
+                                            if (at + 1 >= left) u.z = u.w = 0.f;
                                         }
                                         summ = fma2(pp, pack2f(u.y, u.w), summ);
                                         p.x *= u.x * isig; p.y *= u.z * isig;
                                     }
                                     pk[e >> 1] = pack16<BF>(p.x, p.y);
                                 }
-                                tc::tmem_st8(tS + 32 * h + 8 * c, pk);
+                                tc::tmem_st8(tS + 64 * h + 8 * c, pk);
                             }
-                            float top = max_nan(max_nan(mx[0], mx[1], mx[2]), mx[3]) * a.qscale;
-                            if (masked && vis <= 64 * h) top = -INFINITY;    // (nothing seen, whatever the scale)
-                            const bool far = !(top <= m + C::AHEAD) && !(top == -INFINITY);
+                            const float2 both = unpack2f(add2(sum[0], sum[1]));
+                            constexpr float kMost = BF ? 256.f : 32768.f;                          // 2^(AHEAD + SHIFT)
+                            const float high = mx * a.qscale;
+                            const bool none = masked && left <= 0;
+                            const bool far = !none && (m == -INFINITY || !(both.x + both.y <= kMost) || !(high <= ref + C::AHEAD || high == -INFINITY));
                             if (again || (!__any_sync(0xffffffffu, far) && sig_new == sigma)) break;
+                            float top = -INFINITY;
+#pragma unroll
+                            for (int e = 0; e < 64; e += 2) top = max_nan(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                            top = none ? -INFINITY : top * a.qscale;                // (nothing seen, whatever the scale)
                             float mn = max_nan(m, top);
                             if (mn == INFINITY) mn = __uint_as_float(0x7fffffffu);         // (infinity less itself: the row is NaN)
                             float f = mn == m ? 1.f : m == -INFINITY && mn == mn ? 0.f : fast_exp2(m - mn);
                             l *= f; lm *= f;
                             if (scales) { if (sigma > 0.f) f *= sigma / sig_new; sigma = sig_new; }
                             m = mn;
-                            if (h == 1) {                  // the first half is on its way into the sum
-                                ok = wait_warp(half_done(s), ns & 1, abort_flag);
+                            if (i > 0 || h == 1) {         // (the half before is on its way into the sum)
+                                ok = wait_warp(summed(s), (h ^ 1) & 1, abort_flag);
                                 if (!ok) break;
                                 tc::fence_after_sync();
-                            }
-                            if (i > 0 || h == 1) {
 #pragma unroll 1
                                 for (int c = 0; c < D; c += 16) {
                                     uint32_t o[16];
@@ -1005,9 +1032,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                         if (lane == 0) tc::mbar_arrive(p_full(s, h));
                     }
                     if (!ok) break;
-                } else if (lane == 0) {
-                    tc::mbar_arrive(p_full(s, 0));
-                    tc::mbar_arrive(p_full(s, 1));
+                } else {
+                    for (int h = 0; h < 2; ++h) {
+                        ok = ok && wait_warp(s_full(s, h), ns & 1, abort_flag);
+                        if (ok && lane == 0) tc::mbar_arrive(p_full(s, h));
+                    }
+                    if (!ok) break;
                 }
             }
             if (!ok) break;
