@@ -18,6 +18,7 @@
 #include "moa_paged.cuh"
 #include "moa_paged_io.cuh"
 #include "moa_prompt.cuh"
+#include "moa_prompt32.cuh"
 
 namespace moa {
 
@@ -1308,6 +1309,34 @@ static cudaError_t launch_prompt(int format, int dtype, bool paged, const Prompt
     return launch_prompt_cfg<PromptCfg<MOA_KV_F16, false, D, true>>(a, m, grid, st);
 }
 
+// fp32: a CTA for each unit of 64 rows that there can be, and for each piece of its keys where the units alone do not
+// fill the GPU (256 keys at the least).
+template <class C>
+static cudaError_t launch_prompt32_cfg(const PromptArgs &a, long long keys, cudaStream_t st)
+{
+    static bool attr_set[kMaxDevices] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(prompt32_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
+    const int units = (int)(((long long)a.tokens * a.g / C::ROWS + a.batch) * a.h_kv);
+    long long splits = a.slot_cap / units;
+    if (splits > (keys + 255) / 256) splits = (keys + 255) / 256;
+    if (splits < 1) splits = 1;
+    launch_dependent(prompt32_kernel<C>, (int)(units * splits), C::THREADS, C::SMEM, st, a, (int)splits, units);
+    count_launch();
+    return cudaGetLastError();
+}
+static cudaError_t launch_prompt32(bool paged, int d, const PromptArgs &a, cudaStream_t st)
+{
+    const long long keys = paged ? (long long)a.max_pages * a.page_size : a.tokens;
+    if (d == 128) return paged ? launch_prompt32_cfg<Prompt32Cfg<128, true>>(a, keys, st) : launch_prompt32_cfg<Prompt32Cfg<128, false>>(a, keys, st);
+    return paged ? launch_prompt32_cfg<Prompt32Cfg<64, true>>(a, keys, st) : launch_prompt32_cfg<Prompt32Cfg<64, false>>(a, keys, st);
+}
+
 // What both calls share once their own arguments are in `a`: sizes, scale, workspace, launch.
 static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d, float scale, void *ws, size_t ws_bytes, cudaStream_t st)
 {
@@ -1331,7 +1360,14 @@ static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d
     unsigned long long tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
     if (tag == 0) tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
     a.ticket_tag = (tag << 20) | 1ull;
+    cudaError_t e;
     PromptMaps m = {};
+    if (format == MOA_KV_F32) {
+        e = launch_prompt32(paged, d, a, st);
+        if (e != cudaSuccess) return MOA_ERR_CUDA;
+        g_last_path = MOA_PATH_PROMPT;
+        return MOA_OK;
+    }
     if (format != MOA_KV_INT4) {               // (a whole tile of 128 rows there has to be; pages are multiples of a copy's rows)
         const long long most = paged ? (long long)a.max_pages * a.page_size : a.tokens;
         const int box = !paged || a.page_size % 32 == 0 ? 32 : a.page_size % 16 == 0 ? 16 : 0;
@@ -1342,7 +1378,7 @@ static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d
             make_prompt_map(&m.v, a.v, dtype == MOA_BF16, d, box, rows, a.h_kv, pages, vs))
             a.box = box;
     }
-    const cudaError_t e = d == 128 ? launch_prompt<128>(format, dtype, paged, a, m, grid, st) : launch_prompt<64>(format, dtype, paged, a, m, grid, st);
+    e = d == 128 ? launch_prompt<128>(format, dtype, paged, a, m, grid, st) : launch_prompt<64>(format, dtype, paged, a, m, grid, st);
     if (e != cudaSuccess) return MOA_ERR_CUDA;
     g_last_path = MOA_PATH_PROMPT;
     return MOA_OK;
@@ -1356,7 +1392,6 @@ static int prompt_impl(const void *q, const void *k, const void *v, void *out, i
     if (tokens < 1 || h_q < 1 || h_kv < 1 || h_q % h_kv != 0 || batch < 1 || d < 1 || !isfinite(scale * kLog2e)) return MOA_ERR_INVALID;
     if (dtype < MOA_F32 || dtype > MOA_F16 || (causal != 0 && causal != 1) || (!token_start && batch != 1)) return MOA_ERR_INVALID;
     if (d != 64 && d != 128) return MOA_ERR_UNSUPPORTED;
-    if (dtype == MOA_F32) return MOA_ERR_UNSUPPORTED;
     const int es = element_bytes(dtype);
     const long long dense[4] = {(long long)h_q * d, (long long)h_kv * d, (long long)h_kv * d, (long long)h_q * d};
     long long s[4];
@@ -1392,7 +1427,6 @@ static int paged_chunk_impl(const moa_paged_cache *c, const void *q, void *out, 
     if (rc != MOA_OK) return rc;
     if (h_q % c->h_kv != 0 || dtype < MOA_F32 || dtype > MOA_F16) return MOA_ERR_INVALID;
     if (!paged_dtype_ok(c->format, dtype)) return MOA_ERR_UNSUPPORTED;
-    if (dtype == MOA_F32) return MOA_ERR_UNSUPPORTED;
     if (q_stride == 0) q_stride = (long long)h_q * c->d;
     if (q_stride > (1LL << 40)) return MOA_ERR_INVALID;
     const int es = element_bytes(dtype);
