@@ -955,7 +955,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                         }
                         // The weights by the reference as it is.  Where one may be above 2^AHEAD -- their sum is, or a score that goes
                         // through the polynomial, which takes no larger ones -- the reference moves to the largest
-                        // score (for every row of the warp), and the weights are made again.
+                        // score, and the warp makes its weights again.
                         uint64_t sum[2], summ;
                         for (bool again = false;; again = true) {
                             const float ref = m == -INFINITY ? 0.f : m;
@@ -1001,7 +1001,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
 #pragma unroll
                             for (int e = 0; e < 64; e += 2) top = max_nan(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
                             top = none ? -INFINITY : top * a.qscale;                // (nothing seen, whatever the scale)
-                            float mn = max_nan(m, top);
+                            float mn = far ? max_nan(m, top) : m;          // (a row alone: what it gives does not depend on its neighbours)
                             if (mn == INFINITY) mn = __uint_as_float(0x7fffffffu);         // (infinity less itself: the row is NaN)
                             float f = mn == m ? 1.f : m == -INFINITY && mn == mn ? 0.f : fast_exp2(m - mn);
                             l *= f; lm *= f;
@@ -1045,8 +1045,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
 
             // ---- the unit's end ----
             if (cnt > 0) { ok = wait_warp(o_full(s), no & 1, abort_flag); ++no; if (!ok) break; }
-            const bool nf = s_nf[n & 1] != 0;
-            const int *const nf_key = reinterpret_cast<const int *>(smem + C::OFF_NF) + (n & 1) * D;
             int c0 = 0, c1 = D;                            // this thread's columns
             float fa = 1.f, fb = 0.f;                      // factors of the slots' sums
             float M = m, L = l, add = lm;
@@ -1072,6 +1070,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                 }
                 c0 = s * (D / 2); c1 = c0 + D / 2;
             }
+            // (behind the join: the other slot's tiles have been looked through by then)
+            const bool nf = s_nf[n & 1] != 0;
+            const int *const nf_key = reinterpret_cast<const int *>(smem + C::OFF_NF) + (n & 1) * D;
             const uint32_t tB = t_o(s ^ 1) + lane_at;
             float inv = 1.f;
             float *part = nullptr;
