@@ -246,7 +246,16 @@ __global__ void __launch_bounds__(256, TURN == kTurnAny ? 2 : DT == MOA_F32 || F
 
     // This thread's share of the token's cosines and sines.
     float cs[8], sn[8];
-    if constexpr (TURN == kTurnChunks || TURN == kTurnPairs) {
+    const uint32_t mine = MODE == kByRow ? 0u : (uint32_t)(a.axis_map[(8 * part) >> 5 & 1] >> (2 * (8 * part & 31))) & 0xffffu;     // axes of its eight pairs
+    if (MODE != kByRow && TURN == kTurnChunks && turns && mine == (mine & 3u) * 0x5555u) {
+        const float *at = row_of(8 * part);                // one axis: 16-byte loads (rows of rot floats, rot a multiple of 16)
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const float4 c4 = *reinterpret_cast<const float4 *>(at + 8 * part + i), s4 = *reinterpret_cast<const float4 *>(at + half + 8 * part + i);
+            cs[i] = c4.x; cs[i + 1] = c4.y; cs[i + 2] = c4.z; cs[i + 3] = c4.w;
+            sn[i] = s4.x; sn[i + 1] = s4.y; sn[i + 2] = s4.z; sn[i + 3] = s4.w;
+        }
+    } else if constexpr (TURN == kTurnChunks || TURN == kTurnPairs) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const bool in = turns && (TURN == kTurnChunks || 8 * part + i < half);

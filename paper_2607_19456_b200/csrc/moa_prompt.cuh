@@ -70,7 +70,7 @@ struct PromptCfg {
     static constexpr uint32_t OFF_Q = 0;
     static constexpr uint32_t OFF_K = OFF_Q + 2 * KV;
     static constexpr uint32_t OFF_V = OFF_K + NST * KV;
-    static constexpr uint32_t OFF_PAR = OFF_V + NST * KV;  // [NPAR][2 (K, V)][128] (scale, least + 8 scale)
+    static constexpr uint32_t OFF_PAR = OFF_V + NST * KV;  // [NPAR][4][128]: K scale, K least + 8 scale, V scale, V least + 8 scale
     static constexpr uint32_t OFF_PMAX = OFF_PAR + (Q4 ? NPAR * 2 * 128 * 8 : 0);      // [NPAR][4] largest scales of V
     static constexpr uint32_t OFF_NF = OFF_PMAX + (Q4 ? NPAR * 16 : 0);                // [2][D] first key with a V that is not finite
     static constexpr uint32_t OFF_ML = OFF_NF + 2 * D * 4; // [2][128] (m, l) of the slots
@@ -439,6 +439,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
         s_abort = 0;
     }
     if (warp == 10) tc::tmem_alloc(smem_u32(&s_tmem), 512);
+    if (tid == 32 * 8 && a.box > 0) { tc::prefetch_tmap(&map_k); tc::prefetch_tmap(&map_v); }
     launch_dependents();
     grid_dependency_wait();
     PromptGroup *const groups = reinterpret_cast<PromptGroup *>(smem + C::OFF_PLAN);
@@ -610,31 +611,35 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             return wait_warp(b, parity, abort_flag);
         };
 
+        // Item n: drawn when the copies of the one before are issued (drawing it a tile earlier changed nothing).
+        auto fetch = [&](uint32_t n) {
+            const int set = n & 1;
+            if (n >= 2) {
+                ok = wait_free(item_empty(set), ((n >> 1) - 1) & 1);
+                if (!ok) return;
+            }
+            if (lane == 0) {
+                int i = blockIdx.x;
+                if (n > 0) {
+                    i = 0x7fffffff;
+                    if (plan.items > (int)gridDim.x) {
+                        unsigned long long *word = a.tickets + a.slot_cap;
+                        const unsigned j = ticket_arrive(word, a.ticket_tag);
+                        if (j + 1 == (unsigned)plan.items) *word = 0;          // every CTA has drawn its last number
+                        i = (int)min((unsigned)gridDim.x + j, 0x7fffffffu);
+                    }
+                }
+                prompt_item<PAGED>(a, plan, groups, C::THREADS, i, s_item[set]);
+                s_nf[set] = 0;
+            }
+            for (int f = lane; f < D; f += 32) reinterpret_cast<int *>(smem + C::OFF_NF)[set * D + f] = 0x7fffffff;
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(item_full(set));
+        };
+        if (w == 0) fetch(0);
+
         for (uint32_t n = 0; ok; ++n) {
             const int set = n & 1;
-            if (w == 0) {
-                if (n >= 2) {
-                    ok = wait_free(item_empty(set), ((n >> 1) - 1) & 1);
-                    if (!ok) break;
-                }
-                if (lane == 0) {
-                    int i = blockIdx.x;
-                    if (n > 0) {
-                        i = 0x7fffffff;
-                        if (plan.items > (int)gridDim.x) {
-                            unsigned long long *word = a.tickets + a.slot_cap;
-                            const unsigned j = ticket_arrive(word, a.ticket_tag);
-                            if (j + 1 == (unsigned)plan.items) *word = 0;          // every CTA has drawn its last number
-                            i = (int)min((unsigned)gridDim.x + j, 0x7fffffffu);
-                        }
-                    }
-                    prompt_item<PAGED>(a, plan, groups, C::THREADS, i, s_item[set]);
-                    s_nf[set] = 0;
-                }
-                for (int f = lane; f < D; f += 32) reinterpret_cast<int *>(smem + C::OFF_NF)[set * D + f] = 0x7fffffff;
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(item_full(set));
-            }
             ok = wait_free(item_full(set), (n >> 1) & 1);
             if (!ok) break;
             const PromptItem &it = s_item[set];
@@ -819,10 +824,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
                             const float2 kf = unpack16<false>(k_pair[g]), vf = unpack16<false>(v_pair[g]);
-                            float2 *par = reinterpret_cast<float2 *>(smem + C::OFF_PAR) + ps * 256 + 64 * w + 32 * g + lane;
+                            float *par = reinterpret_cast<float *>(smem + C::OFF_PAR) + ps * 512 + 64 * w + 32 * g + lane;
                             const float nan = __uint_as_float(0x7fffffffu);
-                            par[0] = row_bad[g] ? make_float2(nan, nan) : row_ok[g] ? make_float2(kf.x, fmaf(8.f, kf.x, kf.y)) : make_float2(0.f, 0.f);
-                            par[128] = row_ok[g] ? make_float2(vf.x, fmaf(8.f, vf.x, vf.y)) : make_float2(0.f, 0.f);
+                            par[0] = row_bad[g] ? nan : row_ok[g] ? kf.x : 0.f;
+                            par[128] = row_bad[g] ? nan : row_ok[g] ? fmaf(8.f, kf.x, kf.y) : 0.f;
+                            par[256] = row_ok[g] ? vf.x : 0.f;
+                            par[384] = row_ok[g] ? fmaf(8.f, vf.x, vf.y) : 0.f;
                             float top = row_ok[g] ? vf.x : 0.f;
 #pragma unroll
                             for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -856,8 +863,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                     }
                     ++nk;
                 }
-                drain();              // the next item's number takes a while
+                drain();
             }
+            if (ok && w == 0) fetch(n + 1);
             if (w != 0 && ok) { __syncwarp(); if (lane == 0) tc::mbar_arrive(item_empty(set)); }
         }
         drain();
@@ -912,7 +920,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                     if (!ok) break;
                 }
                 if (!dead) {
-                    float2 *const par = reinterpret_cast<float2 *>(smem + C::OFF_PAR) + ps * 256;
+                    const float *const par = reinterpret_cast<const float *>(smem + C::OFF_PAR) + ps * 512;
                     const int vis = lim - t * 128;         // keys of this tile that the row sees
                     const bool masked = !__all_sync(0xffffffffu, vis >= 128);
                     const uint64_t qs2 = pack2f(a.qscale, a.qscale);
@@ -931,13 +939,17 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             for (int e = 0; e < 32; ++e) x[32 * c + e] = z[e];
                         }
                         tc::tmem_ld_wait();
-                        const float2 *const kpar = par + 64 * h, *const vpar = kpar + 128;
+                        const float *const kpar = par + 64 * h, *const vpar = kpar + 256;
                         const int left = vis - 64 * h;     // keys of this half that the row sees
                         if (Q4) {                          // scale * <q, c - 8> + (least + 8 scale) * sum(q)
+                            const uint64_t sq2 = pack2f(sumq, sumq);
 #pragma unroll
-                            for (int e = 0; e < 64; ++e) {
-                                const float2 k2 = kpar[e];
-                                x[e] = __float_as_uint(fmaf(k2.x, __uint_as_float(x[e]), k2.y * sumq));
+                            for (int e = 0; e < 64; e += 4) {
+                                const float4 ks = *reinterpret_cast<const float4 *>(kpar + e), km = *reinterpret_cast<const float4 *>(kpar + 128 + e);
+                                const uint64_t y0 = fma2(pack2f(ks.x, ks.y), pack2(x[e], x[e + 1]), mul2(pack2f(km.x, km.y), sq2));
+                                const uint64_t y1 = fma2(pack2f(ks.z, ks.w), pack2(x[e + 2], x[e + 3]), mul2(pack2f(km.z, km.w), sq2));
+                                unpack2(y0, x[e], x[e + 1]);
+                                unpack2(y1, x[e + 2], x[e + 3]);
                             }
                         }
                         if (masked) {
@@ -954,15 +966,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             if (st > sigma) sig_new = __uint_as_float((__float_as_uint(st) + 0x007fffffu) & 0x7f800000u);
                         }
                         // The weights by the reference as it is.  Where one may be above 2^AHEAD -- their sum is, or a score that goes
-                        // through the polynomial, which takes no larger ones -- the reference moves to the largest
-                        // score, and the warp makes its weights again.
+                        // through the polynomial, which takes no larger ones -- the largest score is looked for, the
+                        // reference moves to it if it passes AHEAD, and the warp makes its weights again.
                         uint64_t sum[2], summ;
+                        const bool none = masked && left <= 0;
                         for (bool again = false;; again = true) {
                             const float ref = m == -INFINITY ? 0.f : m;
                             const uint64_t nm2 = pack2f(C::SHIFT - ref, C::SHIFT - ref);
                             const float isig = scales ? 1.f / fmaxf(sigma, 1e-30f) : 1.f;
+                            const uint64_t is2 = pack2f(isig, isig);
                             float mx = -INFINITY;
                             sum[0] = sum[1] = summ = 0;
+                            float4 vs4 = make_float4(0.f, 0.f, 0.f, 0.f), vm4 = vs4;
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 uint32_t pk[8];
@@ -979,13 +994,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                                     sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pp);
                                     if (Q4) {
                                         const int at = 16 * c + e;
-                                        float4 u = *reinterpret_cast<const float4 *>(vpar + at);       // (scale, least + 8 scale) of two rows
-                                        if (masked) {      // a row that is not seen may hold anything
-                                            if (at >= left) u.x = u.y = 0.f;
-                                            if (at + 1 >= left) u.z = u.w = 0.f;
+                                        if (e % 4 == 0) {
+                                            vs4 = *reinterpret_cast<const float4 *>(vpar + at);
+                                            vm4 = *reinterpret_cast<const float4 *>(vpar + 128 + at);
                                         }
-                                        summ = fma2(pp, pack2f(u.y, u.w), summ);
-                                        p.x *= u.x * isig; p.y *= u.z * isig;
+                                        float2 vs = e % 4 == 0 ? make_float2(vs4.x, vs4.y) : make_float2(vs4.z, vs4.w);
+                                        float2 vm = e % 4 == 0 ? make_float2(vm4.x, vm4.y) : make_float2(vm4.z, vm4.w);
+                                        if (masked) {      // a row that is not seen may hold anything
+                                            if (at >= left) vs.x = vm.x = 0.f;
+                                            if (at + 1 >= left) vs.y = vm.y = 0.f;
+                                        }
+                                        summ = fma2(pp, pack2f(vm.x, vm.y), summ);
+                                        p = unpack2f(mul2(scales ? mul2(pp, is2) : pp, pack2f(vs.x, vs.y)));
                                     }
                                     pk[e >> 1] = pack16<BF>(p.x, p.y);
                                 }
@@ -994,14 +1014,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             const float2 both = unpack2f(add2(sum[0], sum[1]));
                             constexpr float kMost = BF ? 256.f : 32768.f;                          // 2^(AHEAD + SHIFT)
                             const float high = mx * a.qscale;
-                            const bool none = masked && left <= 0;
                             const bool far = !none && (m == -INFINITY || !(both.x + both.y <= kMost) || !(high <= ref + C::AHEAD || high == -INFINITY));
                             if (again || (!__any_sync(0xffffffffu, far) && sig_new == sigma)) break;
                             float top = -INFINITY;
 #pragma unroll
                             for (int e = 0; e < 64; e += 2) top = max_nan(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
                             top = none ? -INFINITY : top * a.qscale;                // (nothing seen, whatever the scale)
-                            float mn = far ? max_nan(m, top) : m;          // (a row alone: what it gives does not depend on its neighbours)
+                            // (each row by its own largest score: what it gives does not depend on its neighbours)
+                            float mn = !(top <= m + C::AHEAD) ? max_nan(m, top) : m;
                             if (mn == INFINITY) mn = __uint_as_float(0x7fffffffu);         // (infinity less itself: the row is NaN)
                             float f = mn == m ? 1.f : m == -INFINITY && mn == mn ? 0.f : fast_exp2(m - mn);
                             l *= f; lm *= f;
