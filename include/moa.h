@@ -373,10 +373,15 @@ int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int
  *       batch is 1 and all tokens are its.  A sequence whose tokens are not inside [0, tokens) in ascending order sets
  *       MOA_STATUS_SEQLEN_RANGE and is left out.
  * q, k, v, out are 16-byte aligned, token strides multiples of 16 bytes; `scale` is below 2^127 in size.
+ * At most 2^20 - 4096 blocks of 128 rows (a row: one head of one token) in all, over every K/V head and counting one more
+ * per sequence and K/V head; more is MOA_ERR_CAPACITY.
  * Scores, softmax statistics and sums are fp32 and out is rounded once; for 16-bit types the weight of each row is
- * rounded to that type on its way into the weighted sum (fp16: below 2^-36 of the heaviest row's weight it adds nothing).
- * A value that is not finite makes NaN or infinite: in q, the row; in k, the rows that see it; in v, its feature
- * in the rows that see it (NaN also where the definition has an infinity).  What a row does not see does not touch it.
+ * rounded to that type on its way into the weighted sum (half a step of it; fp16: below 2^-33 of the heaviest row's weight it adds
+ * nothing), and bf16 weights are made to 2^-13.  How rows and keys are
+ * cut follows from the call's lengths and the number of CTAs, and the order of the sums from that: the same call gives the same bits.
+ * A value that is not finite makes NaN or infinite: in q, the row; in k, the rows that see it (also those where the
+ * definition makes its weight 0); in v, its feature in the rows that see it (NaN also where the definition has an infinity).  What a
+ * row does not see does not touch it.
  * `workspace`: device memory, 256-byte aligned, at least moa_prompt_workspace_bytes(...) bytes, contents
  * undefined on entry and exit; not to be shared by calls that can overlap on the GPU.
  * One launch; allocates nothing; can be captured into a CUDA graph after one uncaptured call.
@@ -395,7 +400,9 @@ int moa_prompt_attn(const void *q, const void *k, const void *v, void *out, int 
  * A length below the number of new tokens or beyond max_pages*page_size sets MOA_STATUS_SEQLEN_RANGE and leaves
  * the sequence's out untouched; a page number outside [0, num_pages) among the rows that a sequence's tokens see sets
  * MOA_STATUS_PAGE_RANGE, nothing outside the pools is read, and the rows of out that depend on it become NaN.
- * All else (scale, numbers, workspace, launch) as for moa_prompt_attn.
+ * All else (scale, capacity, numbers, workspace, launch) as for moa_prompt_attn.  MOA_KV_INT4: what is rounded to `dtype` is the
+ * weight times the row's scale, against eight steps of the row; a (scale, least) pair that is not finite counts as a row of such values.
+ * A batch of single tokens alone is moa_paged_decode_attn's work (its weights are held in two terms).
  */
 int moa_paged_chunk_attn(const moa_paged_cache *cache, const void *q, void *out, int dtype, long long q_stride, int tokens, int h_q,
                          int batch, const int32_t *token_start, const int32_t *seq_lens, const int32_t *page_table, int max_pages,
@@ -508,8 +515,8 @@ const char *moa_strerror(int code);
                                   fused step: 17..32) */
 #define MOA_PATH_MMA       4   /* streaming kernel with warp-level MMA, 8 or 16 heads per fetched row (larger groups in
                                   several passes), d_k, d_v in {64,128} */
-#define MOA_PATH_PROMPT    6   /* reported only: moa_prompt_attn, moa_paged_chunk_attn */
 #define MOA_PATH_PAGED     5   /* reported only: the paged calls have one kernel family, never forced */
+#define MOA_PATH_PROMPT    6   /* reported only: moa_prompt_attn, moa_paged_chunk_attn */
 int moa_set_option(int option, int value);
 int moa_last_path(void);
 

@@ -1341,7 +1341,8 @@ static cudaError_t launch_prompt32(bool paged, int d, const PromptArgs &a, cudaS
 static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d, float scale, void *ws, size_t ws_bytes, cudaStream_t st)
 {
     const long long rows = (long long)a.tokens * a.g;
-    if ((long long)a.tokens * a.h_q > 0x7fffffffLL - 1024 || ((rows + 127) / 128 + a.batch) * a.h_kv >= (1LL << 20)) return MOA_ERR_CAPACITY;
+    if ((long long)a.tokens * a.h_q > 0x7fffffffLL - 1024 || ((rows + 127) / 128 + a.batch) * a.h_kv >= (1LL << 20) - 4 * kTicketCtas)
+        return MOA_ERR_CAPACITY;               // (units and pieces are counted in 20 bits)
     if (!ws) return MOA_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return MOA_ERR_ALIGN;
     DeviceState *dev = nullptr;

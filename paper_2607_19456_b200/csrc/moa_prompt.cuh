@@ -24,6 +24,12 @@
 // Work is handed out unit by unit (one CTA per SM; the next one's number comes from a counter; what a unit gives does not depend
 // on who takes it).  Where there are few units their keys are cut into pieces; the CTA that delivers a unit's last piece
 // joins them in order.
+//
+// What bounds it: the softmax.  A tile of each slot takes its scheduler 2118 cycles when nothing else runs (1549
+// without the exponentials; a spilled register is an L2 round trip, since shared memory leaves no L1), the tensor
+// core 2048 in whole tiles and 3072 with the scores by halves, and beside MMA and copy warps a tile of both slots comes out at
+// 2700..3100 cycles: 951 GFLOP of two causal prompts (7001 and 8192 tokens, 32/8 heads of 128) in 0.90..1.03 ms, by the power that
+// is left, against 0.57 ms at the measured GEMM rate.  Rows of 64 halve the products, not the softmax.
 #pragma once
 
 #include "moa_grouped64.cuh"
@@ -364,8 +370,10 @@ __device__ __forceinline__ float2 unpack2f(uint64_t v)
 
 // 2^x for two x at once on the FMA units: x = n + f with |f| <= 1/2, a polynomial in f (least relative error over
 // the interval, fitted for this file: 7.5e-5 of degree 3, 2.6e-6 of degree 4), times 2^n as a bit pattern.  x at or
-// below -127 gives 0.  The special function unit makes 16 results a cycle and SM; a tile of 128 x 128 scores would keep it busy
-// exactly as long as the tensor core takes for the tile's two products, so a share of the weights goes this way.
+// below -127 gives 0; the caller sees to it that x is no larger than 15.  The special function unit makes 16 results a cycle and
+// SM; a tile of 128 x 128 scores would keep it busy exactly as long as the tensor core takes for the tile's two products, so a
+// quarter of the weights goes this way (two slots on a scheduler, cycles for a tile of each: a quarter 2118, an eighth 2064, none
+// 2266; beside the other warps, which share the issue slots, a quarter is the best: 2 x 8192 tokens 899 us, an eighth 926).
 template <int DEG>
 __device__ __forceinline__ float2 exp2_pair(uint64_t x)
 {
@@ -870,6 +878,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
         }
         drain();
         cp_wait<0>();
+        if (!ok)                                           // a wait ran out: tiled copies may be under way
+            for (uint32_t j = nk > (uint32_t)NST ? nk - NST : 0u; j <= nk; ++j) {
+                mbar_wait_bounded(k_full(j % NST), (j / NST) & 1, 1u << 8);
+                mbar_wait_bounded(v_full(j % NST), (j / NST) & 1, 1u << 8);
+            }
         }
     } else {
         // ================= softmax =================
