@@ -1090,6 +1090,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             float M = m, L = l, add = lm;
             if (Q4 && !BF) fa = sigma;
             if (it.pair) {                                 // each thread joins half the columns of both slots
+                if (unread) {                              // (a slot without a tile of this unit has not waited for that yet)
+                    ok = wait_warp(parted, (nj - 1) & 1, abort_flag);
+                    unread = false;
+                    if (!ok) break;
+                }
                 ml[s * 128 + row] = make_float2(m, l);
                 if (Q4) s_more[Q4 ? s : 0][Q4 ? row : 0] = make_float2(lm, sigma);
                 tc::fence_before_sync();
