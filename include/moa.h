@@ -370,8 +370,8 @@ int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int
  *       a token are dense: slices of one projection's output are taken as they are), or NULL: dense.
  *   token_start: device int32[batch + 1], ascending: tokens [token_start[b], token_start[b+1]) are sequence b;
  *       tokens behind the last sequence are left alone (a padded batch), sequences without tokens are allowed.  NULL:
- *       batch is 1 and all tokens are its.  A sequence whose tokens are not inside [0, tokens) in ascending order sets
- *       MOA_STATUS_SEQLEN_RANGE and is left out.
+ *       batch is 1 and all tokens are its.  A sequence whose tokens are not inside [0, tokens) in ascending order, or that
+ *       starts below an earlier entry (of those in [0, tokens]), sets MOA_STATUS_SEQLEN_RANGE and is left out.
  * q, k, v, out are 16-byte aligned, token strides multiples of 16 bytes; `scale` is below 2^127 in size.
  * At most 2^20 - 4096 blocks of 128 rows (a row: one head of one token) in all, over every K/V head and counting one more
  * per sequence and K/V head; more is MOA_ERR_CAPACITY.

@@ -1312,7 +1312,7 @@ static cudaError_t launch_prompt(int format, int dtype, bool paged, const Prompt
 // fp32: a CTA for each unit of 64 rows that there can be, and for each piece of its keys where the units alone do not
 // fill the GPU (256 keys at the least).
 template <class C>
-static cudaError_t launch_prompt32_cfg(const PromptArgs &a, long long keys, cudaStream_t st)
+static cudaError_t launch_prompt32_cfg(const PromptArgs &a, long long keys, const DeviceState &s, cudaStream_t st)
 {
     static bool attr_set[kMaxDevices] = {};
     int dev = 0;
@@ -1326,15 +1326,19 @@ static cudaError_t launch_prompt32_cfg(const PromptArgs &a, long long keys, cuda
     long long splits = a.slot_cap / units;
     if (splits > (keys + 255) / 256) splits = (keys + 255) / 256;
     if (splits < 1) splits = 1;
-    launch_dependent(prompt32_kernel<C>, (int)(units * splits), C::THREADS, C::SMEM, st, a, (int)splits, units);
+    // Each CTA looks through the whole batch for starts that descend.  Up to 512 sequences, four looks of a thread, that is
+    // little beside a unit; with more, a CTA takes several units.
+    long long grid = units * splits;
+    if (a.batch > 512 && grid > 16LL * s.sm_count) grid = 16LL * s.sm_count;
+    launch_dependent(prompt32_kernel<C>, (int)grid, C::THREADS, C::SMEM, st, a, (int)splits, units);
     count_launch();
     return cudaGetLastError();
 }
-static cudaError_t launch_prompt32(bool paged, int d, const PromptArgs &a, cudaStream_t st)
+static cudaError_t launch_prompt32(bool paged, int d, const PromptArgs &a, const DeviceState &s, cudaStream_t st)
 {
     const long long keys = paged ? (long long)a.max_pages * a.page_size : a.tokens;
-    if (d == 128) return paged ? launch_prompt32_cfg<Prompt32Cfg<128, true>>(a, keys, st) : launch_prompt32_cfg<Prompt32Cfg<128, false>>(a, keys, st);
-    return paged ? launch_prompt32_cfg<Prompt32Cfg<64, true>>(a, keys, st) : launch_prompt32_cfg<Prompt32Cfg<64, false>>(a, keys, st);
+    if (d == 128) return paged ? launch_prompt32_cfg<Prompt32Cfg<128, true>>(a, keys, s, st) : launch_prompt32_cfg<Prompt32Cfg<128, false>>(a, keys, s, st);
+    return paged ? launch_prompt32_cfg<Prompt32Cfg<64, true>>(a, keys, s, st) : launch_prompt32_cfg<Prompt32Cfg<64, false>>(a, keys, s, st);
 }
 
 // What both calls share once their own arguments are in `a`: sizes, scale, workspace, launch.
@@ -1364,7 +1368,7 @@ static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d
     cudaError_t e;
     PromptMaps m = {};
     if (format == MOA_KV_F32) {
-        e = launch_prompt32(paged, d, a, st);
+        e = launch_prompt32(paged, d, a, *dev, st);
         if (e != cudaSuccess) return MOA_ERR_CUDA;
         g_last_path = MOA_PATH_PROMPT;
         return MOA_OK;

@@ -82,7 +82,7 @@ struct PromptCfg {
     static constexpr uint32_t OFF_ML = OFF_NF + 2 * D * 4; // [2][128] (m, l) of the slots
     static constexpr uint32_t OFF_ROWS = OFF_ML + 2 * 128 * 8;      // [128] places of a tile's rows, K and V
     static constexpr uint32_t OFF_PLAN = OFF_ROWS + (PAGED ? 128 * 16 : 0);
-    static constexpr uint32_t SMEM = OFF_PLAN + THREADS * 24 + 1024;      // (1024: alignment of the base)
+    static constexpr uint32_t SMEM = OFF_PLAN + THREADS * 28 + 1024;      // (1024: alignment of the base)
     // How far (log2) a score may pass the reference before it moves, and what the weights are taken larger by: those held
     // in fp16 reach 2^15, and 64 weights of 1 are no reason to move.
     static constexpr float AHEAD = BF ? 8.0f : 7.0f;
@@ -93,9 +93,11 @@ struct PromptCfg {
 
 struct PromptSeq { int first, n, past, len; };
 
-// Sequence b; n = 0 where it has no new tokens or is refused (bad: its status).
+// Sequence b; n = 0 where it has no new tokens or is refused (bad: its status).  `floor`: the largest entry of token_start before
+// b's that lies inside the call, carried on to b + 1.  A sequence that starts below it is refused, so no token is two sequences'
+// and the host's bound on the blocks of rows, which follows from the number of tokens, holds whatever the entries are.
 template <bool PAGED>
-__device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b, int &bad)
+__host__ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b, int &floor, int &bad)
 {
     PromptSeq s;
     long long first, next;
@@ -103,7 +105,10 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b, int 
     else if (PAGED) { first = b; next = b + 1; }
     else { first = 0; next = a.tokens; }
     bad = 0;
-    if (first < 0 || next < first || next > a.tokens) { bad = MOA_STATUS_SEQLEN_RANGE; first = next = 0; }
+    const int before = floor;
+    if (first <= a.tokens && first > floor) floor = (int)first;
+    if (next <= a.tokens && next > floor) floor = (int)next;
+    if (first < before || next < first || next > a.tokens) { bad = MOA_STATUS_SEQLEN_RANGE; first = next = 0; }
     s.first = (int)first; s.n = (int)(next - first);
     s.len = PAGED ? a.seq_lens[b] : s.n;
     s.past = s.len - s.n;
@@ -114,10 +119,10 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs &a, int b, int 
     return s;
 }
 
-__device__ __forceinline__ int div_g(const PromptArgs &a, int r) { return (int)(((unsigned long long)(uint32_t)r * a.g_mul) >> a.g_sh); }
+__host__ __device__ __forceinline__ int div_g(const PromptArgs &a, int r) { return (int)(((unsigned long long)(uint32_t)r * a.g_mul) >> a.g_sh); }
 
 // Keys that row r (token r / g) of a sequence sees.
-__device__ __forceinline__ int prompt_sees(const PromptArgs &a, const PromptSeq &s, int r)
+__host__ __device__ __forceinline__ int prompt_sees(const PromptArgs &a, const PromptSeq &s, int r)
 {
     if (!a.causal) return s.len;
     return s.past + div_g(a, r) + 1;
@@ -139,7 +144,7 @@ struct PromptItem {
 struct PromptPlan { int rows, step_max, items; };
 
 template <bool PAGED>
-__device__ __forceinline__ void prompt_counts(const PromptArgs &a, const PromptSeq &s, int R, int T, int &tiles, int &pieces)
+__host__ __device__ __forceinline__ void prompt_counts(const PromptArgs &a, const PromptSeq &s, int R, int T, int &tiles, int &pieces)
 {
     const long long rows = (long long)s.n * a.g;
     tiles = (int)((rows + R - 1) / R);
@@ -150,15 +155,15 @@ __device__ __forceinline__ void prompt_counts(const PromptArgs &a, const PromptS
     pieces = steps > T ? (steps + T - 1) / T : 1;
 }
 
-// Sums of two numbers over the block, the same for every thread.
-__device__ __forceinline__ longlong2 prompt_block_sum(long long x, long long y, longlong2 *scratch)
+// Sums of two numbers over the block, the same for every thread; any: whether any thread's was set.
+__device__ __forceinline__ longlong2 prompt_block_sum(long long x, long long y, int &any, longlong2 *scratch)
 {
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) {
         x += __shfl_xor_sync(0xffffffffu, x, off);
         y += __shfl_xor_sync(0xffffffffu, y, off);
     }
-    __syncthreads();
+    any = __syncthreads_or(any);
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = make_longlong2(x, y);
     __syncthreads();
     longlong2 t = make_longlong2(0, 0);
@@ -166,8 +171,34 @@ __device__ __forceinline__ longlong2 prompt_block_sum(long long x, long long y, 
     return t;
 }
 
-// What a thread keeps of its sequences: how many (items, slots) come before them, and the sequence where it is only one.
-struct PromptGroup { int items, slots; PromptSeq s; };
+// The largest entry of token_start inside the call before those of this thread's sequences b0 .. b1 - 1.  Whole blocks; needed only
+// where some sequence is refused (entries that ascend have none).
+__device__ __forceinline__ int prompt_floor(const PromptArgs &a, int b0, int b1, int *scratch)
+{
+    if (a.token_start == nullptr) return 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int x = 0;
+    for (int b = b0; b < b1; ++b) {
+        const int at = a.token_start[b];
+        if (at <= a.tokens) x = max(x, at);
+    }
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x = max(x, y);
+    }
+    __syncthreads();
+    if (lane == 31) scratch[warp] = x;
+    __syncthreads();
+    x = __shfl_up_sync(0xffffffffu, x, 1);
+    if (lane == 0) x = 0;
+    for (int w = 0; w < warp; ++w) x = max(x, scratch[w]);
+    return x;
+}
+
+// What a thread keeps of its sequences: how many (items, slots) come before them, and the sequence where it is only one, else
+// what the first one may not start below.
+struct PromptGroup { int items, slots; PromptSeq s; int floor; };
 
 // Every CTA finds the same plan: rows of a unit and the most steps (a tile of keys for 256 rows) that a piece has.
 template <bool PAGED>
@@ -176,20 +207,26 @@ __device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs &a, PromptGro
     const int tid = threadIdx.x, nt = blockDim.x;
     const int gs = (a.batch + nt - 1) / nt;                // sequences of a group: one thread's
     const int b0 = min(tid * gs, a.batch), b1 = min(b0 + gs, a.batch);
-    long long units = 0, work = 0;
-    int bad, tiles, pieces;
+    int bad, tiles, pieces, floor = 0;
     PromptSeq s = {0, 0, 0, 0};
-    for (int b = b0; b < b1; ++b) {
-        s = prompt_seq<PAGED>(a, b, bad);
-        if (bad != 0 && report) raise_status(bad);
-        if (s.n == 0) continue;
-        prompt_counts<PAGED>(a, s, 256, 0x7fffffff, tiles, pieces);
-        const long long rows = (long long)s.n * a.g;
-        const int last = (prompt_sees(a, s, (int)rows - 1) + 127) >> 7, front = (prompt_sees(a, s, 0) + 127) >> 7;
-        units += (long long)tiles * a.h_kv;
-        work += rows <= 128 ? (long long)a.h_kv * ((last + 1) >> 1) : (long long)a.h_kv * tiles * (last + front + 1) / 2;
+    longlong2 sums;
+    for (bool again = false;; again = true) {              // (again: what was refused may be a start that the ones behind it are to be held against)
+        long long units = 0, work = 0;
+        int wrong = 0, f = floor;
+        for (int b = b0; b < b1; ++b) {
+            s = prompt_seq<PAGED>(a, b, f, bad);
+            if (bad != 0) { wrong = 1; if (report) raise_status(bad); }
+            if (s.n == 0) continue;
+            prompt_counts<PAGED>(a, s, 256, 0x7fffffff, tiles, pieces);
+            const long long rows = (long long)s.n * a.g;
+            const int last = (prompt_sees(a, s, (int)rows - 1) + 127) >> 7, front = (prompt_sees(a, s, 0) + 127) >> 7;
+            units += (long long)tiles * a.h_kv;
+            work += rows <= 128 ? (long long)a.h_kv * ((last + 1) >> 1) : (long long)a.h_kv * tiles * (last + front + 1) / 2;
+        }
+        sums = prompt_block_sum(units, work, wrong, scratch);
+        if (!wrong || again) break;
+        floor = prompt_floor(a, b0, b1, reinterpret_cast<int *>(scratch + 16));
     }
-    const longlong2 sums = prompt_block_sum(units, work, scratch);
     const int grid = gridDim.x;
     PromptPlan p;
     // 256 rows read K and V half as often; 128 spread better where there are few short units (us, 256 rows against 128: 7 prompts of
@@ -201,14 +238,15 @@ __device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs &a, PromptGro
     for (;;) {                                             // (ends: with T long enough nothing is cut)
         long long all = 0;
         items = slots = 0;
+        int none = 0, f = floor;
         for (int b = b0; b < b1; ++b) {
-            if (gs > 1) s = prompt_seq<PAGED>(a, b, bad);
+            if (gs > 1) s = prompt_seq<PAGED>(a, b, f, bad);
             prompt_counts<PAGED>(a, s, p.rows, (int)min(T, 0x7fffffffLL), tiles, pieces);
             const long long c = (long long)tiles * pieces * a.h_kv;
             if (pieces > 1) { all += c; if (c <= a.slot_cap) slots += (int)c; }
             items += (int)min(c, 0x7fffffffLL);
         }
-        const longlong2 t = prompt_block_sum(all, items, scratch);
+        const longlong2 t = prompt_block_sum(all, items, none, scratch);
         p.items = (int)t.y;
         if (t.x <= a.slot_cap) break;
         T += T / 2;
@@ -229,6 +267,7 @@ __device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs &a, PromptGro
     groups[tid].items = before.x + inc.x - items;
     groups[tid].slots = before.y + inc.y - slots;
     groups[tid].s = s;
+    groups[tid].floor = floor;
     return p;                                              // (a block barrier follows)
 }
 
@@ -244,11 +283,11 @@ __device__ __forceinline__ void prompt_item(const PromptArgs &a, const PromptPla
         if (groups[mid].items <= i) lo = mid; else hi = mid;
     }
     const int gs = (a.batch + nt - 1) / nt;
-    int at = groups[lo].items, slot = groups[lo].slots, bad, tiles = 0, pieces = 0, b = lo * gs;
+    int at = groups[lo].items, slot = groups[lo].slots, bad, tiles = 0, pieces = 0, b = lo * gs, floor = groups[lo].floor;
     PromptSeq s = groups[lo].s;
     for (;; ++b) {
         if (b >= a.batch) return;                          // (not reached: the plan counted the item)
-        if (gs > 1) s = prompt_seq<PAGED>(a, b, bad);
+        if (gs > 1) s = prompt_seq<PAGED>(a, b, floor, bad);
         prompt_counts<PAGED>(a, s, p.rows, p.step_max, tiles, pieces);
         const int c = tiles * pieces * a.h_kv;
         if (i < at + c) break;

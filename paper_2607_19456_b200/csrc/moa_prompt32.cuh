@@ -32,36 +32,63 @@ __device__ __forceinline__ Two in_two(float x)
     return {__float_as_uint(hi), __float_as_uint(x - hi)};
 }
 
+// Unit: sequence b's tiles of 64 rows have the numbers from start_b * g / 64 + b on, which no two sequences share.  The last
+// numbers, whose rows see most keys, come first.
 template <class C>
-__global__ void __launch_bounds__(C::THREADS, 2) prompt32_kernel(const __grid_constant__ PromptArgs a, int splits, int units)
+__device__ __forceinline__ long long prompt32_first(const PromptArgs &a, int b)
+{
+    return (long long)(a.token_start != nullptr ? a.token_start[b] : C::PAGED ? b : 0) * a.g / C::ROWS + b;
+}
+
+// Where the sequences are not all in order: the one that unit x is of, -1: none, looked for by the whole block.
+struct Prompt32Find { PromptSeq s; int b; };
+template <class C>
+__device__ __noinline__ Prompt32Find prompt32_find(const PromptArgs &a, long long x)
+{
+    __shared__ Prompt32Find s_found;
+    __shared__ int s_floor[C::THREADS / 32];
+    const int tid = threadIdx.x, gs = (a.batch + C::THREADS - 1) / C::THREADS, b0 = min(tid * gs, a.batch), b1 = min(b0 + gs, a.batch);
+    int floor = prompt_floor(a, b0, b1, s_floor), bad;
+    __syncthreads();                                       // (the unit before has read its own)
+    if (tid == 0) s_found.b = -1;
+    __syncthreads();
+    for (int b = b0; b < b1; ++b) {
+        const PromptSeq s = prompt_seq<C::PAGED>(a, b, floor, bad);
+        if (bad != 0 && blockIdx.x == 0) raise_status(bad);
+        const long long tile = x - prompt32_first<C>(a, b);
+        if (tile >= 0 && tile * C::ROWS < (long long)s.n * a.g) { s_found.s = s; s_found.b = b; }      // (one thread's, as no two share a token)
+    }
+    __syncthreads();
+    return s_found;
+}
+
+// Piece `piece` of unit `u`; the whole block.  `ordered`: token_start ascends.
+template <class C>
+__device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, int units, int piece, int u, bool ordered)
 {
     constexpr int D = C::D, LD = C::LD, KEYS = C::KEYS, NT = D / 8;
     constexpr bool PAGED = C::PAGED;
     extern __shared__ __align__(16) float smem32[];
     __shared__ int s_flag[2];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    launch_dependents();
-    grid_dependency_wait();
-    int bad;
-    if (blockIdx.x == 0)
-        for (int b = tid; b < a.batch; b += C::THREADS) {
-            prompt_seq<PAGED>(a, b, bad);
-            if (bad != 0) raise_status(bad);
-        }
-
-    // Unit: sequence b's tiles of 64 rows have the numbers from start_b * g / 64 + b on, which no two sequences share.  The last
-    // numbers, whose rows see most keys, come first.
-    const int piece = blockIdx.x % splits, u = blockIdx.x / splits, head = u % a.h_kv;
+    const int head = u % a.h_kv;
     const long long x = units / a.h_kv - 1 - u / a.h_kv;
-    auto first_of = [&](int b) { return (long long)(a.token_start != nullptr ? a.token_start[b] : PAGED ? b : 0) * a.g / C::ROWS + b; };
-    int lo = 0, hi = a.batch;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (first_of(mid) <= x) lo = mid; else hi = mid;
+    int b;
+    PromptSeq s;
+    if (ordered) {
+        int lo = 0, hi = a.batch, floor = 0, bad;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (prompt32_first<C>(a, mid) <= x) lo = mid; else hi = mid;
+        }
+        b = lo;
+        s = prompt_seq<PAGED>(a, b, floor, bad);
+    } else {
+        const Prompt32Find found = prompt32_find<C>(a, x);
+        if (found.b < 0) return;
+        b = found.b; s = found.s;
     }
-    const int b = lo;
-    const PromptSeq s = prompt_seq<PAGED>(a, b, bad);
-    const long long tile = x - first_of(b), all = (long long)s.n * a.g;
+    const long long tile = x - prompt32_first<C>(a, b), all = (long long)s.n * a.g;
     if (tile < 0 || tile * C::ROWS >= all) return;
     const int row0 = (int)tile * C::ROWS, rows = (int)min((long long)C::ROWS, all - row0);
     const int least = prompt_sees(a, s, row0), sees = prompt_sees(a, s, row0 + rows - 1);
@@ -284,6 +311,28 @@ __global__ void __launch_bounds__(C::THREADS, 2) prompt32_kernel(const __grid_co
         }
         const float inv = prompt_sees(a, s, row0 + r) <= 0 ? 0.f : 1.f / total;
         *reinterpret_cast<float2 *>(out_row(r) + col) = make_float2(y0 * inv, y1 * inv);
+    }
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, 2) prompt32_kernel(const __grid_constant__ PromptArgs a, int splits, int units)
+{
+    launch_dependents();
+    grid_dependency_wait();
+    // Every CTA looks whether the entries of token_start ascend: only then does a search by halves find a unit's sequence.
+    int down = 0;
+    if (a.token_start != nullptr)
+        for (int b = threadIdx.x; b < a.batch; b += C::THREADS) down |= a.token_start[b + 1] < a.token_start[b];
+    const bool ordered = !__syncthreads_or(down);
+    if (blockIdx.x == 0 && ordered)
+        for (int b = threadIdx.x; b < a.batch; b += C::THREADS) {
+            int floor = 0, bad;
+            prompt_seq<C::PAGED>(a, b, floor, bad);
+            if (bad != 0) raise_status(bad);
+        }
+    for (long long i = blockIdx.x; i < (long long)units * splits; i += gridDim.x) {
+        if (i != blockIdx.x) __syncthreads();              // (the unit before has read what it keeps in shared memory)
+        prompt32_unit<C>(a, splits, units, (int)(i % splits), (int)(i / splits), ordered);
     }
 }
 
