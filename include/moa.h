@@ -401,7 +401,8 @@ int moa_prompt_attn(const void *q, const void *k, const void *v, void *out, int 
  * the sequence's out untouched; a page number outside [0, num_pages) among the rows that a sequence's tokens see sets
  * MOA_STATUS_PAGE_RANGE, nothing outside the pools is read, and the rows of out that depend on it become NaN.
  * All else (scale, capacity, numbers, workspace, launch) as for moa_prompt_attn.  MOA_KV_INT4: what is rounded to `dtype` is the
- * weight times the row's scale, against eight steps of the row; a (scale, least) pair that is not finite counts as a row of such values.
+ * weight times the row's scale, against eight steps of the row (fp16: what is below 2^-33 of the heaviest row's weight times the
+ * largest scale that the query sees adds nothing); a (scale, least) pair that is not finite counts as a row of such values.
  * A batch of single tokens alone is moa_paged_decode_attn's work (its weights are held in two terms).
  */
 int moa_paged_chunk_attn(const moa_paged_cache *cache, const void *q, void *out, int dtype, long long q_stride, int tokens, int h_q,

@@ -884,7 +884,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             par[128] = row_bad[g] ? nan : row_ok[g] ? fmaf(8.f, kf.x, kf.y) : 0.f;
                             par[256] = row_ok[g] ? vf.x : 0.f;
                             par[384] = row_ok[g] ? fmaf(8.f, vf.x, vf.y) : 0.f;
-                            float top = row_ok[g] ? vf.x : 0.f;
+                            float top = row_ok[g] && fabsf(vf.x) < INFINITY ? fabsf(vf.x) : 0.f;
 #pragma unroll
                             for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
                             if (lane == 0) reinterpret_cast<float *>(smem + C::OFF_PMAX)[ps * 4 + 2 * w + g] = top;
@@ -1019,9 +1019,19 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                                 if (!((e < 32 ? see0 : see1) & (1u << (e & 31)))) x[e] = 0xff800000u;
                         }
                         float sig_new = sigma;
-                        if (scales && h == 0) {
+                        if (scales && h == 0) {            // the largest scale among the rows that this query sees
                             const float4 u = *reinterpret_cast<const float4 *>(smem + C::OFF_PMAX + ps * 16);
-                            const float st = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
+                            float st = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
+                            if (masked && vis < 128) {
+                                st = 0.f;
+#pragma unroll 4
+                                for (int e = 0; e < 128; e += 4) {
+                                    const float4 y = *reinterpret_cast<const float4 *>(par + 256 + e);
+                                    const float z[4] = {fabsf(y.x), fabsf(y.y), fabsf(y.z), fabsf(y.w)};
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) if (e + k < vis && z[k] < INFINITY) st = fmaxf(st, z[k]);
+                                }
+                            }
                             if (st > sigma) sig_new = __uint_as_float((__float_as_uint(st) + 0x007fffffu) & 0x7f800000u);
                         }
                         // The weights by the reference as it is.  Where one may be above 2^AHEAD -- their sum is, or a score that goes
@@ -1074,7 +1084,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             constexpr float kMost = BF ? 256.f : 32768.f;                          // 2^(AHEAD + SHIFT)
                             const float high = mx * a.qscale;
                             const bool far = !none && (m == -INFINITY || !(both.x + both.y <= kMost) || !(high <= ref + C::AHEAD || high == -INFINITY));
-                            if (again || (!__any_sync(0xffffffffu, far) && sig_new == sigma)) break;
+                            if (again || !__any_sync(0xffffffffu, far || sig_new != sigma)) break;
                             float top = -INFINITY;
 #pragma unroll
                             for (int e = 0; e < 64; e += 2) top = max_nan(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
