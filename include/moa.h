@@ -378,7 +378,8 @@ int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int
  * Scores, softmax statistics and sums are fp32 and out is rounded once; for 16-bit types the weight of each row is
  * rounded to that type on its way into the weighted sum (half a step of it; fp16: below 2^-33 of the heaviest row's weight it adds
  * nothing), and bf16 weights are made to 2^-13.  How rows and keys are
- * cut follows from the call's lengths and the number of CTAs, and the order of the sums from that: the same call gives the same bits.
+ * cut follows from the sequences' lengths, the call's sizes (`tokens`, `batch`, heads; not `max_pages`) and the number of CTAs, and
+ * the order of the sums from that: the same call gives the same bits.
  * A value that is not finite makes NaN or infinite: in q, the row; in k, the rows that see it (also those where the
  * definition makes its weight 0); in v, its feature in the rows that see it (NaN also where the definition has an infinity).  What a
  * row does not see does not touch it.

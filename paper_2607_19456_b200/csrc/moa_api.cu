@@ -1309,8 +1309,8 @@ static cudaError_t launch_prompt(int format, int dtype, bool paged, const Prompt
     return launch_prompt_cfg<PromptCfg<MOA_KV_F16, false, D, true>>(a, m, grid, st);
 }
 
-// fp32: a CTA for each unit of 64 rows that there can be, and for each piece of its keys where the units alone do not
-// fill the GPU (256 keys at the least).
+// fp32: a CTA for each unit of 64 rows that there can be, and for each piece of its keys that there can be where the units alone
+// do not fill the GPU (256 keys at the least).  How many pieces a unit has follows from the keys that it sees.
 template <class C>
 static cudaError_t launch_prompt32_cfg(const PromptArgs &a, long long keys, const DeviceState &s, cudaStream_t st)
 {

@@ -92,7 +92,10 @@ __device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, i
     if (tile < 0 || tile * C::ROWS >= all) return;
     const int row0 = (int)tile * C::ROWS, rows = (int)min((long long)C::ROWS, all - row0);
     const int least = prompt_sees(a, s, row0), sees = prompt_sees(a, s, row0 + rows - 1);
-    const int tiles = (sees + KEYS - 1) / KEYS, t0 = (int)((long long)tiles * piece / splits), t1 = (int)((long long)tiles * (piece + 1) / splits);
+    // Pieces of this unit: 8 tiles each at the least, of those that were launched.
+    const int tiles = (sees + KEYS - 1) / KEYS, pieces = max(1, min(splits, (tiles + 7) / 8));
+    if (piece >= pieces) return;
+    const int t0 = (int)((long long)tiles * piece / pieces), t1 = (int)((long long)tiles * (piece + 1) / pieces);
 
     float *const sQ = smem32, *const sK = smem32 + C::OFF_K, *const sV = smem32 + C::OFF_V;
     int *const nf = reinterpret_cast<int *>(smem32 + C::OFF_NF);
@@ -262,7 +265,7 @@ __device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, i
         const int row = row0 + r, tok = div_g(a, row);
         return reinterpret_cast<float *>(a.out + (long long)(s.first + tok) * a.o_st + ((long long)head * a.g + (row - tok * a.g)) * (D * 4));
     };
-    if (splits == 1) {
+    if (pieces == 1) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             if (ra + 8 * r >= rows) continue;
@@ -290,7 +293,7 @@ __device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, i
     __syncthreads();
     if (tid == 0) {
         unsigned long long *word = a.tickets + u;
-        const bool last = ticket_arrive(word, a.ticket_tag) + 1 == (unsigned)splits;
+        const bool last = ticket_arrive(word, a.ticket_tag) + 1 == (unsigned)pieces;
         if (last) *word = 0;
         __threadfence();
         s_flag[1] = last;
@@ -301,8 +304,8 @@ __device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, i
     for (int i = tid; i < rows * (D / 2); i += C::THREADS) {
         const int r = i / (D / 2), col = i % (D / 2) * 2;
         float top = -INFINITY, total = 0.f, y0 = 0.f, y1 = 0.f;
-        for (int p = 0; p < splits; ++p) top = max_nan(top, __ldcg(reinterpret_cast<const float2 *>(p0 + p * slot + r * (D + 2) + D)).x);
-        for (int p = 0; p < splits; ++p) {
+        for (int p = 0; p < pieces; ++p) top = max_nan(top, __ldcg(reinterpret_cast<const float2 *>(p0 + p * slot + r * (D + 2) + D)).x);
+        for (int p = 0; p < pieces; ++p) {
             const float *const pp = p0 + p * slot + r * (D + 2);
             const float2 e = __ldcg(reinterpret_cast<const float2 *>(pp + D)), y = __ldcg(reinterpret_cast<const float2 *>(pp + col));
             const float w = exp2_diff(e.x, top);
