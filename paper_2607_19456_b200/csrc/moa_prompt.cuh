@@ -534,12 +534,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                         const uint32_t kt = nk + (uint32_t)(pair ? 2 * (i + 1) + s : i + 1), kst = kt % NST;
                         const bool more = i + 1 < cnt;
                         if (i >= 0) {
-                            // (V behind the weights, not before: in a unit of few rows this warp sees every second tile only, and a
-                            // wait tells a phase that is over by its parity, so the one before, the other slot's, has to be over.
-                            // The first weights of a unit come behind the join of the one before, when all its tiles are used up;
-                            // tiles that slot 0 of more rows does not see are looked through before the next unit's Q is there.)
-                            ok = wait_warp(p_full(s, h), np & 1, abort_flag);
-                            if (h == 0) ok = ok && wait_warp(v_full(vst), (vt / NST) & 1, abort_flag);
+                            // A unit's first V behind its first weights: in a unit of few rows this warp sees every second tile only, and a
+                            // wait tells a phase that is over by its parity, so the one before, the other slot's, has to be over by then.
+                            // The first weights come behind the join of the unit before, when all its tiles are used up.  (Tiles that slot 0
+                            // of more rows does not see are looked through before the next unit's Q is there.)  From then on V
+                            // first: a look at its barrier behind every tile's weights costs 1 % of the long cases.
+                            const bool late = u == 0;
+                            const uint32_t v_bar = v_full(vst), v_par = (vt / NST) & 1, p_bar = p_full(s, h), p_par = np & 1;
+                            if (h == 0) ok = wait_warp(late ? p_bar : v_bar, late ? p_par : v_par, abort_flag);
+                            ok = ok && wait_warp(late ? v_bar : p_bar, late ? v_par : p_par, abort_flag);
                             if (!ok) break;
                             np += h;
                             tc::fence_after_sync();

@@ -37,7 +37,7 @@ class Barrier:
 class Model:
     """units: (pair, tiles of slot 0, tiles of slot 1); a pair takes them by turns, else slot 0 sees the first of slot 1's.
 
-    weights_first: an issuing warp waits for the weights before it waits for V.
+    weights_first: of a step's number: whether an issuing warp waits there for the weights before it waits for V.
     join_waits: a slot waits for the other one's reads of the join before, ahead of writing its own share of the next."""
 
     def __init__(self, rng, units, stages, weights_first, join_waits):
@@ -115,7 +115,7 @@ class Model:
                     if i >= 0:
                         waits = [(self.p_full[s][h], np)]
                         if h == 0:
-                            waits.insert(1 if self.weights_first else 0, (self.v_full[vt % self.NST], vt // self.NST))
+                            waits.insert(1 if self.weights_first(u) else 0, (self.v_full[vt % self.NST], vt // self.NST))
                         for w in waits:
                             yield from self.wait(*w)
                         np += h

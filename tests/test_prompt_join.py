@@ -20,7 +20,7 @@ def test_nothing_is_written_before_it_has_been_read(stages):
     order = join_waits()
     for seed in range(600):
         rng = random.Random(seed)
-        Model(rng, some_units(rng), stages, True, order).run()
+        Model(rng, some_units(rng), stages, lambda u: u == 0, order).run()
 
 
 def test_the_model_sees_a_join_without_the_wait():
@@ -28,7 +28,7 @@ def test_the_model_sees_a_join_without_the_wait():
     for seed in range(200):
         rng = random.Random(seed)
         try:
-            Model(rng, some_units(rng), 2, True, False).run()
+            Model(rng, some_units(rng), 2, lambda u: u == 0, False).run()
         except Early:
             early += 1
     assert early > 0
