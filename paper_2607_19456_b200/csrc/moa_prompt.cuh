@@ -1027,7 +1027,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             float st = fmaxf(fmaxf(u.x, u.y), fmaxf(u.z, u.w));
                             if (masked && vis < 128) {
                                 st = 0.f;
-#pragma unroll 4
+#pragma unroll 1
                                 for (int e = 0; e < 128; e += 4) {
                                     const float4 y = *reinterpret_cast<const float4 *>(par + 256 + e);
                                     const float z[4] = {fabsf(y.x), fabsf(y.y), fabsf(y.z), fabsf(y.w)};
