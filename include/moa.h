@@ -495,12 +495,16 @@ const char *moa_strerror(int code);
  *                        (64 head lanes, smaller groups padded); 1 = only the kernel with
  *                        these operands in shared memory (groups of exactly 16, 32, 64).
  *   MOA_OPT_WAIT_LIMIT : number of polls after which the FMA streaming kernel gives up waiting
- *                        for a tile it has requested (0 = the built-in limit of 2^22 polls).
+ *                        for a tile it has requested, and the kernel of moa_prompt_attn and
+ *                        moa_paged_chunk_attn (16 and 4 bits) any of its waits, behind 64 polls of up
+ *                        to a millisecond each (0 = the built-in limit of 2^22 polls).
  *                        When a wait runs out the kernel sets MOA_STATUS_WAIT_TIMEOUT, stops
  *                        consuming and returns; the results of that call are invalid.
  *   MOA_OPT_TEST_SKIP_COPY : test hook for exactly that path: the copies of the row block with
- *                        this flat index are announced but never issued (nothing is in flight,
- *                        nothing out of bounds), so the wait for them runs out (-1 = off).
+ *                        this flat index (prompt kernel: of K's tiles of 128 keys with this
+ *                        number, where they are tiled copies) are announced but never issued
+ *                        (nothing is in flight, nothing out of bounds), so the wait for them runs
+ *                        out (-1 = off).
  * moa_last_path() reports which kernel family the last successful decode call used.
  */
 #define MOA_OPT_FORCE_PATH 1

@@ -1365,6 +1365,8 @@ static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d
     unsigned long long tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
     if (tag == 0) tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
     a.ticket_tag = (tag << 20) | 1ull;
+    a.wait_limit = g_wait_limit > 0 ? g_wait_limit : (int)kWaitLimit;
+    a.skip_tile = (int)g_skip_copy_block;
     cudaError_t e;
     PromptMaps m = {};
     if (format == MOA_KV_F32) {

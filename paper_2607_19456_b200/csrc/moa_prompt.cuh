@@ -63,6 +63,8 @@ struct PromptArgs {
     int slot_cap, slot_rows;
     unsigned long long *tickets;     // slot_cap counters of pieces, then the counter of items handed out
     unsigned long long ticket_tag;
+    int wait_limit;                  // polls after which a wait gives up (behind the first 64)
+    int skip_tile;                   // test hook: this tile's K is announced and never copied (tiled copies); -1: none
 };
 
 template <int FMT_, bool BF_, int D_, bool PAGED_>
@@ -357,7 +359,7 @@ __device__ __forceinline__ void mma_16_ts(uint32_t d, uint32_t a, uint64_t b, ui
 // Wait of a whole warp: all lanes leave it with the same answer.  The first polls are a loop of a few instructions (code
 // that is fetched from far away costs as much as the wait) and may each be suspended for up to a millisecond: without
 // the hint they take issue slots from the softmax (two prompts of 7001 and 8192 tokens 1280 us instead of 1003, at a step
-// on the way).
+// on the way).  abort_flag[1]: the limit of the polls behind them.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag)
 {
     uint32_t ok;
@@ -368,7 +370,9 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
             "DONE_%=:\n\tselp.u32 %0, 1, 0, p;\n\t}"
             : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
     if (__all_sync(0xffffffffu, ok)) return true;
-    for (uint32_t it = 0; it < kWaitLimit; ++it) {
+    const uint32_t limit = (uint32_t)abort_flag[1];
+#pragma unroll 1
+    for (uint32_t it = 0; it < limit; ++it) {
         if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
         if ((it & 15u) == 15u && __any_sync(0xffffffffu, *abort_flag)) return false;
     }
@@ -450,12 +454,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
     __shared__ PromptItem s_item[2];
     __shared__ longlong2 s_scratch[16 + 8];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort, s_last, s_nf[2];
+    __shared__ int s_abort[2], s_last, s_nf[2];
     __shared__ float2 s_more[Q4 ? 2 : 1][Q4 ? 128 : 1];      // 4 bits: what joins the slots beside (m, l)
     const uint32_t base = (smem_u32(smem_prompt) + 1023u) & ~1023u;
     unsigned char *const smem = smem_prompt + (base - smem_u32(smem_prompt));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    volatile int *abort_flag = &s_abort;
+    volatile int *abort_flag = s_abort;
 
     const uint32_t bar0 = smem_u32(bars);
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
@@ -486,7 +490,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
         mbar_init(joined, 8); mbar_init(parted, 8); mbar_init(delivered, 8); mbar_init(counted, 1); mbar_init(drained, 2);
         for (int i = 0; i < C::NPAR; ++i) mbar_init(par_full(i), 2);
         mbar_fence_init();
-        s_abort = 0;
+        s_abort[0] = 0;
+        s_abort[1] = a.wait_limit;
     }
     if (warp == 10) tc::tmem_alloc(smem_u32(&s_tmem), 512);
     if (tid == 32 * 8 && a.box > 0) { tc::prefetch_tmap(&map_k); tc::prefetch_tmap(&map_v); }
@@ -855,7 +860,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             if (!ok) break;
                             if (lane == 0) mbar_expect_tx(k_full(st), bytes);
                             __syncwarp();
-                            if (copies) tc::tma_load_4d(base + C::OFF_K + st * C::KV + to, &map_k, 64 * half, c1, it.head, c3, k_full(st));
+                            if (copies && it.t0 + t != a.skip_tile) tc::tma_load_4d(base + C::OFF_K + st * C::KV + to, &map_k, 64 * half, c1, it.head, c3, k_full(st));
                             if (t == 0) { copy_q(); if (!ok) break; }
                             ok = nk < NST || wait_free(v_empty(st), (nk / NST - 1) & 1);
                             if (!ok) break;
