@@ -1311,28 +1311,35 @@ static cudaError_t launch_prompt(int format, int dtype, bool paged, const Prompt
 
 // fp32: a CTA for each unit of 64 rows that there can be, and for each piece of its keys that there can be where the units alone
 // do not fill the GPU (256 keys at the least).  How many pieces a unit has follows from the keys that it sees.
-template <class C>
-static cudaError_t launch_prompt32_cfg(const PromptArgs &a, long long keys, const DeviceState &s, cudaStream_t st)
+template <class C, bool MANY>
+static cudaError_t launch_prompt32_cfg(const PromptArgs &a, int splits, int units, int grid, cudaStream_t st)
 {
     static bool attr_set[kMaxDevices] = {};
     int dev = 0;
     cudaGetDevice(&dev);
     if (!attr_set[dev]) {
-        cudaError_t e = cudaFuncSetAttribute(prompt32_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
+        cudaError_t e = cudaFuncSetAttribute(prompt32_kernel<C, MANY>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
+    launch_dependent(prompt32_kernel<C, MANY>, grid, C::THREADS, C::SMEM, st, a, splits, units);
+    count_launch();
+    return cudaGetLastError();
+}
+template <class C>
+static cudaError_t launch_prompt32_cfg(const PromptArgs &a, long long keys, const DeviceState &s, cudaStream_t st)
+{
     const int units = (int)(((long long)a.tokens * a.g / C::ROWS + a.batch) * a.h_kv);
+    // Many sequences: every CTA looks through the batch for starts that descend, so one takes several units (CTAs per SM that were tried: 16;
+    // 4000 prompts of 1..30 tokens 213 us, with a CTA for every unit 307 at a step on the way).
+    if (a.batch > kPrompt32Few) {
+        const int most = 16 * s.sm_count;
+        return launch_prompt32_cfg<C, true>(a, 1, units, units < most ? units : most, st);
+    }
     long long splits = a.slot_cap / units;
     if (splits > (keys + 255) / 256) splits = (keys + 255) / 256;
     if (splits < 1) splits = 1;
-    // Each CTA looks through the whole batch for starts that descend.  Up to 512 sequences, four looks of a thread, that is
-    // little beside a unit; with more, a CTA takes several units.
-    long long grid = units * splits;
-    if (a.batch > 512 && grid > 16LL * s.sm_count) grid = 16LL * s.sm_count;
-    launch_dependent(prompt32_kernel<C>, (int)grid, C::THREADS, C::SMEM, st, a, (int)splits, units);
-    count_launch();
-    return cudaGetLastError();
+    return launch_prompt32_cfg<C, false>(a, (int)splits, units, (int)(units * splits), st);
 }
 static cudaError_t launch_prompt32(bool paged, int d, const PromptArgs &a, const DeviceState &s, cudaStream_t st)
 {

@@ -40,6 +40,8 @@ __device__ __forceinline__ long long prompt32_first(const PromptArgs &a, int b)
     return (long long)(a.token_start != nullptr ? a.token_start[b] : C::PAGED ? b : 0) * a.g / C::ROWS + b;
 }
 
+constexpr int kPrompt32Few = 512;       // sequences up to which a CTA has one unit
+
 // Where the sequences are not all in order: the one that unit x is of, -1: none, looked for by the whole block.
 struct Prompt32Find { PromptSeq s; int b; };
 template <class C>
@@ -62,9 +64,9 @@ __device__ __noinline__ Prompt32Find prompt32_find(const PromptArgs &a, long lon
     return s_found;
 }
 
-// Piece `piece` of unit `u`; the whole block.  `ordered`: token_start ascends.
-template <class C>
-__device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, int units, int piece, int u, bool ordered)
+// Piece `piece` of unit `u`; the whole block.  down(): whether this thread has seen an entry of token_start below the one before it.
+template <class C, class Down>
+__device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, int units, int piece, int u, const Down &down)
 {
     constexpr int D = C::D, LD = C::LD, KEYS = C::KEYS, NT = D / 8;
     constexpr bool PAGED = C::PAGED;
@@ -73,17 +75,20 @@ __device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, i
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int head = u % a.h_kv;
     const long long x = units / a.h_kv - 1 - u / a.h_kv;
-    int b;
-    PromptSeq s;
-    if (ordered) {
-        int lo = 0, hi = a.batch, floor = 0, bad;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (prompt32_first<C>(a, mid) <= x) lo = mid; else hi = mid;
-        }
-        b = lo;
-        s = prompt_seq<PAGED>(a, b, floor, bad);
-    } else {
+    // The last sequence whose first number is at most x, by steps of 128 entries at a time.
+    int b = 0, end = a.batch, floor = 0, bad;
+    while (end - b > 1) {
+        const int step = (end - b + C::THREADS - 1) / C::THREADS, at = b + tid * step;
+        const int n = __syncthreads_count(at < end && prompt32_first<C>(a, at) <= x);
+        b += max(n - 1, 0) * step;
+        end = min(b + step, end);
+    }
+    PromptSeq s = prompt_seq<PAGED>(a, b, floor, bad);
+    float *const sQ = smem32, *const sK = smem32 + C::OFF_K, *const sV = smem32 + C::OFF_V;
+    int *const nf = reinterpret_cast<int *>(smem32 + C::OFF_NF);
+    for (int f = tid; f < D; f += C::THREADS) nf[f] = 0x7fffffff;
+    if (tid < 2) s_flag[tid] = 0;
+    if (__syncthreads_or(down())) {                        // the entries do not ascend: the search has found anything
         const Prompt32Find found = prompt32_find<C>(a, x);
         if (found.b < 0) return;
         b = found.b; s = found.s;
@@ -97,11 +102,6 @@ __device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, i
     if (piece >= pieces) return;
     const int t0 = (int)((long long)tiles * piece / pieces), t1 = (int)((long long)tiles * (piece + 1) / pieces);
 
-    float *const sQ = smem32, *const sK = smem32 + C::OFF_K, *const sV = smem32 + C::OFF_V;
-    int *const nf = reinterpret_cast<int *>(smem32 + C::OFF_NF);
-    for (int f = tid; f < D; f += C::THREADS) nf[f] = 0x7fffffff;
-    if (tid < 2) s_flag[tid] = 0;
-    __syncthreads();
     // ---- copies
     constexpr int CPR = D / 4, RPI = C::THREADS / CPR;     // 16-byte chunks of a row, rows per pass of the block
     const int chunk = tid % CPR, rsub = tid / CPR;
@@ -304,38 +304,72 @@ __device__ __forceinline__ void prompt32_unit(const PromptArgs &a, int splits, i
     for (int i = tid; i < rows * (D / 2); i += C::THREADS) {
         const int r = i / (D / 2), col = i % (D / 2) * 2;
         float top = -INFINITY, total = 0.f, y0 = 0.f, y1 = 0.f;
-        for (int p = 0; p < pieces; ++p) top = max_nan(top, __ldcg(reinterpret_cast<const float2 *>(p0 + p * slot + r * (D + 2) + D)).x);
-        for (int p = 0; p < pieces; ++p) {
-            const float *const pp = p0 + p * slot + r * (D + 2);
-            const float2 e = __ldcg(reinterpret_cast<const float2 *>(pp + D)), y = __ldcg(reinterpret_cast<const float2 *>(pp + col));
-            const float w = exp2_diff(e.x, top);
-            total = fmaf(e.y, w, total);
-            y0 = fmaf(y.x, w, y0); y1 = fmaf(y.y, w, y1);
+        // (eight pieces' loads under way at once: left to the compiler, 148 pieces took 240 us in one build and 325 in another)
+        constexpr int AT_ONCE = 8;
+        const float *const mine = p0 + r * (D + 2);
+        for (int p = 0; p < pieces; p += AT_ONCE) {
+            float m8[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) m8[k] = p + k < pieces ? __ldcg(reinterpret_cast<const float2 *>(mine + (p + k) * slot + D)).x : -INFINITY;
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) top = max_nan(top, m8[k]);
+        }
+        for (int p = 0; p < pieces; p += AT_ONCE) {
+            float2 e[AT_ONCE], y[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const bool in = p + k < pieces;
+                e[k] = in ? __ldcg(reinterpret_cast<const float2 *>(mine + (p + k) * slot + D)) : make_float2(-INFINITY, 0.f);
+                y[k] = in ? __ldcg(reinterpret_cast<const float2 *>(mine + (p + k) * slot + col)) : make_float2(0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const float w = exp2_diff(e[k].x, top);
+                total = fmaf(e[k].y, w, total);
+                y0 = fmaf(y[k].x, w, y0); y1 = fmaf(y[k].y, w, y1);
+            }
         }
         const float inv = prompt_sees(a, s, row0 + r) <= 0 ? 0.f : 1.f / total;
         *reinterpret_cast<float2 *>(out_row(r) + col) = make_float2(y0 * inv, y1 * inv);
     }
 }
 
-template <class C>
+// MANY: more than kPrompt32Few sequences, and a CTA takes several units.
+template <class C, bool MANY>
 __global__ void __launch_bounds__(C::THREADS, 2) prompt32_kernel(const __grid_constant__ PromptArgs a, int splits, int units)
 {
     launch_dependents();
     grid_dependency_wait();
-    // Every CTA looks whether the entries of token_start ascend: only then does a search by halves find a unit's sequence.
-    int down = 0;
-    if (a.token_start != nullptr)
-        for (int b = threadIdx.x; b < a.batch; b += C::THREADS) down |= a.token_start[b + 1] < a.token_start[b];
-    const bool ordered = !__syncthreads_or(down);
-    if (blockIdx.x == 0 && ordered)
+    if (blockIdx.x == 0)
         for (int b = threadIdx.x; b < a.batch; b += C::THREADS) {
             int floor = 0, bad;
             prompt_seq<C::PAGED>(a, b, floor, bad);
             if (bad != 0) raise_status(bad);
         }
-    for (long long i = blockIdx.x; i < (long long)units * splits; i += gridDim.x) {
-        if (i != blockIdx.x) __syncthreads();              // (the unit before has read what it keeps in shared memory)
-        prompt32_unit<C>(a, splits, units, (int)(i % splits), (int)(i / splits), ordered);
+    // Every CTA looks whether the entries of token_start ascend: only then does a search find a unit's sequence.
+    if constexpr (MANY) {
+        int down = 0;
+        if (a.token_start != nullptr)
+            for (int b = threadIdx.x; b < a.batch; b += C::THREADS) down |= a.token_start[b + 1] < a.token_start[b];
+        for (int i = blockIdx.x; i < units; i += gridDim.x) {          // (with so many units none is cut)
+            if (i != blockIdx.x) __syncthreads();          // (the unit before has read what it keeps in shared memory)
+            prompt32_unit<C>(a, 1, units, 0, i, [&] { return down; });
+        }
+    } else {
+        constexpr int N = kPrompt32Few / C::THREADS;       // (they are on their way while the unit is looked for)
+        int x[N] = {}, y[N] = {};
+        if (a.token_start != nullptr)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int b = threadIdx.x + i * C::THREADS;
+                if (b < a.batch) { x[i] = a.token_start[b]; y[i] = a.token_start[b + 1]; }
+            }
+        prompt32_unit<C>(a, splits, units, blockIdx.x % splits, blockIdx.x / splits, [&] {
+            int down = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) down |= y[i] < x[i];
+            return down;
+        });
     }
 }
 

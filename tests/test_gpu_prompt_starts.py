@@ -70,3 +70,22 @@ def test_chunks_whose_starts_descend(fmt):
     check_chunk(out[:50], p, q[:50], [50], dtype, 0.1)
     p.lens = kept
     assert bool((out[50:75] == -3).all())
+
+
+@pytest.mark.parametrize("batch", [128, 129, 511, 512, 513, 20000])
+def test_fp32_by_number_of_sequences(batch):
+    """Where the search takes another round, and where a CTA starts to take several units; the last sequence is out of order."""
+    rng = np.random.default_rng(batch)
+    new = rng.integers(0, 5, batch)
+    starts = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    tokens = int(starts[-1])
+    x = torch.from_numpy(rng.standard_normal((tokens, 5 * 64)).astype(np.float32)).cuda()
+    out = prompt(x, 3, 1, 64, new.tolist(), moa.F32, True, 0.1)
+    assert moa.moa_device_status() == 0
+    check_prompt(out, x, 3, 1, 64, new.tolist(), moa.F32, True, 0.1)
+    starts[-2] = tokens - 1 if starts[-2] != tokens - 1 else tokens       # one sequence longer or shorter than the one behind it
+    starts[-1] = starts[-2] - 1
+    again = prompt(x, 3, 1, 64, new.tolist(), moa.F32, True, 0.1, starts=torch.from_numpy(starts).cuda())
+    assert moa.moa_device_status() == moa.STATUS_SEQLEN_RANGE
+    same = int(starts[-3])
+    assert torch.equal(again[:same], out[:same])
