@@ -1372,7 +1372,7 @@ static int prompt_launch(PromptArgs &a, int format, int dtype, bool paged, int d
     unsigned long long tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
     if (tag == 0) tag = g_launch_tag.fetch_add(1) & ((1ull << 44) - 1ull);
     a.ticket_tag = (tag << 20) | 1ull;
-    a.wait_limit = g_wait_limit > 0 ? g_wait_limit : (int)kWaitLimit;
+    a.wait_limit = g_wait_limit > 0 ? (uint32_t)g_wait_limit : kWaitLimit;
     a.skip_tile = (int)g_skip_copy_block;
     cudaError_t e;
     PromptMaps m = {};

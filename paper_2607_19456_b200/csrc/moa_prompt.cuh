@@ -63,7 +63,7 @@ struct PromptArgs {
     int slot_cap, slot_rows;
     unsigned long long *tickets;     // slot_cap counters of pieces, then the counter of items handed out
     unsigned long long ticket_tag;
-    int wait_limit;                  // polls after which a wait gives up (behind the first 64)
+    uint32_t wait_limit;             // polls after which a wait gives up (behind the first 64)
     int skip_tile;                   // test hook: this tile's K is announced and never copied (tiled copies); -1: none
 };
 
@@ -359,8 +359,9 @@ __device__ __forceinline__ void mma_16_ts(uint32_t d, uint32_t a, uint64_t b, ui
 // Wait of a whole warp: all lanes leave it with the same answer.  The first polls are a loop of a few instructions (code
 // that is fetched from far away costs as much as the wait) and may each be suspended for up to a millisecond: without
 // the hint they take issue slots from the softmax (two prompts of 7001 and 8192 tokens 1280 us instead of 1003, at a step
-// on the way).  abort_flag[1]: the limit of the polls behind them.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+// on the way).  `limit`: of the polls behind them, from the arguments: kept in shared memory beside the flag it cost 3 % of
+// the long cases, a load for each wait that comes this far.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t limit)
 {
     uint32_t ok;
     asm volatile(
@@ -370,7 +371,6 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
             "DONE_%=:\n\tselp.u32 %0, 1, 0, p;\n\t}"
             : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
     if (__all_sync(0xffffffffu, ok)) return true;
-    const uint32_t limit = (uint32_t)abort_flag[1];
 #pragma unroll 1
     for (uint32_t it = 0; it < limit; ++it) {
         if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
@@ -454,12 +454,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
     __shared__ PromptItem s_item[2];
     __shared__ longlong2 s_scratch[16 + 8];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort[2], s_last, s_nf[2];
+    __shared__ int s_abort, s_last, s_nf[2];
     __shared__ float2 s_more[Q4 ? 2 : 1][Q4 ? 128 : 1];      // 4 bits: what joins the slots beside (m, l)
     const uint32_t base = (smem_u32(smem_prompt) + 1023u) & ~1023u;
     unsigned char *const smem = smem_prompt + (base - smem_u32(smem_prompt));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    volatile int *abort_flag = s_abort;
+    volatile int *abort_flag = &s_abort;
 
     const uint32_t bar0 = smem_u32(bars);
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
@@ -490,8 +490,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
         mbar_init(joined, 8); mbar_init(parted, 8); mbar_init(delivered, 8); mbar_init(counted, 1); mbar_init(drained, 2);
         for (int i = 0; i < C::NPAR; ++i) mbar_init(par_full(i), 2);
         mbar_fence_init();
-        s_abort[0] = 0;
-        s_abort[1] = a.wait_limit;
+        s_abort = 0;
     }
     if (warp == 10) tc::tmem_alloc(smem_u32(&s_tmem), 512);
     if (tid == 32 * 8 && a.box > 0) { tc::prefetch_tmap(&map_k); tc::prefetch_tmap(&map_v); }
@@ -522,13 +521,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             uint32_t nk = 0, nq = 0, np = 0;               // tiles of keys, items, own tiles so far
             bool ok = true;
             for (uint32_t n = 0; ok; ++n) {
-                if (!wait_warp(item_full(n & 1), (n >> 1) & 1, abort_flag)) { ok = false; break; }
+                if (!wait_warp(item_full(n & 1), (n >> 1) & 1, abort_flag, a.wait_limit)) { ok = false; break; }
                 const PromptItem &it = s_item[n & 1];
                 if (it.rows == 0) break;
                 const int cnt = prompt_steps(it, s), other = prompt_steps(it, s ^ 1);
                 const bool pair = it.pair;
                 if (max(cnt, other) > 0) {
-                    ok = wait_warp(q_full, nq & 1, abort_flag);
+                    ok = wait_warp(q_full, nq & 1, abort_flag, a.wait_limit);
                     const uint32_t qa = sQ + (pair ? 0u : (uint32_t)(s * C::KV));
                     if (cnt == 0 && lane == 0) tc::mbar_arrive(q_empty);
                     // step (i, h): half h of tile i into the weighted sum, then the scores of half h of tile i + 1 in their place
@@ -546,8 +545,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             // first: a look at its barrier behind every tile's weights costs 1 % of the long cases.
                             const bool late = u == 0;
                             const uint32_t v_bar = v_full(vst), v_par = (vt / NST) & 1, p_bar = p_full(s, h), p_par = np & 1;
-                            if (h == 0) ok = wait_warp(late ? p_bar : v_bar, late ? p_par : v_par, abort_flag);
-                            ok = ok && wait_warp(late ? v_bar : p_bar, late ? v_par : p_par, abort_flag);
+                            if (h == 0) ok = wait_warp(late ? p_bar : v_bar, late ? p_par : v_par, abort_flag, a.wait_limit);
+                            ok = ok && wait_warp(late ? v_bar : p_bar, late ? v_par : p_par, abort_flag, a.wait_limit);
                             if (!ok) break;
                             np += h;
                             tc::fence_after_sync();
@@ -571,7 +570,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                         // and takes whole tiles (64 x 4 draft tokens 296 us; by halves 450).
                         if (more && (h == 1 || !pair)) {
                             if (h == 0 || pair) {
-                                ok = wait_warp(k_full(kst), (kt / NST) & 1, abort_flag);
+                                ok = wait_warp(k_full(kst), (kt / NST) & 1, abort_flag, a.wait_limit);
                                 if (!ok) break;
                                 tc::fence_after_sync();
                             }
@@ -652,7 +651,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             }
         };
         auto retire = [&]() {                              // they have arrived
-            if (pend_tma) { wait_warp(landed(w), lands & 1, abort_flag); ++lands; }
+            if (pend_tma) { wait_warp(landed(w), lands & 1, abort_flag, a.wait_limit); ++lands; }
             if (pend_tile >= 0) look();
             tc::fence_async_smem();
             __syncwarp();
@@ -670,7 +669,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
         auto wait_free = [&](uint32_t b, uint32_t parity) {
             if (test_warp(b, parity)) return true;
             drain();                  // what this waits for may need them
-            return wait_warp(b, parity, abort_flag);
+            return wait_warp(b, parity, abort_flag, a.wait_limit);
         };
 
         // Item n: drawn when the copies of the one before are issued (drawing it a tile earlier changed nothing).
@@ -948,7 +947,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
         uint32_t ns = 0, no = 0, nj = 0, nc = 0, np = 0;   // uses of s_full, o_full, joins, pieces, tiles of keys before the item
         bool ok = true, unread = false;                    // unread: the other slot may still read this slot's sums
         for (uint32_t n = 0; ok; ++n) {
-            ok = wait_warp(item_full(n & 1), (n >> 1) & 1, abort_flag);
+            ok = wait_warp(item_full(n & 1), (n >> 1) & 1, abort_flag, a.wait_limit);
             if (!ok) break;
             const PromptItem &it = s_item[n & 1];
             if (it.rows == 0) break;
@@ -977,13 +976,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             for (int i = 0; ok && i < cnt; ++i, ++ns) {
                 const int t = it.t0 + (it.pair ? 2 * i + s : i);
                 if (i == 0 && unread) {                    // (the join before: the other slot's reads come before these weights)
-                    ok = wait_warp(parted, (nj - 1) & 1, abort_flag);
+                    ok = wait_warp(parted, (nj - 1) & 1, abort_flag, a.wait_limit);
                     unread = false;
                     if (!ok) break;
                 }
                 const uint32_t ps = (np + (uint32_t)(t - it.t0)) % C::NPAR;
                 if (Q4) {
-                    ok = wait_warp(par_full(ps), ((np + (uint32_t)(t - it.t0)) / C::NPAR) & 1, abort_flag);
+                    ok = wait_warp(par_full(ps), ((np + (uint32_t)(t - it.t0)) / C::NPAR) & 1, abort_flag, a.wait_limit);
                     if (!ok) break;
                 }
                 if (!dead) {
@@ -994,7 +993,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                     const bool scales = Q4 && !BF;
 #pragma unroll 1
                     for (int h = 0; h < 2; ++h) {          // 64 keys at a time: the first half's product runs under the second's weights
-                        ok = wait_warp(s_full(s, h), ns & 1, abort_flag);
+                        ok = wait_warp(s_full(s, h), ns & 1, abort_flag, a.wait_limit);
                         if (!ok) break;
                         tc::fence_after_sync();
                         uint32_t x[64];
@@ -1106,7 +1105,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                             if (scales) { if (sigma > 0.f) f *= sigma / sig_new; sigma = sig_new; }
                             m = mn;
                             if (i > 0 || h == 1) {         // (the half before is on its way into the sum)
-                                ok = wait_warp(summed(s), (h ^ 1) & 1, abort_flag);
+                                ok = wait_warp(summed(s), (h ^ 1) & 1, abort_flag, a.wait_limit);
                                 if (!ok) break;
                                 tc::fence_after_sync();
 #pragma unroll 1
@@ -1132,7 +1131,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                     if (!ok) break;
                 } else {
                     for (int h = 0; h < 2; ++h) {
-                        ok = ok && wait_warp(s_full(s, h), ns & 1, abort_flag);
+                        ok = ok && wait_warp(s_full(s, h), ns & 1, abort_flag, a.wait_limit);
                         if (ok && lane == 0) tc::mbar_arrive(p_full(s, h));
                     }
                     if (!ok) break;
@@ -1142,14 +1141,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
             np += (uint32_t)(it.e1 - it.t0);
 
             // ---- the unit's end ----
-            if (cnt > 0) { ok = wait_warp(o_full(s), no & 1, abort_flag); ++no; if (!ok) break; }
+            if (cnt > 0) { ok = wait_warp(o_full(s), no & 1, abort_flag, a.wait_limit); ++no; if (!ok) break; }
             int c0 = 0, c1 = D;                            // this thread's columns
             float fa = 1.f, fb = 0.f;                      // factors of the slots' sums
             float M = m, L = l, add = lm;
             if (Q4 && !BF) fa = sigma;
             if (it.pair) {                                 // each thread joins half the columns of both slots
                 if (unread) {                              // (a slot without a tile of this unit has not waited for that yet)
-                    ok = wait_warp(parted, (nj - 1) & 1, abort_flag);
+                    ok = wait_warp(parted, (nj - 1) & 1, abort_flag, a.wait_limit);
                     unread = false;
                     if (!ok) break;
                 }
@@ -1158,7 +1157,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(joined);
-                ok = wait_warp(joined, nj & 1, abort_flag);
+                ok = wait_warp(joined, nj & 1, abort_flag, a.wait_limit);
                 if (!ok) break;
                 tc::fence_after_sync();
                 const float2 o = ml[(s ^ 1) * 128 + row];
@@ -1232,7 +1231,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                 __threadfence();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(delivered);
-                ok = wait_warp(delivered, nc & 1, abort_flag);
+                ok = wait_warp(delivered, nc & 1, abort_flag, a.wait_limit);
                 if (!ok) break;
                 if (tid == 0) {
                     unsigned long long *word = a.tickets + it.slot;
@@ -1242,7 +1241,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) prompt_attn_kernel(const __grid
                     s_last = last;
                     tc::mbar_arrive(counted);
                 }
-                ok = wait_warp(counted, nc & 1, abort_flag);
+                ok = wait_warp(counted, nc & 1, abort_flag, a.wait_limit);
                 ++nc;
                 if (!ok) break;
                 if (s_last && valid) {                     // join the pieces, in order

@@ -12,7 +12,7 @@ def join_waits():
     text = source()
     end = text.index("ml[s * 128 + row] =")
     text = text[text.rindex("o_full(s), no", 0, end):end]  # from the last product of the unit on
-    return re.search(r"if \(unread\) \{\s*ok = wait_warp\(parted, \(nj - 1\) & 1, abort_flag\);\s*unread = false;\s*if \(!ok\) break;", text) is not None
+    return re.search(r"if \(unread\) \{\s*ok = wait_warp\(parted, \(nj - 1\) & 1, abort_flag[^)]*\);\s*unread = false;\s*if \(!ok\) break;", text) is not None
 
 
 @pytest.mark.parametrize("stages", [2, 4])

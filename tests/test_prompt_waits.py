@@ -13,8 +13,8 @@ def weights_first():
     text = source()
     text = " ".join(text[:text.index("mma_16_ts(tO")].split()[-150:])
     late = re.search(r"const bool late = (u == \d+|true|false);", text)
-    assert late and re.search(r"if \(h == 0\) ok = wait_warp\(late \? p_bar : v_bar, late \? p_par : v_par, abort_flag\); "
-                              r"ok = ok && wait_warp\(late \? v_bar : p_bar, late \? v_par : p_par, abort_flag\); if \(!ok\) break;", text)
+    assert late and re.search(r"if \(h == 0\) ok = wait_warp\(late \? p_bar : v_bar, late \? p_par : v_par, abort_flag[^)]*\); "
+                              r"ok = ok && wait_warp\(late \? v_bar : p_bar, late \? v_par : p_par, abort_flag[^)]*\); if \(!ok\) break;", text)
     assert len(re.findall(r"wait_warp\(", text)) == 2
     return {"true": lambda u: True, "false": lambda u: False}.get(late[1], lambda u: u == int(late[1].split()[-1]))
 
