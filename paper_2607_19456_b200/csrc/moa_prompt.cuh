@@ -28,7 +28,7 @@
 // What bounds it: the softmax.  A tile of each slot takes its scheduler 2118 cycles when nothing else runs (1549
 // without the exponentials; a spilled register is an L2 round trip, since shared memory leaves no L1), the tensor
 // core 2048 in whole tiles and 3072 with the scores by halves, and beside MMA and copy warps a tile of both slots comes out at
-// 2700..3100 cycles: 951 GFLOP of two causal prompts (7001 and 8192 tokens, 32/8 heads of 128) in 0.90..1.03 ms, by the power that
+// 2700..3100 cycles: 951 GFLOP of two causal prompts (7001 and 8192 tokens, 32/8 heads of 128) in 0.94..1.06 ms, by the power that
 // is left, against 0.57 ms at the measured GEMM rate.  Rows of 64 halve the products, not the softmax.
 #pragma once
 
