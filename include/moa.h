@@ -380,8 +380,8 @@ int moa_paged_gather(const moa_paged_cache *cache, void *k_out, void *v_out, int
  * nothing), and bf16 weights are made to 2^-13.  How rows and keys are
  * cut follows from the sequences' lengths, the call's sizes (`tokens`, `batch`, heads; not `max_pages`) and the number of CTAs, and
  * the order of the sums from that: the same call gives the same bits.
- * A value that is not finite makes NaN or infinite: in q, the row; in k, the rows that see it (also those where the
- * definition makes its weight 0); in v, its feature in the rows that see it (NaN also where the definition has an infinity).  What a
+ * A value that is not finite (fp32: not below 2^127 in size) makes NaN or infinite: in q, the row; in k, the rows that see it (also
+ * those where the definition makes its weight 0); in v, its feature in the rows that see it (NaN also where the definition has an infinity).  What a
  * row does not see does not touch it.
  * `workspace`: device memory, 256-byte aligned, at least moa_prompt_workspace_bytes(...) bytes, contents
  * undefined on entry and exit; not to be shared by calls that can overlap on the GPU.
