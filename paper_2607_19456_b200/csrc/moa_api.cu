@@ -1330,8 +1330,8 @@ template <class C>
 static cudaError_t launch_prompt32_cfg(const PromptArgs &a, long long keys, const DeviceState &s, cudaStream_t st)
 {
     const int units = (int)(((long long)a.tokens * a.g / C::ROWS + a.batch) * a.h_kv);
-    // Many sequences: every CTA looks through the batch for starts that descend, so one takes several units (CTAs per SM that were tried: 16;
-    // 4000 prompts of 1..30 tokens 213 us, with a CTA for every unit 307 at a step on the way).
+    // Many sequences: every CTA looks through the batch for starts that descend, so one takes several units (4000 prompts of 1..30 tokens, at
+    // a step on the way: 16 CTAs for every SM 277 us, 2 to 8 286 to 290, a CTA for every unit 307).
     if (a.batch > kPrompt32Few) {
         const int most = 16 * s.sm_count;
         return launch_prompt32_cfg<C, true>(a, 1, units, units < most ? units : most, st);
